@@ -486,6 +486,146 @@ int slaq_shard_finalise_device(slaq_t* h, const int64_t* d_ties_before, int32_t*
 int slaq_allocate_static(const double* d_gain, int32_t n_jobs, int32_t max_cores_per_job, int64_t total_cores,
                          int32_t* d_out_alloc, double* d_out_reduction, void* cuda_stream);
 
+/*
+ * What a trainer computes beside the scheduler, on the scheduler's GPU.
+ *
+ * The paper's jobs compute their loss in every iteration anyway (Evaluation; it names multinomial logistic regression
+ * and perceptrons among them) and the scheduler reads it; how they compute it is theirs.  slaq_append_losses_device
+ * takes losses from trainers on this GPU; the calls below are the losses of such trainers, exact enough to be
+ * differenced, their gradient, and the step that makes them fall.  The paper has no counterpart.
+ *
+ * There is no handle but the AdamW plan: inputs and outputs are device buffers of the caller, the calls run on
+ * cuda_stream (cudaStream_t or NULL) of the current device, wait for nothing, allocate nothing, keep nothing for
+ * a later call and can be captured into a CUDA graph.  Buffers must stay valid until the stream has passed the call.
+ */
+enum {
+    SLAQ_F32 = 0,   /* element types */
+    SLAQ_BF16 = 1,
+    SLAQ_F16 = 2
+};
+
+/*
+ * Log probabilities of given tokens, and what else a row of logits says.  d_logits: `rows` rows of `vocab` elements of
+ * `type`, row r at element r x row_stride, any alignment, rows may overlap.  With z = scale x:
+ * d_out_logprob [rows]: ln softmax(z)[target];  d_out_entropy [rows]: entropy of softmax(z) in nats;
+ * d_out_norm [rows][2]: largest logit m and sum of exp(scale (x - m)), what slaq_token_logprobs_grad asks for;
+ * d_out_top_ids / d_out_top_logprobs [rows][top], 0 <= top <= 32: the tokens of the largest logits, largest first, equal
+ * ones lowest id first, NaN above everything; places beyond the vocabulary get -1 and -inf.
+ * Each of the three first outputs may be NULL.  d_targets may be NULL (no d_out_logprob then; every row is asked for).
+ * A negative target: the row is not asked for and not read; 0 in the first three outputs, -1 and -inf in the last two.
+ * A logit of -inf is a masked token (probability 0).  A row of nothing else has log probability -inf, entropy 0 and norm
+ * (-inf, 0).  A target of vocab or more gives the log probability NaN; a row with a NaN or +inf gives NaN throughout, its
+ * top_ids excepted.
+ * Errors: SLAQ_E_ARG (null, negative counts, vocab < 1, scale not positive and finite, unknown type, unaligned element),
+ * SLAQ_E_RANGE (vocab > 2^22, top > 32, 2^31 rows or more), SLAQ_E_CUDA.
+ */
+int slaq_token_logprobs(const void* d_logits, int type, int64_t rows, int32_t vocab, int64_t row_stride, const int64_t* d_targets,
+                        float scale, float* d_out_logprob, float* d_out_entropy, float* d_out_norm, int32_t top,
+                        int32_t* d_out_top_ids, float* d_out_top_logprobs, void* cuda_stream);
+
+/*
+ * Gradient of sum_r g_r logprob_r + h_r entropy_r with respect to the logits, g = d_grad_logprob [rows], h =
+ * d_grad_entropy [rows] (may be NULL; otherwise d_entropy [rows] is wanted), from the d_norm that slaq_token_logprobs left.
+ * d_out_grad: rows of the logits' type at grad_stride >= vocab; it may be the logits themselves (same pointer and
+ * stride), or rows that alternate with them at the same stride; any other overlap is refused.
+ * A row with a negative target or of masked tokens only gets zeros, a target of vocab or more or a NaN norm gives NaN.
+ * Errors as above.
+ */
+int slaq_token_logprobs_grad(const void* d_logits, int type, int64_t rows, int32_t vocab, int64_t row_stride,
+                             const int64_t* d_targets, float scale, const float* d_norm, const float* d_entropy,
+                             const float* d_grad_logprob, const float* d_grad_entropy, void* d_out_grad, int64_t grad_stride,
+                             void* cuda_stream);
+
+/*
+ * Both at once, for losses whose factors g = d_row_grad [rows] are known beforehand (slaq_job_row_grad): log probabilities
+ * (d_out_logprob may be NULL) and the gradient of sum_r g_r logprob_r, the logits being read once where a row fits on the chip.
+ */
+int slaq_token_loss(const void* d_logits, int type, int64_t rows, int32_t vocab, int64_t row_stride, const int64_t* d_targets,
+                    float scale, const float* d_row_grad, float* d_out_logprob, void* d_out_grad, int64_t grad_stride,
+                    void* cuda_stream);
+
+/*
+ * Mean losses of jobs.  Job j owns rows d_offsets[j] .. d_offsets[j+1) of `rows` rows (d_offsets [n_jobs + 1], not falling);
+ * a row counts with d_weights[r] (NULL: 1), and not at all if its target is negative (d_targets may be NULL) or its weight 0.
+ * slaq_job_losses: d_out_losses[j] = -sum w logprob / sum w, in 64 bits, always summed in the same order.
+ * slaq_job_row_grad: d_out_row_grad[r] = -w_r / sum w of the row's job: the loss's derivative by the row's log
+ * probability.  Rows that belong to no job are left as they were.
+ * A job without a row that counts has loss NaN, and so has one whose offsets leave 0 .. rows or fall (its rows are not
+ * touched).  Errors: SLAQ_E_ARG, SLAQ_E_CUDA.
+ */
+int slaq_job_row_grad(int32_t n_jobs, const int64_t* d_offsets, int64_t rows, const int64_t* d_targets, const float* d_weights,
+                      float* d_out_row_grad, void* cuda_stream);
+int slaq_job_losses(int32_t n_jobs, const int64_t* d_offsets, int64_t rows, const int64_t* d_targets, const float* d_logprob,
+                    const float* d_weights, double* d_out_losses, void* cuda_stream);
+/*
+ * slaq_job_losses on the handle's stream and slaq_append_losses_device of its result: entry i is the new loss of job
+ * d_job_ids[i].  d_out_losses [n] receives the losses.  A loss that is not finite is skipped and reported as there.
+ */
+int slaq_append_token_losses(slaq_t* h, int32_t n, const int32_t* d_job_ids, const int64_t* d_offsets, int64_t rows,
+                             const int64_t* d_targets, const float* d_logprob, const float* d_weights,
+                             const double* d_iter_times, const int32_t* d_cores_used, double* d_out_losses);
+
+/*
+ * AdamW over the tensors of many jobs in one launch.  A plan holds the tensors' addresses and, per group (usually a job),
+ * the step's numbers and the count of its steps; the tensors are the caller's.  Per element, in 32 bits:
+ *   g = grad x grad_scale;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g g;  t = the group's steps, this one included
+ *   p = p (1 - lr weight_decay) - lr / (1 - b1^t) x m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+ * param of type param_type, grad of that type or SLAQ_F32 (grad_type).  With a master copy (fp32; all tensors have one or
+ * none has) the step works on it and param receives its rounding.
+ * state_bits 32: exp_avg = m and exp_avg_sq = v are float [n].
+ * state_bits 8: both are e4m3 codes [n]; elements 256 b .. 256 b + 255 share the scales [b] ([ceil(n / 256)] floats):
+ * m = code x exp_avg_scale, sqrt(v) = code x exp_avg_sq_scale.  A block's scale is its largest (finite) value / 448, and 0, with
+ * its codes, where that value is below 2^-100.  Rounded to nearest; a non-zero second moment never rounds to zero.
+ */
+typedef struct slaq_adamw_tensor {
+    void* param;
+    const void* grad;
+    float* master;           /* NULL without master copies */
+    void* exp_avg;
+    void* exp_avg_sq;
+    float* exp_avg_scale;    /* NULL with 32-bit states */
+    float* exp_avg_sq_scale;
+    int64_t n;               /* elements; 0 is allowed, its pointers are not looked at then */
+    int32_t group;
+    int32_t reserved;
+} slaq_adamw_tensor;
+typedef struct slaq_adamw_group {
+    double lr, beta1, beta2, eps, weight_decay;   /* lr, eps, weight_decay >= 0; betas in [0, 1) */
+    double grad_scale;                            /* factor of the gradients, 1 for none */
+    int64_t step;                                 /* steps taken so far */
+} slaq_adamw_group;
+typedef struct slaq_adamw_handle slaq_adamw_t;
+
+/*
+ * Make a plan.  dev_ws: NULL (the library allocates), or device memory of the caller, 256-byte aligned and
+ * slaq_adamw_workspace_bytes() long, that outlives the plan.  Host arrays; the call returns when the plan is on the device and
+ * must not be captured.  Any alignment of the tensors that suits their type will do.
+ * Errors: SLAQ_E_ARG (null, unknown types, a group out of range, betas outside [0, 1), a tensor listed twice, tensors that
+ * overlap one another or a gradient), SLAQ_E_RANGE (2^40 elements, or 2^39 in all), SLAQ_E_NOMEM, SLAQ_E_CUDA.
+ */
+int slaq_adamw_create(void* dev_ws, size_t bytes, int32_t n_tensors, const slaq_adamw_tensor* tensors, int32_t n_groups,
+                      const slaq_adamw_group* groups, int param_type, int grad_type, int state_bits, void* cuda_stream,
+                      slaq_adamw_t** out);
+/* Bytes slaq_adamw_create needs for tensors of these sizes (0 for sizes outside the limits).  Host arithmetic only. */
+size_t slaq_adamw_workspace_bytes(int32_t n_tensors, const int64_t* numels, int32_t n_groups);
+/* Release the plan (NULL is accepted).  With a workspace of the caller, its steps must have ended. */
+int slaq_adamw_destroy(slaq_adamw_t* h);
+/* Message for the last error of h. */
+const char* slaq_adamw_last_error(const slaq_adamw_t* h);
+/*
+ * One step, asynchronous on cuda_stream.  d_active (device, n_groups entries, or NULL for all): groups with an entry
+ * above 0 are stepped, the others' tensors and counts stay as they are: with a group per job this is the d_out_alloc of
+ * slaq_schedule_device, and a job without cores keeps its weights.  Steps of one plan must run one after the other (one
+ * stream, or ordered streams), replayed graphs included.  Errors: SLAQ_E_ARG, SLAQ_E_CUDA.
+ */
+int slaq_adamw_step(slaq_adamw_t* h, const int32_t* d_active, void* cuda_stream);
+/* New numbers of a group from the next step on, in the stream's order; step < 0 keeps the count.  Errors: SLAQ_E_ARG, SLAQ_E_RANGE, SLAQ_E_CUDA. */
+int slaq_adamw_set_group(slaq_adamw_t* h, int32_t group, const slaq_adamw_group* g, void* cuda_stream);
+/* Other gradients (host array of n_tensors device addresses) from the next step on, in the stream's order; not while it is captured. */
+int slaq_adamw_set_grads(slaq_adamw_t* h, const void* const* grads, void* cuda_stream);
+/* Steps taken per group (host, n_groups entries); waits for the stream. */
+int slaq_adamw_get_steps(slaq_adamw_t* h, int64_t* out_steps, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

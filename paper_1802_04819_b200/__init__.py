@@ -11,3 +11,4 @@ from .binding import (  # noqa: F401
 )
 from .build import build  # noqa: F401
 from .sharded import LocalExchange, ProcessGroupExchange, schedule_sharded  # noqa: F401
+from .training import AdamW, TokenLogprobs, job_losses, job_row_grad, token_logprobs, token_logprobs_grad, token_loss  # noqa: F401

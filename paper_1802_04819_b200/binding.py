@@ -31,6 +31,9 @@ EXPORTED_SYMBOLS = [
     "slaq_import_state", "slaq_allocate_static", "slaq_get_active_count", "slaq_shard_predict", "slaq_shard_histogram",
     "slaq_shard_pick", "slaq_shard_pass", "slaq_shard_count", "slaq_shard_finalise", "slaq_shard_count_device",
     "slaq_shard_finalise_device", "slaq_schedule_group",
+    "slaq_token_logprobs", "slaq_token_logprobs_grad", "slaq_token_loss", "slaq_job_row_grad", "slaq_job_losses",
+    "slaq_append_token_losses", "slaq_adamw_create", "slaq_adamw_workspace_bytes", "slaq_adamw_destroy",
+    "slaq_adamw_last_error", "slaq_adamw_step", "slaq_adamw_set_group", "slaq_adamw_set_grads", "slaq_adamw_get_steps",
 ]
 
 
@@ -120,6 +123,20 @@ def load_library(variant: str | None = None):
         "slaq_shard_count_device": (c_int, [vp, vp]),
         "slaq_shard_finalise_device": (c_int, [vp, vp, vp]),
         "slaq_schedule_group": (c_int, [vp, c_int32, c_double, c_int64, vp]),
+        "slaq_token_logprobs": (c_int, [vp, c_int, c_int64, c_int32, c_int64, vp, c_float, vp, vp, vp, c_int32, vp, vp, vp]),
+        "slaq_token_logprobs_grad": (c_int, [vp, c_int, c_int64, c_int32, c_int64, vp, c_float, vp, vp, vp, vp, vp, c_int64, vp]),
+        "slaq_token_loss": (c_int, [vp, c_int, c_int64, c_int32, c_int64, vp, c_float, vp, vp, vp, c_int64, vp]),
+        "slaq_job_row_grad": (c_int, [c_int32, vp, c_int64, vp, vp, vp, vp]),
+        "slaq_job_losses": (c_int, [c_int32, vp, c_int64, vp, vp, vp, vp, vp]),
+        "slaq_append_token_losses": (c_int, [vp, c_int32, vp, vp, c_int64, vp, vp, vp, vp, vp, vp]),
+        "slaq_adamw_create": (c_int, [vp, c_size_t, c_int32, vp, c_int32, vp, c_int, c_int, c_int, vp, POINTER(vp)]),
+        "slaq_adamw_workspace_bytes": (c_size_t, [c_int32, vp, c_int32]),
+        "slaq_adamw_destroy": (c_int, [vp]),
+        "slaq_adamw_last_error": (c_char_p, [vp]),
+        "slaq_adamw_step": (c_int, [vp, vp, vp]),
+        "slaq_adamw_set_group": (c_int, [vp, c_int32, vp, vp]),
+        "slaq_adamw_set_grads": (c_int, [vp, vp, vp]),
+        "slaq_adamw_get_steps": (c_int, [vp, vp, vp]),
     }
     sig["slaq_result_take"] = (vp, [c_size_t])      # page-locked memory for results, internal to the binding
     sig["slaq_result_give"] = (None, [vp])
@@ -282,6 +299,13 @@ class Scheduler:
         assert d_job_ids.is_contiguous() and d_losses.is_contiguous() and d_job_ids.numel() == d_losses.numel()
         return self._check(self._lib.slaq_append_losses_device(self._h, d_job_ids.numel(), ptr(d_job_ids), ptr(d_losses),
                                                                ptr(d_iter_times), ptr(d_cores_used)))
+
+    def append_token_losses(self, d_job_ids, offsets, targets, logprob, weights=None, d_iter_times=None, d_cores_used=None,
+                            out=None):
+        """The mean loss of each listed job over its rows (see ``job_losses``) as its new iteration, from torch CUDA
+        tensors, asynchronous on the handle's stream; returns the losses (float64, ``out`` if given)."""
+        from .training import append_token_losses
+        return append_token_losses(self, d_job_ids, offsets, targets, logprob, weights, d_iter_times, d_cores_used, out)
 
     def load_histories(self, job_ids, offsets, losses, k_last, m_seen=None, packed=False):
         ids, off = _arr(job_ids, np.int32), _arr(offsets, np.int64)

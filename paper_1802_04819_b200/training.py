@@ -1,0 +1,360 @@
+"""What a trainer computes beside the scheduler, on torch CUDA tensors: same names as the C ABI, argument marshalling only.
+
+A training step of many jobs whose logits lie in one matrix, job j's rows being ``offsets[j] .. offsets[j + 1]``:
+
+    row_grad = slaq.job_row_grad(offsets, targets)                    # derivative of each job's mean loss by its rows
+    logprob, grad = slaq.token_loss(logits, targets, row_grad)        # log probabilities, gradient by the logits
+    sched.append_token_losses(job_ids, offsets, targets, logprob)     # the jobs' losses, into their histories
+    ...                                                               # the model's own backward pass
+    adamw.step(active=alloc)                                          # only the jobs that were given cores
+
+Every call is asynchronous on ``stream`` (a torch stream or a raw cudaStream_t; default: torch's current stream of the
+tensors' device).  Results that are not given as ``out`` are allocated by torch.  Refusals raise ``SlaqError``.
+"""
+
+from __future__ import annotations
+
+import contextlib
+import ctypes
+from ctypes import c_double, c_int32, c_int64, c_void_p
+from typing import NamedTuple
+
+import numpy as np
+
+from .binding import SlaqError, load_library
+
+F32, BF16, F16 = 0, 1, 2
+MAX_VOCAB, MAX_TOP = 1 << 22, 32
+STATE_BLOCK = 256
+
+_torch = None
+_types = {}
+
+
+def _load():
+    global _torch
+    if _torch is None:
+        import torch
+        _types.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+        _torch = torch
+    return _torch
+
+
+_MESSAGES = {-1: "bad argument", -2: f"a size beyond the limits (vocabulary {MAX_VOCAB}, top {MAX_TOP}, 2^31 rows)", -4: "out of memory",
+             -5: "a CUDA call failed"}
+
+
+def _refuse(message):
+    raise SlaqError(-1, message)
+
+
+def _check(rc, message=None):
+    if rc < 0:
+        raise SlaqError(rc, message or _MESSAGES.get(rc, "error"))
+    return rc
+
+
+def _vector(t, name, dtype, n, device):
+    """A contiguous tensor of n entries; None passes."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != device or t.numel() != n or not t.is_contiguous():
+        _refuse(f"{name} is not a contiguous {dtype} tensor of {n} entries on {device}")
+    return t.data_ptr()
+
+
+def _matrix(t, name):
+    if t.dim() != 2 or not t.is_cuda or t.dtype not in _types:
+        _refuse(f"{name} is not a matrix of fp32, bf16 or fp16 on a GPU")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        _refuse(f"the elements of a row of {name} are not next to one another")
+    if t.shape[1] < 1:
+        _refuse("an empty vocabulary")
+    return t.data_ptr(), _types[t.dtype], t.shape[0], t.shape[1], t.stride(0)
+
+
+@contextlib.contextmanager
+def _elsewhere(stream, device):
+    """Another stream than torch's current one, or another device: what is allocated there belongs there."""
+    torch = _load()
+    with torch.cuda.device(device):
+        if stream is None:
+            yield torch.cuda.current_stream().cuda_stream
+        elif isinstance(stream, int):
+            with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
+                yield stream
+        else:
+            with torch.cuda.stream(stream):
+                yield stream.cuda_stream
+
+
+class _Here:
+    """The common case: the current stream of the current device."""
+
+    def __init__(self, raw):
+        self.raw = raw
+
+    def __enter__(self):
+        return self.raw
+
+    def __exit__(self, *exc):
+        return False
+
+
+def _on(stream, device):
+    torch = _load()
+    if stream is None and device.index == torch.cuda.current_device():
+        return _Here(torch.cuda.current_stream().cuda_stream)
+    return _elsewhere(stream, device)
+
+
+class TokenLogprobs(NamedTuple):
+    logprob: object          # [rows] float32, None without targets
+    entropy: object          # [rows] float32
+    norm: object             # [rows, 2] float32: largest logit, sum of exp(scale (x - largest)); for token_logprobs_grad
+    top_ids: object          # [rows, top] int32, None without top
+    top_logprobs: object     # [rows, top] float32
+
+
+def token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, stream=None) -> TokenLogprobs:
+    """slaq_token_logprobs: ``logits`` [rows, vocab] fp32 / bf16 / fp16 with any row stride, ``targets`` int64 [rows] (negative:
+    the row is not asked for) or None, ``top`` alternatives (0 .. 32), ``scale`` the inverse temperature."""
+    torch = _load()
+    x, kind, rows, vocab, pitch = _matrix(logits, "logits")
+    device = logits.device
+    t = _vector(targets, "targets", torch.int64, rows, device)
+    if not 0 <= top <= MAX_TOP:
+        raise SlaqError(-1 if top < 0 else -2, f"top is 0 .. {MAX_TOP}")
+    with _on(stream, device) as raw:
+        out = torch.empty(4 * rows, dtype=torch.float32, device=device)
+        logprob, entropy, norm = out[:rows], out[rows:2 * rows], out[2 * rows:].view(rows, 2)
+        ids = torch.empty(rows, top, dtype=torch.int32, device=device) if top else None
+        best = torch.empty(rows, top, dtype=torch.float32, device=device) if top else None
+        base = out.data_ptr()
+        _check(load_library().slaq_token_logprobs(
+            x, kind, rows, vocab, pitch, t, scale, None if t is None else base, base + 4 * rows, base + 8 * rows, top,
+            ids.data_ptr() if top else None, best.data_ptr() if top else None, raw))
+    return TokenLogprobs(None if t is None else logprob, entropy, norm, ids, best)
+
+
+def _gradient(out, logits):
+    if out is None:
+        return _load().empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    if out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device or (out.shape[1] > 1 and out.stride(1) != 1):
+        _refuse("out is not a matrix like logits with its rows' elements next to one another")
+    return out
+
+
+def token_logprobs_grad(logits, targets, norm, grad_logprob, entropy=None, grad_entropy=None, scale: float = 1.0, out=None, stream=None):
+    """slaq_token_logprobs_grad: gradient of sum(grad_logprob x logprob + grad_entropy x entropy) by the logits, from what
+    ``token_logprobs`` returned.  ``out`` may be ``logits`` itself."""
+    torch = _load()
+    x, kind, rows, vocab, pitch = _matrix(logits, "logits")
+    device = logits.device
+    t = _vector(targets, "targets", torch.int64, rows, device)
+    n, g = _vector(norm, "norm", torch.float32, 2 * rows, device), _vector(grad_logprob, "grad_logprob", torch.float32, rows, device)
+    e, h = _vector(entropy, "entropy", torch.float32, rows, device), _vector(grad_entropy, "grad_entropy", torch.float32, rows, device)
+    with _on(stream, device) as raw:
+        out = _gradient(out, logits)
+        _check(load_library().slaq_token_logprobs_grad(x, kind, rows, vocab, pitch, t, scale, n, e, g, h, out.data_ptr(), out.stride(0), raw),
+               "bad argument: a missing input, a scale that is not positive, or a gradient that overlaps the logits otherwise than row for row")
+    return out
+
+
+def token_loss(logits, targets, row_grad, scale: float = 1.0, out=None, stream=None):
+    """slaq_token_loss: (log probabilities, gradient of sum(row_grad x logprob) by the logits) in one call."""
+    torch = _load()
+    x, kind, rows, vocab, pitch = _matrix(logits, "logits")
+    device = logits.device
+    t, g = _vector(targets, "targets", torch.int64, rows, device), _vector(row_grad, "row_grad", torch.float32, rows, device)
+    with _on(stream, device) as raw:
+        out = _gradient(out, logits)
+        logprob = torch.empty(rows, dtype=torch.float32, device=device)
+        _check(load_library().slaq_token_loss(x, kind, rows, vocab, pitch, t, scale, g, logprob.data_ptr(), out.data_ptr(), out.stride(0), raw),
+               "bad argument: a missing input, a scale that is not positive, or a gradient that overlaps the logits otherwise than row for row")
+    return logprob, out
+
+
+def job_row_grad(offsets, targets=None, weights=None, out=None, stream=None):
+    """slaq_job_row_grad: the derivative of each job's mean loss by the log probability of each of its rows (float32 [rows]).
+    ``offsets`` int64 [jobs + 1]; rows of no job keep what ``out`` holds (zeros without ``out``)."""
+    torch = _load()
+    known = next((t for t in (targets, weights, out) if t is not None), None)
+    if known is None:
+        _refuse("the number of rows follows from targets, weights or out: one of them is wanted")
+    rows, device = known.numel(), offsets.device
+    t, w = _vector(targets, "targets", torch.int64, rows, device), _vector(weights, "weights", torch.float32, rows, device)
+    off = _vector(offsets, "offsets", torch.int64, max(offsets.numel(), 1), device)
+    with _on(stream, device) as raw:
+        if out is None:
+            out = torch.zeros(rows, dtype=torch.float32, device=device)
+        _check(load_library().slaq_job_row_grad(offsets.numel() - 1, off, rows, t, w, _vector(out, "out", torch.float32, rows, device), raw))
+    return out
+
+
+def _job_inputs(offsets, targets, logprob, weights):
+    torch = _load()
+    rows, device = logprob.numel(), logprob.device
+    return (_vector(offsets, "offsets", torch.int64, max(offsets.numel(), 1), device), rows, _vector(targets, "targets", torch.int64, rows, device),
+            _vector(logprob, "logprob", torch.float32, rows, device), _vector(weights, "weights", torch.float32, rows, device))
+
+
+def job_losses(offsets, targets, logprob, weights=None, out=None, stream=None):
+    """slaq_job_losses: float64 [jobs], the weighted mean of -logprob over each job's rows that count."""
+    torch = _load()
+    off, rows, t, lp, w = _job_inputs(offsets, targets, logprob, weights)
+    n = offsets.numel() - 1
+    with _on(stream, logprob.device) as raw:
+        if out is None:
+            out = torch.empty(max(n, 0), dtype=torch.float64, device=logprob.device)
+        _check(load_library().slaq_job_losses(n, off, rows, t, lp, w, _vector(out, "out", torch.float64, n, logprob.device), raw))
+    return out
+
+
+def append_token_losses(sched, d_job_ids, offsets, targets, logprob, weights, d_iter_times, d_cores_used, out):
+    torch = _load()
+    n, device = d_job_ids.numel(), logprob.device
+    off, rows, t, lp, w = _job_inputs(offsets, targets, logprob, weights)
+    if offsets.numel() != n + 1:
+        _refuse("offsets has one entry more than there are jobs")
+    if out is None:
+        out = torch.empty(n, dtype=torch.float64, device=device)
+    sched._check(sched._lib.slaq_append_token_losses(
+        sched._h, n, _vector(d_job_ids, "job ids", torch.int32, n, device), off, rows, t, lp, w,
+        _vector(d_iter_times, "iteration times", torch.float64, n, device), _vector(d_cores_used, "cores", torch.int32, n, device),
+        _vector(out, "out", torch.float64, n, device)))
+    return out
+
+
+class _Tensor(ctypes.Structure):
+    _fields_ = [("param", c_void_p), ("grad", c_void_p), ("master", c_void_p), ("exp_avg", c_void_p), ("exp_avg_sq", c_void_p),
+                ("exp_avg_scale", c_void_p), ("exp_avg_sq_scale", c_void_p), ("n", c_int64), ("group", c_int32), ("reserved", c_int32)]
+
+
+class _Group(ctypes.Structure):
+    _fields_ = [("lr", c_double), ("beta1", c_double), ("beta2", c_double), ("eps", c_double), ("weight_decay", c_double),
+                ("grad_scale", c_double), ("step", c_int64)]
+
+
+def _group(lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=1.0, step=0):
+    return _Group(lr, betas[0], betas[1], eps, weight_decay, grad_scale, step)
+
+
+class AdamW:
+    """A plan of slaq_adamw_*: one step over all tensors is one launch.
+
+    ``params`` and ``grads``: lists of contiguous CUDA tensors (fp32, bf16 or fp16; gradients of the weights' type or fp32);
+    ``group_of``: the group of each tensor (default: all 0); ``groups``: a list of dicts with ``lr``, ``betas``, ``eps``,
+    ``weight_decay``, ``grad_scale``, ``step`` (any may be left out).  ``masters``: fp32 copies that the step works on, the
+    weights being their rounding.  ``state_bits`` 32 (fp32 states) or 8 (float8_e4m3fn codes with a float32 scale per 256
+    elements, the second moment as its square root).  States are made as zeros, or taken over as lists: ``exp_avg``,
+    ``exp_avg_sq`` and, in 8 bits, ``exp_avg_scale``, ``exp_avg_sq_scale``; they are attributes of the same names."""
+
+    def __init__(self, params, grads, group_of=None, groups=None, state_bits: int = 32, masters=None, exp_avg=None, exp_avg_sq=None,
+                 exp_avg_scale=None, exp_avg_sq_scale=None, stream=None):
+        torch = _load()
+        self._h = c_void_p()
+        self._lib = load_library()
+        params, n = list(params), len(params)
+        if not params:
+            _refuse("a plan without tensors")
+        device, kind = params[0].device, params[0].dtype
+        if state_bits not in (8, 32):
+            _refuse("states are kept in 8 or in 32 bits")
+        state, eight = (torch.float8_e4m3fn, True) if state_bits == 8 else (torch.float32, False)
+        group_of = [0] * n if group_of is None else [int(g) for g in group_of]
+        self._groups = [dict(g) for g in ([{}] if groups is None else groups)]
+        groups = [_group(**g) for g in self._groups]
+        grads = list(grads)
+        if kind not in _types or not params[0].is_cuda or len(grads) != n or len(group_of) != n or not groups:
+            _refuse("parameters are fp32, bf16 or fp16 tensors on a GPU, with a gradient and a group each")
+
+        with _on(stream, device) as raw:
+            def states(given, dtype, count):
+                return [torch.zeros(count(p), device=device).to(dtype) for p in params] if given is None else list(given)
+            blocks = lambda p: -(-p.numel() // STATE_BLOCK)   # noqa: E731
+            self.exp_avg = states(exp_avg, state, lambda p: p.numel())
+            self.exp_avg_sq = states(exp_avg_sq, state, lambda p: p.numel())
+            self.exp_avg_scale = states(exp_avg_scale, torch.float32, blocks) if eight else None
+            self.exp_avg_sq_scale = states(exp_avg_sq_scale, torch.float32, blocks) if eight else None
+            self.params, self.grads, self.masters = params, grads, None if masters is None else list(masters)
+            grad_kind = grads[0].dtype
+            if grad_kind not in (kind, torch.float32):
+                _refuse("gradients are of the parameters' type or fp32")
+            lists = [("params", params, kind), ("grads", grads, grad_kind), ("masters", self.masters, torch.float32),
+                     ("exp_avg", self.exp_avg, state), ("exp_avg_sq", self.exp_avg_sq, state)]
+            table = (_Tensor * n)()
+            for name, field, tensors, dtype in [(f, {"params": "param", "grads": "grad", "masters": "master"}.get(f, f), ts, d) for f, ts, d in lists]:
+                if tensors is None:
+                    continue
+                if len(tensors) != n:
+                    _refuse(f"{name} has another length than params")
+                for row, p, t in zip(table, params, tensors):
+                    setattr(row, field, _vector(t, name, dtype, p.numel(), device))
+            if eight:
+                for name, tensors in (("exp_avg_scale", self.exp_avg_scale), ("exp_avg_sq_scale", self.exp_avg_sq_scale)):
+                    if len(tensors) != n:
+                        _refuse(f"{name} has another length than params")
+                    for row, p, t in zip(table, params, tensors):
+                        setattr(row, name, _vector(t, name, torch.float32, blocks(p), device))
+            for row, p, k in zip(table, params, group_of):
+                row.n, row.group = p.numel(), k
+            numels = np.array([p.numel() for p in params], np.int64)
+            need = self._lib.slaq_adamw_workspace_bytes(n, numels.ctypes.data, len(groups))
+            self._ws = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
+            rc = self._lib.slaq_adamw_create(self._ws.data_ptr(), need, n, table, len(groups), (_Group * len(groups))(*groups),
+                                             _types[kind], _types[grad_kind], state_bits, raw, ctypes.byref(self._h))
+        _check(rc, {-1: "a group out of range, betas outside [0, 1), a tensor listed twice, or tensors that overlap"}.get(rc))
+        self._device, self._n_groups = device, len(groups)
+
+    def _ok(self, rc):
+        return _check(rc, self._lib.slaq_adamw_last_error(self._h).decode() if rc < 0 else None)
+
+    def step(self, active=None, stream=None):
+        """One step of the groups whose entry of ``active`` (int32 CUDA tensor [groups], for instance the allocation of
+        ``schedule_device``) is above 0; None: of all."""
+        a = None if active is None else _vector(active, "active", _load().int32, self._n_groups, self._device)
+        with _on(stream, self._device) as raw:
+            self._ok(self._lib.slaq_adamw_step(self._h, a, raw))
+
+    def set_group(self, group: int, stream=None, **values):
+        """New numbers of a group from the next step on; what is not named stays as it is, the count of steps too."""
+        if not 0 <= group < self._n_groups:
+            raise SlaqError(-2, "no such group")
+        merged = {**self._groups[group], **values}
+        with _on(stream, self._device) as raw:
+            self._ok(self._lib.slaq_adamw_set_group(self._h, group, ctypes.byref(_group(**{"step": -1, **{k: v for k, v in merged.items() if k != "step"}, **values})), raw))
+        self._groups[group] = merged
+
+    def set_grads(self, grads, stream=None):
+        """Other gradient tensors of the same types and sizes from the next step on."""
+        grads = list(grads)
+        if len(grads) != len(self.params):
+            _refuse("grads has another length than params")
+        for g, old in zip(grads, self.grads):
+            _vector(g, "grads", old.dtype, old.numel(), self._device)
+        rows = (c_void_p * len(grads))(*[g.data_ptr() for g in grads])
+        with _on(stream, self._device) as raw:
+            self._ok(self._lib.slaq_adamw_set_grads(self._h, rows, raw))
+        self.grads = grads
+
+    def get_steps(self, stream=None) -> np.ndarray:
+        """Steps taken per group; waits for the stream."""
+        out = np.empty(self._n_groups, np.int64)
+        with _on(stream, self._device) as raw:
+            self._ok(self._lib.slaq_adamw_get_steps(self._h, out.ctypes.data, raw))
+        return out
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._lib.slaq_adamw_destroy(self._h)
+            self._h = c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+__all__ = ["AdamW", "TokenLogprobs", "token_logprobs", "token_logprobs_grad", "token_loss", "job_row_grad", "job_losses"]
