@@ -4,15 +4,20 @@
 //     log probability  d_t - ln S          entropy  ln S - (sum exp(d_i) d_i) / S
 // Both terms of the entropy are non-negative, so nothing cancels.  What a later gradient needs of the row is kept as (m, S)
 // and not as m c + ln S: a sum near 20 would carry 1e-6 of rounding into every probability.
+#include <cooperative_groups.h>
+
 #include "slaq_internal.cuh"
 #include "slaq_rows.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace slaq {
 namespace {
 
-constexpr int kThreads = 256;
 constexpr int kMaxVocab = 1 << 22;
 constexpr int kMaxTop = 32;
+constexpr int kMaxCluster = 8;
+constexpr int kUnroll = 4;         // vectors that a thread has in flight
 
 struct RowArgs {
     const void* logits;
@@ -26,138 +31,523 @@ struct RowArgs {
     const float *g_logprob, *g_entropy, *in_norm, *in_entropy;
     void* grad;
     int64_t grad_stride;
+    int32_t slice;                 // vectors per block of a cluster
 };
 
-template <class T, class Op>
-__device__ T block_reduce(T v, T* shared, Op op) {
-    for (int o = 16; o; o >>= 1) v = op(v, __shfl_xor_sync(~0u, v, o));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = shared[0];
-    for (int w = 1; w < kThreads / 32; ++w) v = op(v, shared[w]);
-    return v;
-}
+template <class E>
+__device__ __forceinline__ const E* row_of(const RowArgs& a, int64_t row) { return static_cast<const E*>(a.logits) + row * a.stride; }
 
+// A row's outputs from its sums.
 struct RowStats {
     float m, s, log_s, entropy;
 };
-
-template <class E>
-__device__ RowStats row_stats(const E* x, int V, float scale, float* shared) {
-    auto plus = [](float a, float b) { return a + b; };
-    float m = -CUDART_INF_F;
-    for (int i = threadIdx.x; i < V; i += kThreads) m = max_nan(m, as_float(x[i]));
-    m = block_reduce(m, shared, [](float a, float b) { return max_nan(a, b); });
-    if (m != m || m == CUDART_INF_F) return {CUDART_NAN_F, CUDART_NAN_F, CUDART_NAN_F, CUDART_NAN_F};
-    if (m == -CUDART_INF_F) return {m, 0.0f, -CUDART_INF_F, 0.0f};
-    const float c = scale * kLog2E;
-    float s = 0.0f, u = 0.0f;
-    for (int i = threadIdx.x; i < V; i += kThreads) {
-        const float t = fmaxf((as_float(x[i]) - m) * c, -200.0f);
-        const float e = exp2_fast(t);
-        s += e;
-        u = fmaf(e, t, u);
+__device__ __forceinline__ RowStats stats_of(const Sums& a) {
+    if (a.m != a.m || a.m == CUDART_INF_F) return {CUDART_NAN_F, CUDART_NAN_F, CUDART_NAN_F, CUDART_NAN_F};
+    if (a.m == -CUDART_INF_F) return {a.m, 0.0f, -CUDART_INF_F, 0.0f};
+    const float log_s = logf(a.s);
+    return {a.m, a.s, log_s, log_s - a.u / a.s * kLn2};
+}
+// the log probability of an element x: -inf where the row or the element is masked
+__device__ __forceinline__ float logprob_of(float x, const RowStats& r, float scale) {
+    return r.m == -CUDART_INF_F ? r.m : (x - r.m) * scale - r.log_s;
+}
+__device__ __forceinline__ void write_stats(const RowArgs& a, int64_t row, int64_t t, float x_t, const RowStats& r) {
+    if (a.logprob) a.logprob[row] = t >= a.vocab ? CUDART_NAN_F : logprob_of(x_t, r, a.scale);
+    if (a.entropy) a.entropy[row] = r.entropy;
+    if (a.norm) reinterpret_cast<float2*>(a.norm)[row] = make_float2(r.m, r.s);
+}
+__device__ __forceinline__ void write_top(const RowArgs& a, int64_t row, int k, unsigned long long key, const RowStats& r) {
+    a.top_ids[row * a.top + k] = key ? (int)position_of(key) : -1;
+    a.top_logprobs[row * a.top + k] = key ? logprob_of(value_of((uint32_t)(key >> 32)), r, a.scale) : -CUDART_INF_F;
+}
+// a row that nobody asked for
+__device__ __forceinline__ void write_nothing(const RowArgs& a, int64_t row, int thread, int threads) {
+    if (thread == 0) {
+        if (a.logprob) a.logprob[row] = 0.0f;
+        if (a.entropy) a.entropy[row] = 0.0f;
+        if (a.norm) reinterpret_cast<float2*>(a.norm)[row] = make_float2(0.0f, 0.0f);
     }
-    s = block_reduce(s, shared, plus);
-    u = block_reduce(u, shared, plus);
-    return {m, s, logf(s), logf(s) - u / s * 0.6931471805599453f};
+    for (int k = thread; k < a.top; k += threads) {
+        a.top_ids[row * a.top + k] = -1;
+        a.top_logprobs[row * a.top + k] = -CUDART_INF_F;
+    }
 }
 
-// the log probability of token t: NaN if there is no such token, -inf where the row or the token is masked
-template <class E>
-__device__ float given(const E* x, int V, int64_t t, const RowStats& r, float scale) {
-    if (t >= V) return CUDART_NAN_F;
-    if (r.m == -CUDART_INF_F) return r.m;
-    return (as_float(x[t]) - r.m) * scale - r.log_s;
+// ---- the gradient of a row ----
+//
+// dx_i = c [ g (1[i = t] - p_i) - h p_i (ln p_i + H) ] with p_i = 2^t_i / S, t_i in units of log 2:
+//      = 2^t_i (A + B t_i) + 1[i = t] c g,     B = -h c ln 2 / S,   A = -(g + h (H - ln S)) c / S
+struct Gradient {
+    float base, c, A, B, at_target;
+    int target;
+    int kind;                      // 0: as above; 1: zeros (nobody asked, or nothing but masked tokens); 2: NaN (no such token)
+};
+__device__ __forceinline__ Gradient gradient_of(const RowArgs& a, int64_t t, float m, float s, float log_s, float entropy, float g, float h) {
+    Gradient r;
+    r.base = base_of(m);
+    r.c = a.scale * kLog2E;
+    r.target = (int)(t < a.vocab ? t : -1);
+    const float per = a.scale / s;
+    r.B = -h * per * kLn2;
+    r.A = -(h == 0.0f ? g : fmaf(h, entropy - log_s, g)) * per;
+    r.at_target = g * a.scale;
+    r.kind = t >= a.vocab ? 2 : t < 0 || m == -CUDART_INF_F ? 1 : 0;
+    return r;
 }
-
-template <class E>
-__global__ void __launch_bounds__(kThreads) logprobs_kernel(RowArgs a) {
-    __shared__ float shared[kThreads / 32];
-    __shared__ unsigned long long best[kThreads / 32];
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const E* const x = static_cast<const E*>(a.logits) + row * a.stride;
-        const int64_t t = a.targets ? a.targets[row] : 0;
-        if (t < 0) {   // nobody asked for this row
-            if (threadIdx.x == 0) {
-                if (a.logprob) a.logprob[row] = 0.0f;
-                if (a.entropy) a.entropy[row] = 0.0f;
-                if (a.norm) a.norm[2 * row] = a.norm[2 * row + 1] = 0.0f;
-            }
-            for (int k = threadIdx.x; k < a.top; k += kThreads) {
-                a.top_ids[row * a.top + k] = -1;
-                a.top_logprobs[row * a.top + k] = -CUDART_INF_F;
-            }
-            continue;
+template <bool kEntropy>
+__device__ __forceinline__ float gradient_at(const Gradient& r, float x, int i) {
+    if (r.kind) return r.kind == 1 ? 0.0f : CUDART_NAN_F;
+    float t = (x - r.base) * r.c, y = r.A;
+    if (kEntropy) {
+        t = t < kGone ? kGone : t;    // not fmaxf: NaN stays
+        y = fmaf(r.B, t, y);
+    }
+    y *= exp2_fast(t);
+    return i == r.target ? y + r.at_target : y;
+}
+// .. of the vector that begins with element `first`
+template <bool kEntropy, class E>
+__device__ __forceinline__ Vector<E> gradient_at(const Gradient& r, const Vector<E>& x, int first) {
+    constexpr int N = Vector<E>::N;
+    Vector<E> out;
+    if (r.kind) {
+        const Pair p = r.kind == 1 ? pair_of(0.0f, 0.0f) : pair_of(CUDART_NAN_F, CUDART_NAN_F);
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) out.put(i, p);
+        return out;
+    }
+    const Pair off = pair_of(-r.base, -r.base), by = pair_of(r.c, r.c), A = pair_of(r.A, r.A), B = pair_of(r.B, r.B);
+    const bool here = (unsigned)(r.target - first) < (unsigned)N;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        float p, q;
+        Pair t = (x.at(i) + off) * by, y = A;
+        split(t, p, q);
+        if (kEntropy) {
+            p = p < kGone ? kGone : p, q = q < kGone ? kGone : q;
+            y = fma2(B, pair_of(p, q), A);
         }
-        const RowStats r = row_stats(x, a.vocab, a.scale, shared);
-        if (threadIdx.x == 0) {
-            if (a.logprob) a.logprob[row] = given(x, a.vocab, t, r, a.scale);
-            if (a.entropy) a.entropy[row] = r.entropy;
-            if (a.norm) a.norm[2 * row] = r.m, a.norm[2 * row + 1] = r.s;
+        y = y * pair_of(exp2_fast(p), exp2_fast(q));
+        if (here) {
+            split(y, p, q);
+            if (r.target == first + 2 * i) p += r.at_target;
+            if (r.target == first + 2 * i + 1) q += r.at_target;
+            y = pair_of(p, q);
         }
-        unsigned long long last = ~0ull;
-        for (int k = 0; k < a.top; ++k) {
-            unsigned long long mine = 0;
-            for (int i = threadIdx.x; i < a.vocab; i += kThreads) {
-                const unsigned long long key = key_of(as_float(x[i]), i);
-                if (key < last && key > mine) mine = key;
+        out.put(i, y);
+    }
+    return out;
+}
+template <class E>
+__device__ __forceinline__ void store_whole(E* to, const Vector<E>& x) {
+    asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(to), "r"(x.w.x), "r"(x.w.y), "r"(x.w.z), "r"(x.w.w) : "memory");
+}
+template <class E>
+__device__ __forceinline__ void store_partial(E* row, const Row<E>& r, int v, const Vector<E>& x) {
+#pragma unroll
+    for (int k = 0; k < Vector<E>::N; ++k) {
+        const int i = r.first(v) + k;
+        if (i >= 0 && i < r.V) row[i] = reinterpret_cast<const E*>(&x.w)[k];
+    }
+}
+
+// ---- few elements a row: L lanes share one, N elements each, kept in registers ----
+template <class E, int L, int N, bool kGrad>
+__global__ void __launch_bounds__(256) narrow_kernel(RowArgs a) {
+    const int sub = threadIdx.x % L;
+    const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
+    const bool real = row < a.rows;
+    const int64_t t = !real ? -1 : a.targets ? a.targets[row] : 0;
+    const E* const from = row_of<E>(a, real ? row : 0);
+    const float c = a.scale * kLog2E;
+    float x[N], m = -CUDART_INF_F;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int i = sub + k * L;
+        x[k] = t >= 0 && i < a.vocab ? as_float(from[i]) : -CUDART_INF_F;
+        m = max_nan(m, x[k]);
+    }
+    const float x_t = t >= 0 && t < a.vocab ? as_float(from[t]) : 0.0f;   // before a gradient takes its place
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(~0u, m, o));
+    Sums all = {m, 0.0f, 0.0f};
+    const float base = base_of(m);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const float d = fmaxf((x[k] - base) * c, kGone), e = exp2_fast(d);
+        all.s += e;
+        all.u = fmaf(e, d, all.u);
+    }
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) {
+        all.s += __shfl_xor_sync(~0u, all.s, o);
+        all.u += __shfl_xor_sync(~0u, all.u, o);
+    }
+    const RowStats r = stats_of(all);
+    if (real && sub == 0) {
+        if (t < 0) write_nothing(a, row, 0, 1);
+        else write_stats(a, row, t, x_t, r);
+    }
+    if (kGrad) {
+        __syncwarp();                  // the row's logits have been read by all of its lanes
+        if (!real) return;
+        const Gradient y = gradient_of(a, t, r.m, r.s, r.log_s, 0.0f, a.g_logprob[row], 0.0f);
+        E* const to = static_cast<E*>(a.grad) + row * a.grad_stride;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int i = sub + k * L;
+            if (i < a.vocab) to[i] = from_float<E>(gradient_at<false>(y, x[k], i));
+        }
+        return;
+    }
+    unsigned long long last = ~0ull;
+    for (int n = 0; n < a.top; ++n) {
+        unsigned long long best = 0;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int i = sub + k * L;
+            const unsigned long long key = i < a.vocab ? key_of(x[k], i) : 0;
+            if (key < last && key > best) best = key;
+        }
+#pragma unroll
+        for (int o = L / 2; o; o >>= 1) {
+            const unsigned long long other = __shfl_xor_sync(~0u, best, o);
+            best = other > best ? other : best;
+        }
+        if (real && t >= 0 && sub == 0) write_top(a, row, n, best, r);
+        last = best ? best : 1;        // the row has no more: every later key is below
+    }
+}
+
+// ---- a row that a warp holds in registers: 4 vectors a lane ----
+template <class E, bool kGrad>
+__global__ void __launch_bounds__(128) warp_kernel(RowArgs a) {
+    __shared__ unsigned long long shared[4][32];
+    const int lane = threadIdx.x & 31;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (row >= a.rows) return;
+    const int64_t t = a.targets ? a.targets[row] : 0;
+    const Row<E> x(row_of<E>(a, row), a.vocab);
+    const float c = a.scale * kLog2E;
+    Vector<E> v[kUnroll];
+    Sums all = {-CUDART_INF_F, 0.0f, 0.0f};
+    RowStats r = {0.0f, 0.0f, 0.0f, 0.0f};
+    float mine = -CUDART_INF_F;
+    if (t >= 0) {
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) v[k] = x.load(k * 32 + lane);
+        const float x_t = t < a.vocab ? as_float(x.x[t]) : 0.0f;
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) mine = max_nan(mine, v[k].max());
+        add_vectors<!kGrad>(all, v, warp_max_nan(mine), c);     // one maximum for all lanes: nothing to rescale
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+            all.s += __shfl_xor_sync(~0u, all.s, o);
+            if (!kGrad) all.u += __shfl_xor_sync(~0u, all.u, o);
+        }
+        r = stats_of(all);
+        if (lane == 0) write_stats(a, row, t, x_t, r);
+    } else {
+        write_nothing(a, row, lane, 32);
+        if (!kGrad) return;
+    }
+    if (kGrad) {
+        const Gradient y = gradient_of(a, t, r.m, r.s, r.log_s, 0.0f, a.g_logprob[row], 0.0f);
+        E* const to = static_cast<E*>(a.grad) + row * a.grad_stride;
+        const bool alike = ((reinterpret_cast<uintptr_t>(to) - reinterpret_cast<uintptr_t>(x.x)) & 15) == 0;
+        __syncwarp();              // the target's element has been read
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) {
+            const int n = k * 32 + lane;
+            if (n >= x.vectors) continue;
+            const Vector<E> out = gradient_at<false>(y, v[k], x.first(n));
+            if (alike && x.whole(n)) store_whole(to + x.first(n), out);
+            else store_partial(to, x, n, out);
+        }
+        return;
+    }
+    if (!a.top) return;
+    // Every lane's largest element is one of the row's: the top-th largest of these 32 bounds the top-th largest element from
+    // below.  What reaches the bound - a few more than wanted, unless many are equal - is collected and sorted.
+    const unsigned long long bounds = sorted((unsigned long long)order_of(mine) << 32 | lane);
+    const uint32_t bound = (uint32_t)(__shfl_sync(~0u, bounds, a.top - 1) >> 32);
+    unsigned long long best = 0, *const list = shared[threadIdx.x >> 5];
+    int listed = 0;
+    auto flush = [&] {
+        __syncwarp();
+        best = with_more(best, lane < listed ? list[lane] : 0);
+        __syncwarp();
+        listed = 0;
+    };
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k)
+#pragma unroll
+        for (int e = 0; e < Vector<E>::N; ++e) {
+            const int i = x.first(k * 32 + lane) + e;
+            const float value = v[k].one(e);
+            const bool in = i >= 0 && i < x.V && order_of(value) >= bound;
+            const unsigned who = __ballot_sync(~0u, in);
+            if (!who) continue;
+            if (listed + __popc(who) > 32) flush();
+            if (in) list[listed + __popc(who & ((1u << lane) - 1))] = key_of(value, i);
+            listed += __popc(who);
+        }
+    flush();
+    if (lane < a.top) write_top(a, row, lane, best, r);
+}
+
+// ---- long rows: a block, or a cluster of blocks, for each ----
+
+template <int T>
+struct SumsShared {
+    Sums warp[T / 32], cluster[kMaxCluster];
+};
+template <int T>
+struct BlockShared : SumsShared<T> {
+    unsigned long long top[T / 32][32];
+    unsigned long long cluster_top[kMaxCluster][32];
+};
+
+template <int T>
+__device__ __forceinline__ Sums block_merged(Sums mine, Sums* shared, float c) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    mine = warp_merged(mine, c);
+    if (lane == 0) shared[warp] = mine;
+    __syncthreads();
+    return warp_merged(lane < T / 32 ? shared[lane] : Sums{-CUDART_INF_F, 0.0f, 0.0f}, c);
+}
+
+// The 32 largest keys of the block's warps, in warp 0.
+template <int T>
+__device__ __forceinline__ unsigned long long block_top(unsigned long long best, unsigned long long (*shared)[32]) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    __syncthreads();
+#pragma unroll
+    for (int half = T / 64; half; half >>= 1) {
+        if (warp >= half && warp < 2 * half) shared[warp][lane] = best;
+        __syncthreads();
+        if (warp < half) best = merge_sorted(best, shared[warp + half][31 - lane]);
+    }
+    return best;
+}
+
+template <class E, int T, bool kTop>
+__global__ void __launch_bounds__(T) block_kernel(RowArgs a) {
+    __shared__ BlockShared<T> sh;
+    extern __shared__ uint32_t group_max[];    // per 32 vectors of the slice: the order of their largest element
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = (int)cluster.block_rank(), blocks = (int)cluster.num_blocks();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t row = blockIdx.x / blocks;
+    const int64_t t = a.targets ? a.targets[row] : 0;
+    if (t < 0) {
+        if (rank == 0) write_nothing(a, row, threadIdx.x, T);
+        return;
+    }
+    if (blocks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // awaited before another block's memory is used
+    const Row<E> x(row_of<E>(a, row), a.vocab);
+    const float x_t = rank == 0 && threadIdx.x == 0 && a.logprob && t < a.vocab ? as_float(x.x[t]) : 0.0f;
+    const float c = a.scale * kLog2E;
+    const int begin = rank * a.slice, end = min(begin + a.slice, x.vectors);
+    Sums mine = {-CUDART_INF_F, 0.0f, 0.0f};
+    for (int v = begin + threadIdx.x; v - lane < end; v += kUnroll * T) {
+        Vector<E> in[kUnroll];
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) in[k] = v + k * T < end ? x.load(v + k * T) : Row<E>::nothing();
+        float most = -CUDART_INF_F;
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) {
+            const float one = in[k].max();
+            most = max_nan(most, one);
+            if (kTop) {
+                const float group = warp_max_nan(one);
+                const int at = (v + k * T - begin) >> 5;
+                if (lane == 0 && v + k * T < end) group_max[at] = order_of(group);
             }
-            last = block_reduce(mine, best, [](unsigned long long p, unsigned long long q) { return p > q ? p : q; });
-            if (threadIdx.x == 0) {
-                a.top_ids[row * a.top + k] = last ? (int)position_of(last) : -1;
-                a.top_logprobs[row * a.top + k] =
-                    last ? r.m == -CUDART_INF_F ? r.m : (as_float(x[position_of(last)]) - r.m) * a.scale - r.log_s : -CUDART_INF_F;
+        }
+        add_vectors<true>(mine, in, most, c);
+    }
+    Sums all = block_merged<T>(mine, sh.warp, c);
+    unsigned long long best = 0;
+    if (kTop) {
+        // The top largest elements lie in the top groups with the largest maxima (equal ones: the first of them): an element
+        // outside is behind the maxima of all these groups.  So: those groups, then what of them reaches the last one's maximum.
+        const int groups = (end - begin + 31) >> 5;
+        for (int g = warp * 32; g < groups; g += T) {
+            const int at = g + lane;
+            best = with_more(best, at < groups ? (unsigned long long)group_max[at] << 32 | (0xFFFFFFFFu - at) : 0);
+        }
+        best = block_top<T>(best, sh.top);
+        __syncthreads();
+        if (warp == 0) sh.top[0][lane] = best;
+        __syncthreads();
+        const uint32_t bound = (uint32_t)(sh.top[0][a.top - 1] >> 32);
+        best = 0;
+        for (int g = warp; g < a.top; g += T / 32) {
+            const unsigned long long group = sh.top[0][g];
+            if (!group) break;
+            const int v = begin + (int)position_of(group) * 32 + lane;
+            const Vector<E> in = v < end ? x.load(v) : Row<E>::nothing();
+#pragma unroll
+            for (int e = 0; e < Vector<E>::N; ++e) {
+                const int i = x.first(v) + e;
+                const float value = in.one(e);
+                const bool counts = v < end && i >= 0 && i < x.V && order_of(value) >= bound;
+                if (__any_sync(~0u, counts)) best = with_more(best, counts ? key_of(value, i) : 0);
             }
-            if (!last) last = 1;   // the row has no more: every later key is below
+        }
+        best = block_top<T>(best, sh.top);
+    }
+    if (blocks > 1) {
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");    // every block has begun
+        if (warp == 0 && rank) {
+            BlockShared<T>* const first = cluster.map_shared_rank(&sh, 0);
+            if (lane == 0) first->cluster[rank] = all;
+            if (kTop) first->cluster_top[rank][lane] = best;
+        }
+        cluster.sync();
+        if (rank) return;
+        for (int b = 1; b < blocks; ++b) {
+            all = merged(all, sh.cluster[b], c);
+            if (kTop && warp == 0) best = merge_sorted(best, sh.cluster_top[b][31 - lane]);
         }
     }
+    if (warp) return;
+    const RowStats r = stats_of(all);
+    if (lane == 0) write_stats(a, row, t, x_t, r);
+    if (kTop && lane < a.top) write_top(a, row, lane, best, r);
 }
 
-// dx_i = c [ g (1[i = t] - p_i) - h p_i (ln p_i + H) ]
-template <class E>
-__device__ void write_gradient(const RowArgs& a, int64_t row, int64_t t, float m, float s, float log_s, float entropy, float g, float h) {
-    const E* const x = static_cast<const E*>(a.logits) + row * a.stride;
-    E* const out = static_cast<E*>(a.grad) + row * a.grad_stride;
-    const float c = a.scale * kLog2E, per = 1.0f / s;
-    const bool zero = t < 0 || m == -CUDART_INF_F, none = t >= a.vocab;
-    for (int i = threadIdx.x; i < a.vocab; i += kThreads) {
-        float y = 0.0f;
-        if (none) {
-            y = CUDART_NAN_F;
-        } else if (!zero) {
-            const float d = as_float(x[i]) - m, p = exp2_fast(d * c) * per;
-            y = g * ((i == t ? 1.0f : 0.0f) - p);
-            if (p > 0.0f && h != 0.0f) y -= h * p * (d * a.scale - log_s + entropy);
-            y *= a.scale;
+// The loss and its gradient of a long row.  The block's slice of the row is copied to shared memory (by the thread that
+// works on it: nothing to wait for but its own copies), summed up, and read again for the gradient when the cluster has
+// agreed on m and S.  kResident false: it does not fit, and is read from global memory again.
+template <class E, int T, bool kResident>
+__global__ void __launch_bounds__(T) loss_kernel(RowArgs a) {
+    __shared__ SumsShared<T> sh;
+    extern __shared__ uint4 slice[];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = (int)cluster.block_rank(), blocks = (int)cluster.num_blocks();
+    const int64_t row = blockIdx.x / blocks;
+    const int64_t t = a.targets[row];
+    const Row<E> x(row_of<E>(a, row), a.vocab);
+    const int begin = rank * a.slice, end = min(begin + a.slice, x.vectors);
+    const float c = a.scale * kLog2E;
+    Sums all = {0.0f, 1.0f, 0.0f};
+    if (t >= 0) {
+        if (blocks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+        if (kResident)
+            for (int v = begin + threadIdx.x; v < end; v += T) {
+                if (x.whole(v)) {
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(slice + (v - begin))), "l"(x.x + x.first(v))
+                                 : "memory");
+                } else {
+                    slice[v - begin] = x.partial(v).w;
+                }
+            }
+        const float x_t = rank == 0 && threadIdx.x == 0 && t < a.vocab ? as_float(x.x[t]) : 0.0f;
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        Sums mine = {-CUDART_INF_F, 0.0f, 0.0f};
+        for (int v = begin + threadIdx.x; v < end; v += kUnroll * T) {
+            Vector<E> in[kUnroll];
+#pragma unroll
+            for (int k = 0; k < kUnroll; ++k) {
+                const int n = v + k * T;
+                if (n >= end) in[k] = Row<E>::nothing();
+                else if (kResident) in[k].w = slice[n - begin];
+                else in[k] = x.load(n);
+            }
+            float most = -CUDART_INF_F;
+#pragma unroll
+            for (int k = 0; k < kUnroll; ++k) most = max_nan(most, in[k].max());
+            add_vectors<false>(mine, in, most, c);
         }
-        out[i] = from_float<E>(y);
+        all = block_merged<T>(mine, sh.warp, c);
+        if (blocks > 1) {
+            asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+            if ((int)threadIdx.x < blocks) cluster.map_shared_rank(&sh, threadIdx.x)->cluster[rank] = all;
+            cluster.sync();       // the logits have been read by everybody: the gradient may take their place
+            all = sh.cluster[0];
+            for (int b = 1; b < blocks; ++b) all = merged(all, sh.cluster[b], c);
+        } else {
+            __syncthreads();
+        }
+        if (rank == 0 && threadIdx.x == 0) write_stats(a, row, t, x_t, stats_of(all));
+    } else if (rank == 0 && threadIdx.x == 0) {
+        write_nothing(a, row, 0, 1);
+    }
+    const RowStats r = stats_of(all);
+    const Gradient y = gradient_of(a, t, r.m, r.s, r.log_s, 0.0f, a.g_logprob[row], 0.0f);
+    E* const to = static_cast<E*>(a.grad) + row * a.grad_stride;
+    if (((reinterpret_cast<uintptr_t>(to) - reinterpret_cast<uintptr_t>(x.x)) & 15) == 0) {
+        for (int v = begin + threadIdx.x; v < end; v += T) {
+            Vector<E> in;
+            if (kResident) in.w = slice[v - begin];
+            else in = x.load(v);
+            const Vector<E> out = gradient_at<false>(y, in, x.first(v));
+            if (x.whole(v)) store_whole(to + x.first(v), out);
+            else store_partial(to, x, v, out);
+        }
+    } else {   // the rows of the gradient are aligned otherwise than the logits': element by element, neighbours by neighbours
+        const int i0 = max(x.first(begin), 0), i1 = min(x.first(end), x.V);
+        const E* const kept = reinterpret_cast<const E*>(slice) - x.first(begin);
+        for (int i = i0 + threadIdx.x; i < i1; i += T) to[i] = from_float<E>(gradient_at<false>(y, as_float(kResident ? kept[i] : x.x[i]), i));
     }
 }
 
-template <class E>
-__global__ void __launch_bounds__(kThreads) grad_kernel(RowArgs a) {
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const float s = a.in_norm[2 * row + 1];
-        write_gradient<E>(a, row, a.targets[row], a.in_norm[2 * row], s, logf(s), a.in_entropy ? a.in_entropy[row] : 0.0f, a.g_logprob[row],
-                          a.g_entropy ? a.g_entropy[row] : 0.0f);
+// ---- the gradient alone, from the sums that the log probabilities left ----
+
+__device__ __forceinline__ Gradient gradient_from_norm(const RowArgs& a, int64_t row) {
+    const float2 n = reinterpret_cast<const float2*>(a.in_norm)[row];
+    const float h = a.g_entropy ? a.g_entropy[row] : 0.0f;
+    return gradient_of(a, a.targets[row], n.x, n.y, a.g_entropy ? logf(n.y) : 0.0f, a.g_entropy ? a.in_entropy[row] : 0.0f, a.g_logprob[row], h);
+}
+
+// L lanes take L kUnroll vectors of a row.
+template <class E, bool kEntropy, int L>
+__global__ void __launch_bounds__(256) grad_kernel(RowArgs a, int segments) {
+    const int sub = threadIdx.x % L;
+    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L, row = item / segments;
+    if (row >= a.rows) return;
+    const Row<E> x(row_of<E>(a, row), a.vocab);
+    const int v = (int)(item - row * segments) * L * kUnroll + sub;
+    Vector<E> in[kUnroll];
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) in[k] = x.load(v + L * k);
+    const Gradient y = gradient_from_norm(a, row);
+    E* const to = static_cast<E*>(a.grad) + row * a.grad_stride;
+    if (((reinterpret_cast<uintptr_t>(to) - reinterpret_cast<uintptr_t>(x.x)) & 15) == 0) {
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) {
+            const int n = v + L * k;
+            if (n >= x.vectors) continue;
+            const Vector<E> out = gradient_at<kEntropy>(y, in[k], x.first(n));
+            if (x.whole(n)) store_whole(to + x.first(n), out);
+            else store_partial(to, x, n, out);
+        }
+    } else {
+        const int lo = max(x.first(v - sub), 0), hi = min(x.first(v - sub + L * kUnroll), x.V);
+        for (int i = lo + sub; i < hi; i += L) to[i] = from_float<E>(gradient_at<kEntropy>(y, as_float(x.x[i]), i));
     }
 }
 
-template <class E>
-__global__ void __launch_bounds__(kThreads) loss_kernel(RowArgs a) {
-    __shared__ float shared[kThreads / 32];
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const E* const x = static_cast<const E*>(a.logits) + row * a.stride;
-        const int64_t t = a.targets[row];
-        RowStats r = {0.0f, 1.0f, 0.0f, 0.0f};
-        if (t >= 0) r = row_stats(x, a.vocab, a.scale, shared);
-        if (threadIdx.x == 0 && a.logprob) a.logprob[row] = t < 0 ? 0.0f : given(x, a.vocab, t, r, a.scale);
-        __syncthreads();   // the gradient may take the logits' place
-        write_gradient<E>(a, row, t, r.m, r.s, r.log_s, 0.0f, a.g_logprob[row], 0.0f);
-    }
+// Few elements a row: L lanes share one, element by element.
+template <class E, bool kEntropy, int L, int N>
+__global__ void __launch_bounds__(256) narrow_grad_kernel(RowArgs a) {
+    const int sub = threadIdx.x % L;
+    const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
+    if (row >= a.rows) return;
+    const E* const from = row_of<E>(a, row);
+    E* const to = static_cast<E*>(a.grad) + row * a.grad_stride;
+    float x[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = sub + k * L < a.vocab ? as_float(from[sub + k * L]) : 0.0f;
+    const Gradient y = gradient_from_norm(a, row);
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        if (sub + k * L < a.vocab) to[sub + k * L] = from_float<E>(gradient_at<kEntropy>(y, x[k], sub + k * L));
 }
+
+// ---- launches ----
 
 bool type_ok(int type) { return type == SLAQ_F32 || type == SLAQ_BF16 || type == SLAQ_F16; }
 int64_t size_of(int type) { return type == SLAQ_F32 ? 4 : 2; }
@@ -168,8 +558,9 @@ bool overlap(const RowArgs& a, int64_t es) {
     const int64_t width = a.vocab * es;
     const char *x_end = x + (a.rows - 1) * a.stride * es + width, *y_end = y + (a.rows - 1) * a.grad_stride * es + width;
     if (x_end <= y || y_end <= x) return false;
-    if (a.stride != a.grad_stride) return true;
+    if (a.rows > 1 && a.stride != a.grad_stride) return true;
     if (x == y) return false;
+    if (a.rows == 1) return true;
     const int64_t pitch = a.stride * es, apart = ((y - x) % pitch + pitch) % pitch;
     return apart < width || pitch - apart < width;
 }
@@ -187,14 +578,100 @@ int check_gradient(const RowArgs& a, int type) {
     return a.rows && overlap(a, size_of(type)) ? SLAQ_E_ARG : SLAQ_OK;
 }
 
-int done() { return cudaGetLastError() == cudaSuccess ? SLAQ_OK : SLAQ_E_CUDA; }
-
 template <class F>
 int by_type(int type, F&& f) {
-    if (type == SLAQ_F32) f(0.0f);
-    else if (type == SLAQ_BF16) f(__nv_bfloat16());
-    else f(__half());
-    return done();
+    cudaError_t e;
+    if (type == SLAQ_F32) e = f(0.0f);
+    else if (type == SLAQ_BF16) e = f(__nv_bfloat16());
+    else e = f(__half());
+    if (e != cudaSuccess) (void)cudaGetLastError();
+    return e == cudaSuccess ? SLAQ_OK : SLAQ_E_CUDA;
+}
+
+template <class... Params, class... Args>
+cudaError_t launch(void (*kernel)(Params...), int64_t blocks, int threads, size_t smem, int cluster, cudaStream_t st, Args... args) {
+    if (smem > 40 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1] = {};
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+constexpr int kSms = 148;
+constexpr size_t kSliceBytes = 64 * 1024, kMostSlice = 200 * 1024;   // per block of the loss: three blocks on an SM, or one
+
+// Vectors a row may touch, whatever its alignment.
+template <class E>
+int most_vectors(int vocab) { return (vocab + 2 * (Vector<E>::N - 1)) / Vector<E>::N; }
+// What every block of a cluster takes of them: whole groups of 32.
+int slice_of(int vectors, int blocks) { return ((vectors + blocks - 1) / blocks + 31) / 32 * 32; }
+
+// Rows of at most this many elements are shared by a few lanes, the next by a warp with all its vectors in registers.
+constexpr int kNarrow = 64;
+template <class E>
+bool fits_a_warp(int vocab) { return most_vectors<E>(vocab) <= 32 * kUnroll; }
+
+template <class E, bool kGrad>
+cudaError_t launch_short(const RowArgs& a, cudaStream_t st) {
+    auto blocks = [&](int64_t per) { return (a.rows + per - 1) / per; };
+    if (a.vocab <= 16) return launch(narrow_kernel<E, 4, 4, kGrad>, blocks(256 / 4), 256, 0, 1, st, a);
+    if (a.vocab <= kNarrow) return launch(narrow_kernel<E, 16, 4, kGrad>, blocks(256 / 16), 256, 0, 1, st, a);
+    return launch(warp_kernel<E, kGrad>, blocks(4), 128, 0, 1, st, a);
+}
+
+template <class E, int T>
+cudaError_t launch_block(RowArgs a, int cluster, cudaStream_t st) {
+    a.slice = slice_of(most_vectors<E>(a.vocab), cluster);
+    return a.top ? launch(block_kernel<E, T, true>, a.rows * cluster, T, (size_t)a.slice / 32 * 4, cluster, st, a)
+                 : launch(block_kernel<E, T, false>, a.rows * cluster, T, 0, cluster, st, a);
+}
+
+template <class E>
+cudaError_t launch_logprobs(const RowArgs& a, cudaStream_t st) {
+    if (a.vocab <= kNarrow || fits_a_warp<E>(a.vocab)) return launch_short<E, false>(a, st);
+    const int vectors = most_vectors<E>(a.vocab);
+    int cluster = 1;
+    while (cluster < kMaxCluster && a.rows * cluster * 2 <= 2 * kSms && vectors / (2 * cluster) >= 256) cluster *= 2;
+    const int each = vectors / cluster;
+    if (each <= 1024) return launch_block<E, 128>(a, cluster, st);
+    if (each <= 4096) return launch_block<E, 256>(a, cluster, st);
+    return launch_block<E, 512>(a, cluster, st);
+}
+
+template <class E>
+cudaError_t launch_loss(RowArgs a, cudaStream_t st) {
+    if (a.vocab <= kNarrow || fits_a_warp<E>(a.vocab)) return launch_short<E, true>(a, st);
+    const int vectors = most_vectors<E>(a.vocab);
+    int cluster = 1;
+    while (cluster < kMaxCluster && ((a.rows * cluster * 2 <= 2 * kSms && vectors / (2 * cluster) >= 256) || (size_t)slice_of(vectors, cluster) * 16 > kSliceBytes))
+        cluster *= 2;
+    a.slice = slice_of(vectors, cluster);
+    const size_t bytes = (size_t)a.slice * 16;
+    if (bytes > kMostSlice) return launch(loss_kernel<E, 512, false>, a.rows * cluster, 512, 0, cluster, st, a);
+    return launch(loss_kernel<E, 256, true>, a.rows * cluster, 256, bytes, cluster, st, a);
+}
+
+template <class E, bool kEntropy>
+cudaError_t launch_grad(const RowArgs& a, cudaStream_t st) {
+    auto blocks = [&](int64_t per) { return (a.rows + per - 1) / per; };
+    if (a.vocab <= 16) return launch(narrow_grad_kernel<E, kEntropy, 4, 4>, blocks(256 / 4), 256, 0, 1, st, a);
+    if (a.vocab <= kNarrow) return launch(narrow_grad_kernel<E, kEntropy, 16, 4>, blocks(256 / 16), 256, 0, 1, st, a);
+    const int vectors = most_vectors<E>(a.vocab);
+    if (vectors <= 8 * kUnroll) return launch(grad_kernel<E, kEntropy, 8>, blocks(256 / 8), 256, 0, 1, st, a, 1);
+    const int segments = (vectors + 32 * kUnroll - 1) / (32 * kUnroll);
+    const int64_t n = (a.rows * segments + 7) / 8;
+    return n > 0x7FFFFFFF ? cudaErrorInvalidValue : launch(grad_kernel<E, kEntropy, 32>, n, 256, 0, 1, st, a, segments);
 }
 
 }  // namespace
@@ -210,11 +687,10 @@ extern "C" int slaq_token_logprobs(const void* d_logits, int type, int64_t rows,
     a.top = top, a.top_ids = d_out_top_ids, a.top_logprobs = d_out_top_logprobs;
     if (const int rc = check_rows(a, type)) return rc;
     if (top < 0 || (top > 0 && rows && (!d_out_top_ids || !d_out_top_logprobs)) || (d_out_logprob && !d_targets && rows)) return SLAQ_E_ARG;
+    if (reinterpret_cast<uintptr_t>(d_out_norm) % 8) return SLAQ_E_ARG;
     if (top > kMaxTop) return SLAQ_E_RANGE;
     if (rows == 0) return SLAQ_OK;
-    return by_type(type, [&](auto e) {
-        logprobs_kernel<decltype(e)><<<(unsigned)rows, kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(a);
-    });
+    return by_type(type, [&](auto e) { return launch_logprobs<decltype(e)>(a, static_cast<cudaStream_t>(cuda_stream)); });
 }
 
 extern "C" int slaq_token_logprobs_grad(const void* d_logits, int type, int64_t rows, int32_t vocab, int64_t row_stride,
@@ -228,10 +704,12 @@ extern "C" int slaq_token_logprobs_grad(const void* d_logits, int type, int64_t 
     a.grad = d_out_grad, a.grad_stride = grad_stride;
     if (const int rc = check_rows(a, type)) return rc;
     if (rows && (!d_norm || (d_grad_entropy && !d_entropy))) return SLAQ_E_ARG;
+    if (reinterpret_cast<uintptr_t>(d_norm) % 8) return SLAQ_E_ARG;
     if (const int rc = check_gradient(a, type)) return rc;
     if (rows == 0) return SLAQ_OK;
     return by_type(type, [&](auto e) {
-        grad_kernel<decltype(e)><<<(unsigned)rows, kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(a);
+        return d_grad_entropy ? launch_grad<decltype(e), true>(a, static_cast<cudaStream_t>(cuda_stream))
+                              : launch_grad<decltype(e), false>(a, static_cast<cudaStream_t>(cuda_stream));
     });
 }
 
@@ -245,7 +723,5 @@ extern "C" int slaq_token_loss(const void* d_logits, int type, int64_t rows, int
     if (const int rc = check_rows(a, type)) return rc;
     if (const int rc = check_gradient(a, type)) return rc;
     if (rows == 0) return SLAQ_OK;
-    return by_type(type, [&](auto e) {
-        loss_kernel<decltype(e)><<<(unsigned)rows, kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(a);
-    });
+    return by_type(type, [&](auto e) { return launch_loss<decltype(e)>(a, static_cast<cudaStream_t>(cuda_stream)); });
 }

@@ -31,6 +31,10 @@ _torch = None
 _types = {}
 
 
+def _lib():
+    return load_library()
+
+
 def _load():
     global _torch
     if _torch is None:
@@ -55,41 +59,31 @@ def _check(rc, message=None):
 
 
 def _vector(t, name, dtype, n, device):
-    """A contiguous tensor of n entries; None passes."""
+    """The address of a contiguous tensor of n entries on GPU `device`; None passes."""
     if t is None:
         return None
-    if t.dtype != dtype or t.device != device or t.numel() != n or not t.is_contiguous():
-        _refuse(f"{name} is not a contiguous {dtype} tensor of {n} entries on {device}")
+    if t.dtype is not dtype or t.get_device() != device or t.numel() != n or not t.is_contiguous():
+        _refuse(f"{name} is not a contiguous {dtype} tensor of {n} entries on GPU {device}")
     return t.data_ptr()
 
 
 def _matrix(t, name):
-    if t.dim() != 2 or not t.is_cuda or t.dtype not in _types:
+    """(address, type, rows, elements of a row, row stride, GPU) of a matrix whose rows' elements are neighbours."""
+    kind, shape = _types.get(t.dtype), t.shape
+    if len(shape) != 2 or not t.is_cuda or kind is None:
         _refuse(f"{name} is not a matrix of fp32, bf16 or fp16 on a GPU")
-    if t.shape[1] > 1 and t.stride(1) != 1:
-        _refuse(f"the elements of a row of {name} are not next to one another")
-    if t.shape[1] < 1:
+    rows, vocab = shape
+    pitch, step = t.stride()
+    if vocab < 1:
         _refuse("an empty vocabulary")
-    return t.data_ptr(), _types[t.dtype], t.shape[0], t.shape[1], t.stride(0)
-
-
-@contextlib.contextmanager
-def _elsewhere(stream, device):
-    """Another stream than torch's current one, or another device: what is allocated there belongs there."""
-    torch = _load()
-    with torch.cuda.device(device):
-        if stream is None:
-            yield torch.cuda.current_stream().cuda_stream
-        elif isinstance(stream, int):
-            with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
-                yield stream
-        else:
-            with torch.cuda.stream(stream):
-                yield stream.cuda_stream
+    if step != 1 and vocab > 1:
+        _refuse(f"the elements of a row of {name} are not next to one another")
+    return t.data_ptr(), kind, rows, vocab, pitch, t.get_device()
 
 
 class _Here:
-    """The common case: the current stream of the current device."""
+    """The current stream of the current device: the common case, without a context to enter."""
+    __slots__ = ("raw",)
 
     def __init__(self, raw):
         self.raw = raw
@@ -101,9 +95,21 @@ class _Here:
         return False
 
 
+@contextlib.contextmanager
+def _elsewhere(stream, device):
+    """Another stream than torch's current one, or another device: what is allocated there belongs there."""
+    torch = _load()
+    with torch.cuda.device(device):
+        if stream is None:
+            yield torch.cuda.current_stream().cuda_stream
+        else:
+            with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream):
+                yield getattr(stream, "cuda_stream", stream)
+
+
 def _on(stream, device):
     torch = _load()
-    if stream is None and device.index == torch.cuda.current_device():
+    if stream is None and device == torch.cuda.current_device():
         return _Here(torch.cuda.current_stream().cuda_stream)
     return _elsewhere(stream, device)
 
@@ -120,27 +126,30 @@ def token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, strea
     """slaq_token_logprobs: ``logits`` [rows, vocab] fp32 / bf16 / fp16 with any row stride, ``targets`` int64 [rows] (negative:
     the row is not asked for) or None, ``top`` alternatives (0 .. 32), ``scale`` the inverse temperature."""
     torch = _load()
-    x, kind, rows, vocab, pitch = _matrix(logits, "logits")
-    device = logits.device
-    t = _vector(targets, "targets", torch.int64, rows, device)
+    x, kind, rows, vocab, pitch, gpu = _matrix(logits, "logits")
+    t = _vector(targets, "targets", torch.int64, rows, gpu)
     if not 0 <= top <= MAX_TOP:
         raise SlaqError(-1 if top < 0 else -2, f"top is 0 .. {MAX_TOP}")
-    with _on(stream, device) as raw:
-        out = torch.empty(4 * rows, dtype=torch.float32, device=device)
-        logprob, entropy, norm = out[:rows], out[rows:2 * rows], out[2 * rows:].view(rows, 2)
-        ids = torch.empty(rows, top, dtype=torch.int32, device=device) if top else None
-        best = torch.empty(rows, top, dtype=torch.float32, device=device) if top else None
-        base = out.data_ptr()
-        _check(load_library().slaq_token_logprobs(
-            x, kind, rows, vocab, pitch, t, scale, None if t is None else base, base + 4 * rows, base + 8 * rows, top,
-            ids.data_ptr() if top else None, best.data_ptr() if top else None, raw))
-    return TokenLogprobs(None if t is None else logprob, entropy, norm, ids, best)
+    device = logits.device
+    with _on(stream, gpu) as raw:
+        logprob = None if t is None else torch.empty(rows, device=device, dtype=torch.float32)
+        entropy = torch.empty(rows, device=device, dtype=torch.float32)
+        norm = torch.empty((rows, 2), device=device, dtype=torch.float32)
+        ids = best = None
+        if top:
+            ids = torch.empty((rows, top), device=device, dtype=torch.int32)
+            best = torch.empty((rows, top), device=device, dtype=torch.float32)
+        rc = _lib().slaq_token_logprobs(x, kind, rows, vocab, pitch, t, scale, None if t is None else logprob.data_ptr(), entropy.data_ptr(),
+                                        norm.data_ptr(), top, ids.data_ptr() if top else None, best.data_ptr() if top else None, raw)
+    if rc < 0:
+        _check(rc)
+    return TokenLogprobs(logprob, entropy, norm, ids, best)
 
 
 def _gradient(out, logits):
     if out is None:
         return _load().empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    if out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device or (out.shape[1] > 1 and out.stride(1) != 1):
+    if out.shape != logits.shape or out.dtype is not logits.dtype or out.get_device() != logits.get_device() or (out.stride(1) != 1 and out.shape[1] > 1):
         _refuse("out is not a matrix like logits with its rows' elements next to one another")
     return out
 
@@ -149,14 +158,13 @@ def token_logprobs_grad(logits, targets, norm, grad_logprob, entropy=None, grad_
     """slaq_token_logprobs_grad: gradient of sum(grad_logprob x logprob + grad_entropy x entropy) by the logits, from what
     ``token_logprobs`` returned.  ``out`` may be ``logits`` itself."""
     torch = _load()
-    x, kind, rows, vocab, pitch = _matrix(logits, "logits")
-    device = logits.device
-    t = _vector(targets, "targets", torch.int64, rows, device)
-    n, g = _vector(norm, "norm", torch.float32, 2 * rows, device), _vector(grad_logprob, "grad_logprob", torch.float32, rows, device)
-    e, h = _vector(entropy, "entropy", torch.float32, rows, device), _vector(grad_entropy, "grad_entropy", torch.float32, rows, device)
-    with _on(stream, device) as raw:
+    x, kind, rows, vocab, pitch, gpu = _matrix(logits, "logits")
+    t = _vector(targets, "targets", torch.int64, rows, gpu)
+    n, g = _vector(norm, "norm", torch.float32, 2 * rows, gpu), _vector(grad_logprob, "grad_logprob", torch.float32, rows, gpu)
+    e, h = _vector(entropy, "entropy", torch.float32, rows, gpu), _vector(grad_entropy, "grad_entropy", torch.float32, rows, gpu)
+    with _on(stream, gpu) as raw:
         out = _gradient(out, logits)
-        _check(load_library().slaq_token_logprobs_grad(x, kind, rows, vocab, pitch, t, scale, n, e, g, h, out.data_ptr(), out.stride(0), raw),
+        _check(_lib().slaq_token_logprobs_grad(x, kind, rows, vocab, pitch, t, scale, n, e, g, h, out.data_ptr(), out.stride(0), raw),
                "bad argument: a missing input, a scale that is not positive, or a gradient that overlaps the logits otherwise than row for row")
     return out
 
@@ -164,13 +172,12 @@ def token_logprobs_grad(logits, targets, norm, grad_logprob, entropy=None, grad_
 def token_loss(logits, targets, row_grad, scale: float = 1.0, out=None, stream=None):
     """slaq_token_loss: (log probabilities, gradient of sum(row_grad x logprob) by the logits) in one call."""
     torch = _load()
-    x, kind, rows, vocab, pitch = _matrix(logits, "logits")
-    device = logits.device
-    t, g = _vector(targets, "targets", torch.int64, rows, device), _vector(row_grad, "row_grad", torch.float32, rows, device)
-    with _on(stream, device) as raw:
+    x, kind, rows, vocab, pitch, gpu = _matrix(logits, "logits")
+    t, g = _vector(targets, "targets", torch.int64, rows, gpu), _vector(row_grad, "row_grad", torch.float32, rows, gpu)
+    with _on(stream, gpu) as raw:
         out = _gradient(out, logits)
-        logprob = torch.empty(rows, dtype=torch.float32, device=device)
-        _check(load_library().slaq_token_loss(x, kind, rows, vocab, pitch, t, scale, g, logprob.data_ptr(), out.data_ptr(), out.stride(0), raw),
+        logprob = torch.empty(rows, device=out.device, dtype=torch.float32)
+        _check(_lib().slaq_token_loss(x, kind, rows, vocab, pitch, t, scale, g, logprob.data_ptr(), out.data_ptr(), out.stride(0), raw),
                "bad argument: a missing input, a scale that is not positive, or a gradient that overlaps the logits otherwise than row for row")
     return logprob, out
 
@@ -182,47 +189,48 @@ def job_row_grad(offsets, targets=None, weights=None, out=None, stream=None):
     known = next((t for t in (targets, weights, out) if t is not None), None)
     if known is None:
         _refuse("the number of rows follows from targets, weights or out: one of them is wanted")
-    rows, device = known.numel(), offsets.device
-    t, w = _vector(targets, "targets", torch.int64, rows, device), _vector(weights, "weights", torch.float32, rows, device)
-    off = _vector(offsets, "offsets", torch.int64, max(offsets.numel(), 1), device)
-    with _on(stream, device) as raw:
+    rows, gpu = known.numel(), offsets.get_device()
+    if gpu < 0:
+        _refuse("offsets lies not on a GPU")
+    t, w = _vector(targets, "targets", torch.int64, rows, gpu), _vector(weights, "weights", torch.float32, rows, gpu)
+    n = offsets.numel() - 1
+    off = _vector(offsets, "offsets", torch.int64, max(n, 0) + 1, gpu)
+    with _on(stream, gpu) as raw:
         if out is None:
-            out = torch.zeros(rows, dtype=torch.float32, device=device)
-        _check(load_library().slaq_job_row_grad(offsets.numel() - 1, off, rows, t, w, _vector(out, "out", torch.float32, rows, device), raw))
+            out = torch.zeros(rows, dtype=torch.float32, device=offsets.device)
+        _check(_lib().slaq_job_row_grad(n, off, rows, t, w, _vector(out, "out", torch.float32, rows, gpu), raw))
     return out
 
 
 def _job_inputs(offsets, targets, logprob, weights):
     torch = _load()
-    rows, device = logprob.numel(), logprob.device
-    return (_vector(offsets, "offsets", torch.int64, max(offsets.numel(), 1), device), rows, _vector(targets, "targets", torch.int64, rows, device),
-            _vector(logprob, "logprob", torch.float32, rows, device), _vector(weights, "weights", torch.float32, rows, device))
+    rows, gpu, n = logprob.numel(), logprob.get_device(), offsets.numel() - 1
+    if gpu < 0:
+        _refuse("logprob lies not on a GPU")
+    return (n, gpu, _vector(offsets, "offsets", torch.int64, max(n, 0) + 1, gpu), rows, _vector(targets, "targets", torch.int64, rows, gpu),
+            _vector(logprob, "logprob", torch.float32, rows, gpu), _vector(weights, "weights", torch.float32, rows, gpu))
 
 
 def job_losses(offsets, targets, logprob, weights=None, out=None, stream=None):
     """slaq_job_losses: float64 [jobs], the weighted mean of -logprob over each job's rows that count."""
     torch = _load()
-    off, rows, t, lp, w = _job_inputs(offsets, targets, logprob, weights)
-    n = offsets.numel() - 1
-    with _on(stream, logprob.device) as raw:
+    n, gpu, off, rows, t, lp, w = _job_inputs(offsets, targets, logprob, weights)
+    with _on(stream, gpu) as raw:
         if out is None:
-            out = torch.empty(max(n, 0), dtype=torch.float64, device=logprob.device)
-        _check(load_library().slaq_job_losses(n, off, rows, t, lp, w, _vector(out, "out", torch.float64, n, logprob.device), raw))
+            out = torch.empty(n, dtype=torch.float64, device=logprob.device)
+        _check(_lib().slaq_job_losses(n, off, rows, t, lp, w, _vector(out, "out", torch.float64, n, gpu), raw))
     return out
 
 
 def append_token_losses(sched, d_job_ids, offsets, targets, logprob, weights, d_iter_times, d_cores_used, out):
     torch = _load()
-    n, device = d_job_ids.numel(), logprob.device
-    off, rows, t, lp, w = _job_inputs(offsets, targets, logprob, weights)
-    if offsets.numel() != n + 1:
-        _refuse("offsets has one entry more than there are jobs")
+    n, gpu, off, rows, t, lp, w = _job_inputs(offsets, targets, logprob, weights)
     if out is None:
-        out = torch.empty(n, dtype=torch.float64, device=device)
+        out = torch.empty(n, dtype=torch.float64, device=logprob.device)
     sched._check(sched._lib.slaq_append_token_losses(
-        sched._h, n, _vector(d_job_ids, "job ids", torch.int32, n, device), off, rows, t, lp, w,
-        _vector(d_iter_times, "iteration times", torch.float64, n, device), _vector(d_cores_used, "cores", torch.int32, n, device),
-        _vector(out, "out", torch.float64, n, device)))
+        sched._h, n, _vector(d_job_ids, "job ids", torch.int32, n, gpu), off, rows, t, lp, w,
+        _vector(d_iter_times, "iteration times", torch.float64, n, gpu), _vector(d_cores_used, "cores", torch.int32, n, gpu),
+        _vector(out, "out", torch.float64, n, gpu)))
     return out
 
 
@@ -269,7 +277,8 @@ class AdamW:
         if kind not in _types or not params[0].is_cuda or len(grads) != n or len(group_of) != n or not groups:
             _refuse("parameters are fp32, bf16 or fp16 tensors on a GPU, with a gradient and a group each")
 
-        with _on(stream, device) as raw:
+        gpu = device.index
+        with _on(stream, gpu) as raw:
             def states(given, dtype, count):
                 return [torch.zeros(count(p), device=device).to(dtype) for p in params] if given is None else list(given)
             blocks = lambda p: -(-p.numel() // STATE_BLOCK)   # noqa: E731
@@ -290,13 +299,13 @@ class AdamW:
                 if len(tensors) != n:
                     _refuse(f"{name} has another length than params")
                 for row, p, t in zip(table, params, tensors):
-                    setattr(row, field, _vector(t, name, dtype, p.numel(), device))
+                    setattr(row, field, _vector(t, name, dtype, p.numel(), gpu))
             if eight:
                 for name, tensors in (("exp_avg_scale", self.exp_avg_scale), ("exp_avg_sq_scale", self.exp_avg_sq_scale)):
                     if len(tensors) != n:
                         _refuse(f"{name} has another length than params")
                     for row, p, t in zip(table, params, tensors):
-                        setattr(row, name, _vector(t, name, torch.float32, blocks(p), device))
+                        setattr(row, name, _vector(t, name, torch.float32, blocks(p), gpu))
             for row, p, k in zip(table, params, group_of):
                 row.n, row.group = p.numel(), k
             numels = np.array([p.numel() for p in params], np.int64)
@@ -305,7 +314,7 @@ class AdamW:
             rc = self._lib.slaq_adamw_create(self._ws.data_ptr(), need, n, table, len(groups), (_Group * len(groups))(*groups),
                                              _types[kind], _types[grad_kind], state_bits, raw, ctypes.byref(self._h))
         _check(rc, {-1: "a group out of range, betas outside [0, 1), a tensor listed twice, or tensors that overlap"}.get(rc))
-        self._device, self._n_groups = device, len(groups)
+        self._gpu, self._n_groups = gpu, len(groups)
 
     def _ok(self, rc):
         return _check(rc, self._lib.slaq_adamw_last_error(self._h).decode() if rc < 0 else None)
@@ -313,8 +322,8 @@ class AdamW:
     def step(self, active=None, stream=None):
         """One step of the groups whose entry of ``active`` (int32 CUDA tensor [groups], for instance the allocation of
         ``schedule_device``) is above 0; None: of all."""
-        a = None if active is None else _vector(active, "active", _load().int32, self._n_groups, self._device)
-        with _on(stream, self._device) as raw:
+        a = None if active is None else _vector(active, "active", _load().int32, self._n_groups, self._gpu)
+        with _on(stream, self._gpu) as raw:
             self._ok(self._lib.slaq_adamw_step(self._h, a, raw))
 
     def set_group(self, group: int, stream=None, **values):
@@ -322,7 +331,7 @@ class AdamW:
         if not 0 <= group < self._n_groups:
             raise SlaqError(-2, "no such group")
         merged = {**self._groups[group], **values}
-        with _on(stream, self._device) as raw:
+        with _on(stream, self._gpu) as raw:
             self._ok(self._lib.slaq_adamw_set_group(self._h, group, ctypes.byref(_group(**{"step": -1, **{k: v for k, v in merged.items() if k != "step"}, **values})), raw))
         self._groups[group] = merged
 
@@ -332,16 +341,16 @@ class AdamW:
         if len(grads) != len(self.params):
             _refuse("grads has another length than params")
         for g, old in zip(grads, self.grads):
-            _vector(g, "grads", old.dtype, old.numel(), self._device)
+            _vector(g, "grads", old.dtype, old.numel(), self._gpu)
         rows = (c_void_p * len(grads))(*[g.data_ptr() for g in grads])
-        with _on(stream, self._device) as raw:
+        with _on(stream, self._gpu) as raw:
             self._ok(self._lib.slaq_adamw_set_grads(self._h, rows, raw))
         self.grads = grads
 
     def get_steps(self, stream=None) -> np.ndarray:
         """Steps taken per group; waits for the stream."""
         out = np.empty(self._n_groups, np.int64)
-        with _on(stream, self._device) as raw:
+        with _on(stream, self._gpu) as raw:
             self._ok(self._lib.slaq_adamw_get_steps(self._h, out.ctypes.data, raw))
         return out
 
