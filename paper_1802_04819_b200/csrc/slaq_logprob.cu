@@ -105,19 +105,12 @@ __device__ __forceinline__ float gradient_at(const Gradient& r, float x, int i) 
     y *= exp2_fast(t);
     return i == r.target ? y + r.at_target : y;
 }
-// .. of the vector that begins with element `first`
+// .. of a vector in which the target is not
 template <bool kEntropy, class E>
-__device__ __forceinline__ Vector<E> gradient_at(const Gradient& r, const Vector<E>& x, int first) {
+__device__ __forceinline__ Vector<E> gradient_at(const Gradient& r, const Vector<E>& x) {
     constexpr int N = Vector<E>::N;
     Vector<E> out;
-    if (r.kind) {
-        const Pair p = r.kind == 1 ? pair_of(0.0f, 0.0f) : pair_of(CUDART_NAN_F, CUDART_NAN_F);
-#pragma unroll
-        for (int i = 0; i < N / 2; ++i) out.put(i, p);
-        return out;
-    }
     const Pair off = pair_of(-r.base, -r.base), by = pair_of(r.c, r.c), A = pair_of(r.A, r.A), B = pair_of(r.B, r.B);
-    const bool here = (unsigned)(r.target - first) < (unsigned)N;
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) {
         float p, q;
@@ -127,14 +120,7 @@ __device__ __forceinline__ Vector<E> gradient_at(const Gradient& r, const Vector
             p = p < kGone ? kGone : p, q = q < kGone ? kGone : q;
             y = fma2(B, pair_of(p, q), A);
         }
-        y = y * pair_of(exp2_fast(p), exp2_fast(q));
-        if (here) {
-            split(y, p, q);
-            if (r.target == first + 2 * i) p += r.at_target;
-            if (r.target == first + 2 * i + 1) q += r.at_target;
-            y = pair_of(p, q);
-        }
-        out.put(i, y);
+        out.put(i, y * pair_of(exp2_fast(p), exp2_fast(q)));
     }
     return out;
 }
@@ -142,14 +128,26 @@ template <class E>
 __device__ __forceinline__ void store_whole(E* to, const Vector<E>& x) {
     asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(to), "r"(x.w.x), "r"(x.w.y), "r"(x.w.z), "r"(x.w.w) : "memory");
 }
-template <class E>
-__device__ __forceinline__ void store_partial(E* row, const Row<E>& r, int v, const Vector<E>& x) {
+// What a thread adds to the whole vectors that it has written: the row's vector number v, which is not whole ..
+template <bool kEntropy, class E>
+__device__ __forceinline__ void store_partial(E* row, const Row<E>& r, int v, const Vector<E>& x, const Gradient& y) {
 #pragma unroll
     for (int k = 0; k < Vector<E>::N; ++k) {
         const int i = r.first(v) + k;
-        if (i >= 0 && i < r.V) row[i] = reinterpret_cast<const E*>(&x.w)[k];
+        if (i >= 0 && i < r.V) row[i] = from_float<E>(gradient_at<kEntropy>(y, x.one(k), i));
     }
 }
+// .. and zeros, or NaN, where the row has no gradient
+template <class E>
+__device__ __forceinline__ Vector<E> gradient_of_kind(const Gradient& r) {
+    Vector<E> out;
+    const Pair p = r.kind == 1 ? pair_of(0.0f, 0.0f) : pair_of(CUDART_NAN_F, CUDART_NAN_F);
+#pragma unroll
+    for (int i = 0; i < Vector<E>::N / 2; ++i) out.put(i, p);
+    return out;
+}
+template <class E>
+__device__ __forceinline__ bool aligned_alike(const E* a, const E* b) { return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15) == 0; }
 
 // ---- few elements a row: L lanes share one, N elements each, kept in registers ----
 template <class E, int L, int N, bool kGrad>
@@ -219,109 +217,86 @@ __global__ void __launch_bounds__(256) narrow_kernel(RowArgs a) {
     }
 }
 
-// ---- a row that a warp holds in registers: 4 vectors a lane ----
-template <class E, bool kGrad>
-__global__ void __launch_bounds__(128) warp_kernel(RowArgs a) {
-    __shared__ unsigned long long shared[4][32];
+// ---- the loss and gradient of a row that a warp holds in registers: 4 vectors a lane ----
+template <class E>
+__global__ void __launch_bounds__(128) warp_loss_kernel(RowArgs a) {
     const int lane = threadIdx.x & 31;
     const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
     if (row >= a.rows) return;
-    const int64_t t = a.targets ? a.targets[row] : 0;
+    const int64_t t = a.targets[row];
     const Row<E> x(row_of<E>(a, row), a.vocab);
     const float c = a.scale * kLog2E;
     Vector<E> v[kUnroll];
-    Sums all = {-CUDART_INF_F, 0.0f, 0.0f};
-    RowStats r = {0.0f, 0.0f, 0.0f, 0.0f};
-    float mine = -CUDART_INF_F;
+    RowStats r = {0.0f, 1.0f, 0.0f, 0.0f};
     if (t >= 0) {
 #pragma unroll
         for (int k = 0; k < kUnroll; ++k) v[k] = x.load(k * 32 + lane);
-        const float x_t = t < a.vocab ? as_float(x.x[t]) : 0.0f;
+        const float given = t < a.vocab ? as_float(x.x[t]) : 0.0f;
+        float most = -CUDART_INF_F;
 #pragma unroll
-        for (int k = 0; k < kUnroll; ++k) mine = max_nan(mine, v[k].max());
-        add_vectors<!kGrad>(all, v, warp_max_nan(mine), c);     // one maximum for all lanes: nothing to rescale
+        for (int k = 0; k < kUnroll; ++k) most = max_nan(most, v[k].max());
+        Sums all = {-CUDART_INF_F, 0.0f, 0.0f};
+        add_vectors<false>(all, v, warp_max_nan(most), c);      // one maximum for all lanes: nothing to rescale
 #pragma unroll
-        for (int o = 16; o; o >>= 1) {
-            all.s += __shfl_xor_sync(~0u, all.s, o);
-            if (!kGrad) all.u += __shfl_xor_sync(~0u, all.u, o);
-        }
+        for (int o = 16; o; o >>= 1) all.s += __shfl_xor_sync(~0u, all.s, o);
         r = stats_of(all);
-        if (lane == 0) write_stats(a, row, t, x_t, r);
+        if (lane == 0) write_stats(a, row, t, given, r);
     } else {
         write_nothing(a, row, lane, 32);
-        if (!kGrad) return;
     }
-    if (kGrad) {
-        const Gradient y = gradient_of(a, t, r.m, r.s, r.log_s, 0.0f, a.g_logprob[row], 0.0f);
-        E* const to = static_cast<E*>(a.grad) + row * a.grad_stride;
-        const bool alike = ((reinterpret_cast<uintptr_t>(to) - reinterpret_cast<uintptr_t>(x.x)) & 15) == 0;
-        __syncwarp();              // the target's element has been read
+    const Gradient y = gradient_of(a, t, r.m, r.s, r.log_s, 0.0f, a.g_logprob[row], 0.0f);
+    E* const to = static_cast<E*>(a.grad) + row * a.grad_stride;
+    const bool alike = aligned_alike(to, x.x);
+    // the lane that writes the target's vector adds the target's own term
+    const int at = y.target >= 0 ? (y.target + x.skip) / Row<E>::N : -1;
+    const bool owner = alike && at >= 0 && at % 32 == lane && x.whole(at) && y.kind == 0;
+    const float x_t = owner ? as_float(x.x[y.target]) : 0.0f;
+    __syncwarp();                  // the row's logits have been read by all lanes
 #pragma unroll
-        for (int k = 0; k < kUnroll; ++k) {
-            const int n = k * 32 + lane;
-            if (n >= x.vectors) continue;
-            const Vector<E> out = gradient_at<false>(y, v[k], x.first(n));
-            if (alike && x.whole(n)) store_whole(to + x.first(n), out);
-            else store_partial(to, x, n, out);
-        }
-        return;
+    for (int k = 0; k < kUnroll; ++k) {
+        const int n = k * 32 + lane;
+        if (alike && x.whole(n)) store_whole(to + x.first(n), y.kind ? gradient_of_kind<E>(y) : gradient_at<false>(y, v[k]));
+        else if (n < x.vectors) store_partial<false>(to, x, n, v[k], y);
     }
-    if (!a.top) return;
-    // Every lane's largest element is one of the row's: the top-th largest of these 32 bounds the top-th largest element from
-    // below.  What reaches the bound - a few more than wanted, unless many are equal - is collected and sorted.
-    const unsigned long long bounds = sorted((unsigned long long)order_of(mine) << 32 | lane);
-    const uint32_t bound = (uint32_t)(__shfl_sync(~0u, bounds, a.top - 1) >> 32);
-    unsigned long long best = 0, *const list = shared[threadIdx.x >> 5];
-    int listed = 0;
-    auto flush = [&] {
-        __syncwarp();
-        best = with_more(best, lane < listed ? list[lane] : 0);
-        __syncwarp();
-        listed = 0;
-    };
-#pragma unroll
-    for (int k = 0; k < kUnroll; ++k)
-#pragma unroll
-        for (int e = 0; e < Vector<E>::N; ++e) {
-            const int i = x.first(k * 32 + lane) + e;
-            const float value = v[k].one(e);
-            const bool in = i >= 0 && i < x.V && order_of(value) >= bound;
-            const unsigned who = __ballot_sync(~0u, in);
-            if (!who) continue;
-            if (listed + __popc(who) > 32) flush();
-            if (in) list[listed + __popc(who & ((1u << lane) - 1))] = key_of(value, i);
-            listed += __popc(who);
-        }
-    flush();
-    if (lane < a.top) write_top(a, row, lane, best, r);
+    if (owner) to[y.target] = from_float<E>(gradient_at<false>(y, x_t, y.target));
 }
 
-// ---- long rows: a block, or a cluster of blocks, for each ----
+// ---- rows that a team of T threads, or a cluster of such blocks, sums up in one pass ----
 
+constexpr int kListed = 256;       // elements that reach the bound, before a slower way is taken
 template <int T>
 struct SumsShared {
     Sums warp[T / 32], cluster[kMaxCluster];
 };
 template <int T>
-struct BlockShared : SumsShared<T> {
-    unsigned long long top[T / 32][32];
-    unsigned long long cluster_top[kMaxCluster][32];
+struct TopShared {
+    uint32_t bound[T / 32][32];
+    int listed, threads;
+    uint16_t thread[T];
+    unsigned long long list[kListed], warp[T / 32][32], cluster[T > 32 ? kMaxCluster : 1][32];
+};
+struct NoTop {
+    int listed, threads;
 };
 
 template <int T>
-__device__ __forceinline__ Sums block_merged(Sums mine, Sums* shared, float c) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+__device__ __forceinline__ void team_sync() {
+    if constexpr (T == 32) __syncwarp();
+    else __syncthreads();
+}
+template <int T>
+__device__ __forceinline__ Sums team_merged(Sums mine, Sums* shared, float c) {
     mine = warp_merged(mine, c);
-    if (lane == 0) shared[warp] = mine;
+    if constexpr (T == 32) return mine;
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) shared[threadIdx.x >> 5] = mine;
     __syncthreads();
     return warp_merged(lane < T / 32 ? shared[lane] : Sums{-CUDART_INF_F, 0.0f, 0.0f}, c);
 }
-
-// The 32 largest keys of the block's warps, in warp 0.
-template <int T>
-__device__ __forceinline__ unsigned long long block_top(unsigned long long best, unsigned long long (*shared)[32]) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    __syncthreads();
+// The 32 largest keys of the team's warps, each warp's sorted, in its warp 0.
+template <int T, class K>
+__device__ __forceinline__ K team_top(K best, K (*shared)[32]) {
+    const int lane = threadIdx.x & 31, warp = (threadIdx.x % T) >> 5;
 #pragma unroll
     for (int half = T / 64; half; half >>= 1) {
         if (warp >= half && warp < 2 * half) shared[warp][lane] = best;
@@ -331,167 +306,263 @@ __device__ __forceinline__ unsigned long long block_top(unsigned long long best,
     return best;
 }
 
+// The part of a row that a block of a cluster takes: its whole vectors [lo, lo + n), and the vectors at the ends.
+template <class E>
+struct Part {
+    int lo, n;
+    bool head, tail;
+    __device__ __forceinline__ Part(const Row<E>& x, int rank, int blocks, int slice) {
+        const int begin = rank * slice, end = min(begin + slice, x.vectors);
+        lo = max(begin, x.lo);
+        n = max(min(end, x.hi) - lo, 0);
+        head = x.head() && rank == 0;
+        tail = x.tail() && begin < x.vectors && end == x.vectors;
+    }
+};
+
+// The sums of a thread's share of a part: every T-th of its whole vectors, which vector(i) gives, and `edge`.
+template <bool kEntropy, int T, class E, class Get>
+__device__ __forceinline__ Sums sums_of_part(const Part<E>& part, int tid, float c, const Vector<E>& edge, Get&& vector) {
+    constexpr int U = kUnroll;
+    Sums mine = {-CUDART_INF_F, 0.0f, 0.0f};
+    int i = tid;
+    const int ahead = 31 - (tid & 31);                 // a warp's lanes go the same way
+    for (; i + ahead + (U - 1) * T < part.n; i += U * T) {
+        Vector<E> in[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) in[k] = vector(i + k * T);
+        float most = in[0].max();
+#pragma unroll
+        for (int k = 1; k < U; ++k) most = max_nan(most, in[k].max());
+        add_vectors<kEntropy>(mine, in, most, c);
+    }
+    for (; i - (tid & 31) < part.n; i += U * T) {      // once, unless the last lanes have nothing where the first have all
+        Vector<E> in[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) in[k] = i + k * T < part.n ? vector(i + k * T) : Row<E>::nothing();
+        float most = in[0].max();
+#pragma unroll
+        for (int k = 1; k < U; ++k) most = max_nan(most, in[k].max());
+        add_vectors<kEntropy>(mine, in, most, c);
+    }
+    if ((part.head && tid < 32) || (part.tail && tid >= T - 32)) {
+        const Vector<E> in[1] = {edge};
+        add_vectors<kEntropy>(mine, in, edge.max(), c);
+    }
+    return mine;
+}
+// The vector of the row that is not whole and belongs to this thread: -1 for none.
+template <int T, class E>
+__device__ __forceinline__ int edge_of(const Row<E>& x, const Part<E>& part, int tid) {
+    return part.head && tid == 0 ? 0 : part.tail && tid == T - 1 ? x.vectors - 1 : -1;
+}
+
 template <class E, int T, bool kTop>
-__global__ void __launch_bounds__(T) block_kernel(RowArgs a) {
-    __shared__ BlockShared<T> sh;
-    extern __shared__ uint32_t group_max[];    // per 32 vectors of the slice: the order of their largest element
-    cg::cluster_group cluster = cg::this_cluster();
-    const int rank = (int)cluster.block_rank(), blocks = (int)cluster.num_blocks();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t row = blockIdx.x / blocks;
+__global__ void __launch_bounds__(T < 128 ? 128 : T) stream_kernel(RowArgs a) {
+    constexpr int kTeams = T < 128 ? 128 / T : 1;
+    __shared__ SumsShared<T> sums_shared[kTeams];
+    __shared__ std::conditional_t<kTop, TopShared<T>, NoTop> top_shared[kTeams];
+    const int tid = threadIdx.x % T, team = threadIdx.x / T, lane = threadIdx.x & 31;
+    auto& sh = sums_shared[team];
+    auto& st = top_shared[team];
+    int rank = 0, blocks = 1;
+    int64_t row = (int64_t)blockIdx.x * kTeams + team;
+    if constexpr (T > 32) {
+        rank = (int)cg::this_cluster().block_rank(), blocks = (int)cg::this_cluster().num_blocks();
+        row = blockIdx.x / blocks;
+    }
+    if (row >= a.rows) return;
     const int64_t t = a.targets ? a.targets[row] : 0;
     if (t < 0) {
-        if (rank == 0) write_nothing(a, row, threadIdx.x, T);
+        if (rank == 0) write_nothing(a, row, tid, T);
         return;
     }
-    if (blocks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // awaited before another block's memory is used
+    if (T > 32 && blocks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // awaited before another block's memory is used
+    if (kTop && tid == 0) st.listed = st.threads = 0;
     const Row<E> x(row_of<E>(a, row), a.vocab);
-    const float x_t = rank == 0 && threadIdx.x == 0 && a.logprob && t < a.vocab ? as_float(x.x[t]) : 0.0f;
+    const float x_t = rank == 0 && tid == 0 && a.logprob && t < a.vocab ? as_float(x.x[t]) : 0.0f;
     const float c = a.scale * kLog2E;
-    const int begin = rank * a.slice, end = min(begin + a.slice, x.vectors);
-    Sums mine = {-CUDART_INF_F, 0.0f, 0.0f};
-    for (int v = begin + threadIdx.x; v - lane < end; v += kUnroll * T) {
-        Vector<E> in[kUnroll];
-#pragma unroll
-        for (int k = 0; k < kUnroll; ++k) in[k] = v + k * T < end ? x.load(v + k * T) : Row<E>::nothing();
-        float most = -CUDART_INF_F;
-#pragma unroll
-        for (int k = 0; k < kUnroll; ++k) {
-            const float one = in[k].max();
-            most = max_nan(most, one);
-            if (kTop) {
-                const float group = warp_max_nan(one);
-                const int at = (v + k * T - begin) >> 5;
-                if (lane == 0 && v + k * T < end) group_max[at] = order_of(group);
-            }
-        }
-        add_vectors<true>(mine, in, most, c);
-    }
-    Sums all = block_merged<T>(mine, sh.warp, c);
+    const Part<E> part(x, rank, blocks, T > 32 ? a.slice : x.vectors);
+    const char* const from = reinterpret_cast<const char*>(x.x + x.first(part.lo));
+    const int edge = edge_of<T>(x, part, tid);
+    const Vector<E> at_edge = edge >= 0 ? x.partial(edge) : Row<E>::nothing();
+    auto vector = [&](int i) { return Row<E>::load_at(from + (int64_t)i * 16); };
+    const Sums mine = sums_of_part<true, T>(part, tid, c, at_edge, vector);
+    Sums all = team_merged<T>(mine, sh.warp, c);
     unsigned long long best = 0;
-    if (kTop) {
-        // The top largest elements lie in the top groups with the largest maxima (equal ones: the first of them): an element
-        // outside is behind the maxima of all these groups.  So: those groups, then what of them reaches the last one's maximum.
-        const int groups = (end - begin + 31) >> 5;
-        for (int g = warp * 32; g < groups; g += T) {
-            const int at = g + lane;
-            best = with_more(best, at < groups ? (unsigned long long)group_max[at] << 32 | (0xFFFFFFFFu - at) : 0);
+    if constexpr (kTop) {
+        // Every thread's largest element is one of the row's: the top-th largest of these bounds the top-th largest element
+        // from below.  Elements that reach the bound are in threads whose largest does: about `top` threads.  Those are read once
+        // more; their elements from the bound on - a few more than wanted, unless many are equal - are listed and sorted.
+        uint32_t order = sorted(order_of(mine.m));
+        if constexpr (T > 32) {
+            order = team_top<T>(order, st.bound);
+            if (tid < 32) st.bound[0][lane] = order;
+            __syncthreads();
+            order = st.bound[0][a.top - 1];
+        } else {
+            order = __shfl_sync(~0u, order, a.top - 1);
+            __syncwarp();
         }
-        best = block_top<T>(best, sh.top);
-        __syncthreads();
-        if (warp == 0) sh.top[0][lane] = best;
-        __syncthreads();
-        const uint32_t bound = (uint32_t)(sh.top[0][a.top - 1] >> 32);
-        best = 0;
-        for (int g = warp; g < a.top; g += T / 32) {
-            const unsigned long long group = sh.top[0][g];
-            if (!group) break;
-            const int v = begin + (int)position_of(group) * 32 + lane;
-            const Vector<E> in = v < end ? x.load(v) : Row<E>::nothing();
+        const float bound = value_of(order);              // NaN counts as above everything: "not below" is what is asked
+        if (!(mine.m < bound)) st.thread[atomicAdd(&st.threads, 1)] = (uint16_t)tid;
+        team_sync<T>();
+        const int threads = st.threads;
+        auto list = [&](float value, int i) {
+            if (value < bound) return;
+            const int at = atomicAdd(&st.listed, 1);
+            if (at < kListed) st.list[at] = key_of(value, i);
+        };
+        constexpr int kAtOnce = 4;                        // a warp's threads whose vectors it has in flight
+        for (int b = tid >> 5; b < threads; b += kAtOnce * (T / 32)) {
+            int first[kAtOnce];
 #pragma unroll
-            for (int e = 0; e < Vector<E>::N; ++e) {
-                const int i = x.first(v) + e;
-                const float value = in.one(e);
-                const bool counts = v < end && i >= 0 && i < x.V && order_of(value) >= bound;
-                if (__any_sync(~0u, counts)) best = with_more(best, counts ? key_of(value, i) : 0);
+            for (int k = 0; k < kAtOnce; ++k) first[k] = b + k * (T / 32) < threads ? st.thread[b + k * (T / 32)] : part.n;
+            for (int j = lane * T; j - lane * T < part.n; j += 32 * T) {
+                Vector<E> q[kAtOnce];
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) q[k] = first[k] + j < part.n ? vector(first[k] + j) : Row<E>::nothing();
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k)
+                    if (first[k] + j < part.n && !(q[k].max() < bound)) {
+                        const int n = x.first(part.lo + first[k] + j);
+#pragma unroll
+                        for (int e = 0; e < Vector<E>::N; ++e) list(q[k].one(e), n + e);
+                    }
             }
         }
-        best = block_top<T>(best, sh.top);
-    }
-    if (blocks > 1) {
-        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");    // every block has begun
-        if (warp == 0 && rank) {
-            BlockShared<T>* const first = cluster.map_shared_rank(&sh, 0);
-            if (lane == 0) first->cluster[rank] = all;
-            if (kTop) first->cluster_top[rank][lane] = best;
+        if (edge >= 0)
+            for (int i = max(x.first(edge), 0); i < min(x.first(edge + 1), x.V); ++i) list(as_float(x.x[i]), i);
+        team_sync<T>();
+        const int listed = st.listed;
+        if (listed <= kListed) {
+            if (tid < 32)
+                for (int n = 0; n < listed; n += 32) best = with_more(best, n + lane < listed ? st.list[n + lane] : 0ull);
+        } else {   // many are equal: every warp keeps the best it has seen, and takes only what is better
+            auto take = [&](bool in, float value, int i) {
+                const unsigned long long key = in ? key_of(value, i) : 0;
+                const bool better = key > __shfl_sync(~0u, best, a.top - 1);
+                if (__any_sync(~0u, better)) best = with_more(best, better ? key : 0ull);
+            };
+            for (int b = tid >> 5; b < threads; b += T / 32) {
+                for (int j = (int)st.thread[b] + lane * T; j - lane * T < part.n; j += 32 * T) {
+                    const Vector<E> q = j < part.n ? vector(j) : Row<E>::nothing();
+#pragma unroll
+                    for (int e = 0; e < Vector<E>::N; ++e) take(j < part.n, q.one(e), x.first(part.lo + j) + e);
+                }
+            }
+            if ((part.head && tid < 32) || (part.tail && tid >= T - 32))
+#pragma unroll
+                for (int e = 0; e < Vector<E>::N; ++e) {
+                    const int i = x.first(max(edge, 0)) + e;
+                    take(edge >= 0 && i >= 0 && i < x.V, at_edge.one(e), i);
+                }
+            if constexpr (T > 32) best = team_top<T>(best, st.warp);
         }
-        cluster.sync();
-        if (rank) return;
-        for (int b = 1; b < blocks; ++b) {
-            all = merged(all, sh.cluster[b], c);
-            if (kTop && warp == 0) best = merge_sorted(best, sh.cluster_top[b][31 - lane]);
-        }
     }
-    if (warp) return;
+    if constexpr (T > 32) {
+        if (blocks > 1) {
+            cg::cluster_group cluster = cg::this_cluster();
+            asm volatile("barrier.cluster.wait.aligned;" ::: "memory");    // every block has begun
+            if (tid < 32 && rank) {
+                if (lane == 0) cluster.map_shared_rank(&sh, 0)->cluster[rank] = all;
+                if constexpr (kTop) cluster.map_shared_rank(&st, 0)->cluster[rank][lane] = best;
+            }
+            cluster.sync();
+            if (rank) return;
+            for (int b = 1; b < blocks; ++b) {
+                all = merged(all, sh.cluster[b], c);
+                if constexpr (kTop)
+                    if (tid < 32) best = merge_sorted(best, st.cluster[b][31 - lane]);
+            }
+        }
+        if (tid >= 32) return;
+    }
     const RowStats r = stats_of(all);
     if (lane == 0) write_stats(a, row, t, x_t, r);
     if (kTop && lane < a.top) write_top(a, row, lane, best, r);
 }
 
-// The loss and its gradient of a long row.  The block's slice of the row is copied to shared memory (by the thread that
+// The loss and its gradient of a long row.  The block's part of the row is copied to shared memory (by the thread that
 // works on it: nothing to wait for but its own copies), summed up, and read again for the gradient when the cluster has
 // agreed on m and S.  kResident false: it does not fit, and is read from global memory again.
 template <class E, int T, bool kResident>
 __global__ void __launch_bounds__(T) loss_kernel(RowArgs a) {
+    constexpr int U = kUnroll, N = Vector<E>::N;
     __shared__ SumsShared<T> sh;
-    extern __shared__ uint4 slice[];
+    extern __shared__ uint4 kept[];
     cg::cluster_group cluster = cg::this_cluster();
-    const int rank = (int)cluster.block_rank(), blocks = (int)cluster.num_blocks();
+    const int rank = (int)cluster.block_rank(), blocks = (int)cluster.num_blocks(), tid = threadIdx.x;
     const int64_t row = blockIdx.x / blocks;
     const int64_t t = a.targets[row];
     const Row<E> x(row_of<E>(a, row), a.vocab);
-    const int begin = rank * a.slice, end = min(begin + a.slice, x.vectors);
+    const Part<E> part(x, rank, blocks, a.slice);
+    const char* const from = reinterpret_cast<const char*>(x.x + x.first(part.lo));
     const float c = a.scale * kLog2E;
+    const int edge = edge_of<T>(x, part, tid);
+    // the thread that writes the target's vector adds the target's own term
+    const int at = t >= 0 && t < a.vocab ? ((int)t + x.skip) / N - part.lo : -1;
+    const bool owner = at >= 0 && at < part.n && at % T == tid;
+    Vector<E> at_edge = Row<E>::nothing();
+    float x_t = 0.0f;
     Sums all = {0.0f, 1.0f, 0.0f};
+    auto vector = [&](int i) {
+        if (!kResident) return Row<E>::load_at(from + (int64_t)i * 16);
+        Vector<E> v;
+        v.w = kept[i];
+        return v;
+    };
     if (t >= 0) {
         if (blocks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-        if (kResident)
-            for (int v = begin + threadIdx.x; v < end; v += T) {
-                if (x.whole(v)) {
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(slice + (v - begin))), "l"(x.x + x.first(v))
-                                 : "memory");
-                } else {
-                    slice[v - begin] = x.partial(v).w;
-                }
-            }
-        const float x_t = rank == 0 && threadIdx.x == 0 && t < a.vocab ? as_float(x.x[t]) : 0.0f;
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        Sums mine = {-CUDART_INF_F, 0.0f, 0.0f};
-        for (int v = begin + threadIdx.x; v < end; v += kUnroll * T) {
-            Vector<E> in[kUnroll];
-#pragma unroll
-            for (int k = 0; k < kUnroll; ++k) {
-                const int n = v + k * T;
-                if (n >= end) in[k] = Row<E>::nothing();
-                else if (kResident) in[k].w = slice[n - begin];
-                else in[k] = x.load(n);
-            }
-            float most = -CUDART_INF_F;
-#pragma unroll
-            for (int k = 0; k < kUnroll; ++k) most = max_nan(most, in[k].max());
-            add_vectors<false>(mine, in, most, c);
+        if (kResident) {
+            const uint32_t to = (uint32_t)__cvta_generic_to_shared(kept);
+#pragma unroll 4
+            for (int i = tid; i < part.n; i += T)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * 16), "l"(from + (int64_t)i * 16) : "memory");
         }
-        all = block_merged<T>(mine, sh.warp, c);
+        if (edge >= 0) at_edge = x.partial(edge);
+        if ((owner || (rank == 0 && tid == 0)) && t < a.vocab) x_t = as_float(x.x[t]);
+        if (kResident) asm volatile("cp.async.wait_all;" ::: "memory");
+        all = team_merged<T>(sums_of_part<false, T>(part, tid, c, at_edge, vector), sh.warp, c);
         if (blocks > 1) {
             asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-            if ((int)threadIdx.x < blocks) cluster.map_shared_rank(&sh, threadIdx.x)->cluster[rank] = all;
+            if (tid < blocks) cluster.map_shared_rank(&sh, tid)->cluster[rank] = all;
             cluster.sync();       // the logits have been read by everybody: the gradient may take their place
             all = sh.cluster[0];
             for (int b = 1; b < blocks; ++b) all = merged(all, sh.cluster[b], c);
         } else {
             __syncthreads();
         }
-        if (rank == 0 && threadIdx.x == 0) write_stats(a, row, t, x_t, stats_of(all));
-    } else if (rank == 0 && threadIdx.x == 0) {
+        if (rank == 0 && tid == 0) write_stats(a, row, t, x_t, stats_of(all));
+    } else if (rank == 0 && tid == 0) {
         write_nothing(a, row, 0, 1);
     }
     const RowStats r = stats_of(all);
     const Gradient y = gradient_of(a, t, r.m, r.s, r.log_s, 0.0f, a.g_logprob[row], 0.0f);
     E* const to = static_cast<E*>(a.grad) + row * a.grad_stride;
-    if (((reinterpret_cast<uintptr_t>(to) - reinterpret_cast<uintptr_t>(x.x)) & 15) == 0) {
-        for (int v = begin + threadIdx.x; v < end; v += T) {
-            Vector<E> in;
-            if (kResident) in.w = slice[v - begin];
-            else in = x.load(v);
-            const Vector<E> out = gradient_at<false>(y, in, x.first(v));
-            if (x.whole(v)) store_whole(to + x.first(v), out);
-            else store_partial(to, x, v, out);
+    E* const out = to + x.first(part.lo);
+    if (aligned_alike(to, x.x)) {
+        int i = tid;
+        if (y.kind) {
+            const Vector<E> same = gradient_of_kind<E>(y);
+            for (; i < part.n; i += T) store_whole(out + i * N, same);
+        } else {
+            for (; i + (U - 1) * T < part.n; i += U * T) {
+                Vector<E> in[U];
+#pragma unroll
+                for (int k = 0; k < U; ++k) in[k] = vector(i + k * T);
+#pragma unroll
+                for (int k = 0; k < U; ++k) store_whole(out + (i + k * T) * N, gradient_at<false>(y, in[k]));
+            }
+            for (; i < part.n; i += T) store_whole(out + i * N, gradient_at<false>(y, vector(i)));
+            if (owner) to[t] = from_float<E>(gradient_at<false>(y, x_t, (int)t));
         }
     } else {   // the rows of the gradient are aligned otherwise than the logits': element by element, neighbours by neighbours
-        const int i0 = max(x.first(begin), 0), i1 = min(x.first(end), x.V);
-        const E* const kept = reinterpret_cast<const E*>(slice) - x.first(begin);
-        for (int i = i0 + threadIdx.x; i < i1; i += T) to[i] = from_float<E>(gradient_at<false>(y, as_float(kResident ? kept[i] : x.x[i]), i));
+        const E* const elements = kResident ? reinterpret_cast<const E*>(kept) : reinterpret_cast<const E*>(from);
+        const int first = x.first(part.lo);
+        for (int i = tid; i < part.n * N; i += T) out[i] = from_float<E>(gradient_at<false>(y, as_float(elements[i]), first + i));
     }
+    if (edge >= 0) store_partial<false>(to, x, edge, at_edge, y);
 }
 
 // ---- the gradient alone, from the sums that the log probabilities left ----
@@ -510,24 +581,28 @@ __global__ void __launch_bounds__(256) grad_kernel(RowArgs a, int segments) {
     if (row >= a.rows) return;
     const Row<E> x(row_of<E>(a, row), a.vocab);
     const int v = (int)(item - row * segments) * L * kUnroll + sub;
+    E* const to = static_cast<E*>(a.grad) + row * a.grad_stride;
+    if (!aligned_alike(to, x.x)) {
+        const Gradient y = gradient_from_norm(a, row);
+        const int lo = max(x.first(v - sub), 0), hi = min(x.first(v - sub + L * kUnroll), x.V);
+        for (int i = lo + sub; i < hi; i += L) to[i] = from_float<E>(gradient_at<kEntropy>(y, as_float(x.x[i]), i));
+        return;
+    }
     Vector<E> in[kUnroll];
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) in[k] = x.load(v + L * k);
     const Gradient y = gradient_from_norm(a, row);
-    E* const to = static_cast<E*>(a.grad) + row * a.grad_stride;
-    if (((reinterpret_cast<uintptr_t>(to) - reinterpret_cast<uintptr_t>(x.x)) & 15) == 0) {
+    // the lane that writes the target's vector adds the target's own term
+    const int at = y.target >= 0 ? (y.target + x.skip) / Row<E>::N : -1;
+    const bool owner = at >= v && (at - v) % L == 0 && at - v < L * kUnroll && x.whole(at);
+    const float x_t = owner ? as_float(x.x[y.target]) : 0.0f;
 #pragma unroll
-        for (int k = 0; k < kUnroll; ++k) {
-            const int n = v + L * k;
-            if (n >= x.vectors) continue;
-            const Vector<E> out = gradient_at<kEntropy>(y, in[k], x.first(n));
-            if (x.whole(n)) store_whole(to + x.first(n), out);
-            else store_partial(to, x, n, out);
-        }
-    } else {
-        const int lo = max(x.first(v - sub), 0), hi = min(x.first(v - sub + L * kUnroll), x.V);
-        for (int i = lo + sub; i < hi; i += L) to[i] = from_float<E>(gradient_at<kEntropy>(y, as_float(x.x[i]), i));
+    for (int k = 0; k < kUnroll; ++k) {
+        const int n = v + L * k;
+        if (x.whole(n)) store_whole(to + x.first(n), y.kind ? gradient_of_kind<E>(y) : gradient_at<kEntropy>(y, in[k]));
+        else if (n < x.vectors) store_partial<kEntropy>(to, x, n, in[k], y);
     }
+    if (owner) to[y.target] = from_float<E>(gradient_at<kEntropy>(y, x_t, y.target));
 }
 
 // Few elements a row: L lanes share one, element by element.
@@ -604,7 +679,7 @@ cudaError_t launch(void (*kernel)(Params...), int64_t blocks, int threads, size_
     attr[0].val.clusterDim.x = (unsigned)cluster;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
@@ -623,35 +698,35 @@ template <class E>
 bool fits_a_warp(int vocab) { return most_vectors<E>(vocab) <= 32 * kUnroll; }
 
 template <class E, bool kGrad>
-cudaError_t launch_short(const RowArgs& a, cudaStream_t st) {
-    auto blocks = [&](int64_t per) { return (a.rows + per - 1) / per; };
-    if (a.vocab <= 16) return launch(narrow_kernel<E, 4, 4, kGrad>, blocks(256 / 4), 256, 0, 1, st, a);
-    if (a.vocab <= kNarrow) return launch(narrow_kernel<E, 16, 4, kGrad>, blocks(256 / 16), 256, 0, 1, st, a);
-    return launch(warp_kernel<E, kGrad>, blocks(4), 128, 0, 1, st, a);
+cudaError_t launch_narrow(const RowArgs& a, cudaStream_t st) {
+    if (a.vocab <= 16) return launch(narrow_kernel<E, 4, 4, kGrad>, (a.rows + 63) / 64, 256, 0, 1, st, a);
+    return launch(narrow_kernel<E, 16, 4, kGrad>, (a.rows + 15) / 16, 256, 0, 1, st, a);
 }
 
 template <class E, int T>
-cudaError_t launch_block(RowArgs a, int cluster, cudaStream_t st) {
+cudaError_t launch_stream(RowArgs a, int cluster, cudaStream_t st) {
     a.slice = slice_of(most_vectors<E>(a.vocab), cluster);
-    return a.top ? launch(block_kernel<E, T, true>, a.rows * cluster, T, (size_t)a.slice / 32 * 4, cluster, st, a)
-                 : launch(block_kernel<E, T, false>, a.rows * cluster, T, 0, cluster, st, a);
+    const int64_t blocks = T == 32 ? (a.rows + 3) / 4 : a.rows * cluster;
+    return launch(a.top ? stream_kernel<E, T, true> : stream_kernel<E, T, false>, blocks, T < 128 ? 128 : T, 0, cluster, st, a);
 }
 
 template <class E>
 cudaError_t launch_logprobs(const RowArgs& a, cudaStream_t st) {
-    if (a.vocab <= kNarrow || fits_a_warp<E>(a.vocab)) return launch_short<E, false>(a, st);
+    if (a.vocab <= kNarrow) return launch_narrow<E, false>(a, st);
     const int vectors = most_vectors<E>(a.vocab);
+    if (vectors <= 32 * kUnroll || (a.rows >= 16 * kSms && vectors <= 2048)) return launch_stream<E, 32>(a, 1, st);
     int cluster = 1;
     while (cluster < kMaxCluster && a.rows * cluster * 2 <= 2 * kSms && vectors / (2 * cluster) >= 256) cluster *= 2;
     const int each = vectors / cluster;
-    if (each <= 1024) return launch_block<E, 128>(a, cluster, st);
-    if (each <= 4096) return launch_block<E, 256>(a, cluster, st);
-    return launch_block<E, 512>(a, cluster, st);
+    if (each <= 1024) return launch_stream<E, 128>(a, cluster, st);
+    if (each <= 4096 || a.rows * cluster > 2 * kSms) return launch_stream<E, 256>(a, cluster, st);
+    return launch_stream<E, 512>(a, cluster, st);
 }
 
 template <class E>
 cudaError_t launch_loss(RowArgs a, cudaStream_t st) {
-    if (a.vocab <= kNarrow || fits_a_warp<E>(a.vocab)) return launch_short<E, true>(a, st);
+    if (a.vocab <= kNarrow) return launch_narrow<E, true>(a, st);
+    if (fits_a_warp<E>(a.vocab)) return launch(warp_loss_kernel<E>, (a.rows + 3) / 4, 128, 0, 1, st, a);
     const int vectors = most_vectors<E>(a.vocab);
     int cluster = 1;
     while (cluster < kMaxCluster && ((a.rows * cluster * 2 <= 2 * kSms && vectors / (2 * cluster) >= 256) || (size_t)slice_of(vectors, cluster) * 16 > kSliceBytes))

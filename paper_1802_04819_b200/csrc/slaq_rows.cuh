@@ -128,18 +128,24 @@ struct Vector {
     __device__ __forceinline__ float one(int e) const { return as_float(reinterpret_cast<const E*>(&w)[e]); }
 };
 
-// The 16-byte vectors that a row of V elements touches: the row begins with element `skip` of vector 0.  Vectors that lie
-// inside the row are read whole, the (at most two) others element by element, -inf in the places outside.
+// The 16-byte vectors that a row of V elements touches: the row begins with element `skip` of vector 0.  The vectors that lie
+// inside the row, [lo, hi), are read and written whole; the others, at most one at each end, element by element, with -inf in
+// the places outside.
 template <class E>
 struct Row {
     static constexpr int N = Vector<E>::N;
     const E* x;
-    int V, skip, vectors;
+    int V, skip, vectors, lo, hi;
     __device__ __forceinline__ Row(const E* row, int n) : x(row), V(n), skip((int)(reinterpret_cast<uintptr_t>(row) & 15) / (int)sizeof(E)) {
         vectors = (skip + n + N - 1) / N;
+        lo = skip || n < N ? 1 : 0;
+        hi = (skip + n) % N ? vectors - 1 : vectors;
+        if (hi < lo) hi = lo;                              // one vector in all, not whole
     }
+    __device__ __forceinline__ bool head() const { return lo == 1; }
+    __device__ __forceinline__ bool tail() const { return hi < vectors; }
     __device__ __forceinline__ int first(int v) const { return v * N - skip; }   // the element a vector begins with
-    __device__ __forceinline__ bool whole(int v) const { return first(v) >= 0 && first(v) + N <= V; }
+    __device__ __forceinline__ bool whole(int v) const { return v >= lo && v < hi; }
     __device__ __forceinline__ Vector<E> partial(int v) const {
         Vector<E> r;
         E* const e = reinterpret_cast<E*>(&r.w);
@@ -150,11 +156,14 @@ struct Row {
         }
         return r;
     }
-    __device__ __forceinline__ Vector<E> load(int v) const {
-        if (!whole(v)) return v >= 0 && v < vectors ? partial(v) : nothing();
+    static __device__ __forceinline__ Vector<E> load_at(const void* p) {
         Vector<E> r;
-        asm("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.w.x), "=r"(r.w.y), "=r"(r.w.z), "=r"(r.w.w) : "l"(x + first(v)));
+        asm("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.w.x), "=r"(r.w.y), "=r"(r.w.z), "=r"(r.w.w) : "l"(p));
         return r;
+    }
+    __device__ __forceinline__ Vector<E> load(int v) const {
+        if (whole(v)) return load_at(x + first(v));
+        return v >= 0 && v < vectors ? partial(v) : nothing();
     }
     static __device__ __forceinline__ Vector<E> nothing() {
         const uint32_t b = sizeof(E) == 4 ? 0xFF800000u : std::is_same_v<E, __half> ? 0xFC00FC00u : 0xFF80FF80u;
@@ -226,15 +235,18 @@ __device__ __forceinline__ void add_vectors(Sums& a, const Vector<E> (&x)[U], fl
 }
 
 // ---- the largest keys of a warp: lane i holds the i-th largest, 0 where there is none ----
-__device__ __forceinline__ unsigned long long larger_if(bool want, unsigned long long a, unsigned long long b) { return (a > b) == want ? a : b; }
-__device__ __forceinline__ unsigned long long merge_sorted(unsigned long long a, unsigned long long b_reversed) {
+template <class K>
+__device__ __forceinline__ K larger_if(bool want, K a, K b) { return (a > b) == want ? a : b; }
+template <class K>
+__device__ __forceinline__ K merge_sorted(K a, K b_reversed) {
     const int lane = threadIdx.x & 31;
     a = a > b_reversed ? a : b_reversed;
 #pragma unroll
     for (int o = 16; o; o >>= 1) a = larger_if(!(lane & o), a, __shfl_xor_sync(~0u, a, o));
     return a;
 }
-__device__ __forceinline__ unsigned long long sorted(unsigned long long a) {
+template <class K>
+__device__ __forceinline__ K sorted(K a) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int n = 2; n <= 32; n *= 2)
@@ -242,7 +254,8 @@ __device__ __forceinline__ unsigned long long sorted(unsigned long long a) {
         for (int o = n / 2; o; o >>= 1) a = larger_if(!(lane & o) == !(lane & n), a, __shfl_xor_sync(~0u, a, o));
     return a;
 }
-__device__ __forceinline__ unsigned long long with_more(unsigned long long best, unsigned long long unsorted) {
+template <class K>
+__device__ __forceinline__ K with_more(K best, K unsorted) {
     return merge_sorted(best, __shfl_sync(~0u, sorted(unsorted), 31 - (threadIdx.x & 31)));
 }
 

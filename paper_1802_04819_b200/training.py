@@ -27,7 +27,7 @@ F32, BF16, F16 = 0, 1, 2
 MAX_VOCAB, MAX_TOP = 1 << 22, 32
 STATE_BLOCK = 256
 
-_torch = None
+_torch = _current_stream = _current_device = None
 _types = {}
 
 
@@ -36,10 +36,13 @@ def _lib():
 
 
 def _load():
-    global _torch
+    global _torch, _current_stream, _current_device
     if _torch is None:
         import torch
         _types.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+        # the address alone: torch.cuda.current_stream() makes an object, 3 of the 8 us of a call
+        _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
+        _current_device = torch.cuda.current_device
         _torch = torch
     return _torch
 
@@ -108,9 +111,8 @@ def _elsewhere(stream, device):
 
 
 def _on(stream, device):
-    torch = _load()
-    if stream is None and device == torch.cuda.current_device():
-        return _Here(torch.cuda.current_stream().cuda_stream)
+    if stream is None and device == _current_device():
+        return _Here(_current_stream(device))
     return _elsewhere(stream, device)
 
 
