@@ -601,7 +601,7 @@ typedef struct slaq_adamw_handle slaq_adamw_t;
  * slaq_adamw_workspace_bytes() long, that outlives the plan.  Host arrays; the call returns when the plan is on the device and
  * must not be captured.  Any alignment of the tensors that suits their type will do.
  * Errors: SLAQ_E_ARG (null, unknown types, a group out of range, betas outside [0, 1), a tensor listed twice, tensors that
- * overlap one another or a gradient), SLAQ_E_RANGE (2^40 elements, or 2^39 in all), SLAQ_E_NOMEM, SLAQ_E_CUDA.
+ * overlap one another or a gradient), SLAQ_E_RANGE (more than 2^38 elements), SLAQ_E_NOMEM, SLAQ_E_CUDA.
  */
 int slaq_adamw_create(void* dev_ws, size_t bytes, int32_t n_tensors, const slaq_adamw_tensor* tensors, int32_t n_groups,
                       const slaq_adamw_group* groups, int param_type, int grad_type, int state_bits, void* cuda_stream,
