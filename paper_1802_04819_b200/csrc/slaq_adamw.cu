@@ -23,7 +23,6 @@ namespace {
 
 constexpr int kBlock = 256;          // elements that share a scale, and what a warp works on at a time: 8 a lane
 constexpr int kThreads = 128;
-constexpr bool kAhead = true;
 constexpr int64_t kMostElements = (int64_t)1 << 38;   // of a plan: its blocks are counted in 31 bits
 constexpr float kE4m3Max = 448.0f;
 constexpr float kTiny = 7.888609052210118e-31f;   // 2^-100: a block with nothing above it is kept as zeros
@@ -36,7 +35,7 @@ struct TensorRef {
     float* avg_scale;
     float* sq_scale;
     int64_t n;
-    int32_t group, first;            // the number of its first block among all tensors' blocks
+    int32_t group, first;            // the number of its first unit among all tensors' units
 };
 
 // What a step needs of a group, ready for its next step: the block that finishes a step last moves it on.
@@ -68,143 +67,180 @@ __device__ inline void advance(Group& g) {
 struct StepArgs {
     const TensorRef* tensors;
     const void* const* grads;
-    const int32_t* tensor_of;        // per block
-    int32_t n_blocks, n_groups;
+    const int32_t* tensor_of;        // per unit
+    int32_t n_units, n_groups, unit; // blocks of a unit, a power of two
     Group* groups;
     const int32_t* active;
     unsigned int* ticket;
 };
 
-// 8 elements as they lie in memory.
+// Eight elements of a lane, two by two: the arithmetic is on pairs, which take one instruction together.
+struct Eight {
+    Pair at[4];
+    __device__ __forceinline__ void get(int k, float& a, float& b) const { split(at[k], a, b); }
+    __device__ __forceinline__ void set(int k, float a, float b) { at[k] = pair_of(a, b); }
+};
+// .. as they lie in memory
 template <class E>
 struct Raw {
     uint4 w[sizeof(E) / 2];
-    __device__ __forceinline__ void load(const E* from) {
+    __device__ __forceinline__ void load(const void* from) {
 #pragma unroll
-        for (int k = 0; k < (int)sizeof(E) / 2; ++k) w[k] = reinterpret_cast<const uint4*>(from)[k];
+        for (int k = 0; k < (int)sizeof(E) / 2; ++k) w[k] = static_cast<const uint4*>(from)[k];
     }
-    __device__ __forceinline__ void store(E* to) const {
+    __device__ __forceinline__ void store(void* to) const {
 #pragma unroll
-        for (int k = 0; k < (int)sizeof(E) / 2; ++k) reinterpret_cast<uint4*>(to)[k] = w[k];
+        for (int k = 0; k < (int)sizeof(E) / 2; ++k) static_cast<uint4*>(to)[k] = w[k];
     }
-    __device__ __forceinline__ void unpack(float (&x)[8]) const {
+    __device__ __forceinline__ Eight unpack() const {
+        Eight x;
 #pragma unroll
-        for (int k = 0; k < 8; k += 2) {
-            Vector<E> v;
-            v.w = w[k * sizeof(E) / 16];
-            split(v.at(k % Vector<E>::N / 2), x[k], x[k + 1]);
-        }
+        for (int k = 0; k < 4; ++k) x.at[k] = Vector<E>{w[2 * k * sizeof(E) / 16]}.at(2 * k % Vector<E>::N / 2);
+        return x;
     }
-    __device__ __forceinline__ void pack(const float (&x)[8]) {
+    __device__ __forceinline__ void pack(const Eight& x) {
 #pragma unroll
-        for (int k = 0; k < 8; k += 2) {
-            Vector<E> v;
-            v.w = w[k * sizeof(E) / 16];
-            v.put(k % Vector<E>::N / 2, pair_of(x[k], x[k + 1]));
-            w[k * sizeof(E) / 16] = v.w;
+        for (int k = 0; k < 4; ++k) {
+            Vector<E> v{w[2 * k * sizeof(E) / 16]};
+            v.put(2 * k % Vector<E>::N / 2, x.at[k]);
+            w[2 * k * sizeof(E) / 16] = v.w;
         }
     }
 };
-// The elements i .. i + 8 of n; `whole`: all of them are there, and the address is a multiple of 16 bytes.
 template <class E>
-__device__ __forceinline__ void load8(const E* from, int64_t i, int64_t n, bool whole, float (&x)[8]) {
-    if (whole) {
-        Raw<E> r;
-        r.load(from + i);
-        r.unpack(x);
-    } else {
+__device__ __forceinline__ void store_whole8(E* to, const Eight& x) {
+    Raw<E> r = {};
+    r.pack(x);
+    r.store(to);
+}
+// .. element by element, as many as `n` of them there are
+template <class E>
+__device__ __forceinline__ Eight load_some(const E* from, int64_t n) {
+    Eight x;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = i + k < n ? as_float(from[i + k]) : 0.0f;
-    }
+    for (int k = 0; k < 8; k += 2) x.set(k / 2, k < n ? as_float(from[k]) : 0.0f, k + 1 < n ? as_float(from[k + 1]) : 0.0f);
+    return x;
 }
 template <class E>
-__device__ __forceinline__ void store8(E* to, int64_t i, int64_t n, bool whole, const float (&x)[8]) {
-    if (whole) {
-        Raw<E> r = {};
-        r.pack(x);
-        r.store(to + i);
-    } else {
+__device__ __forceinline__ void store_some(E* to, int64_t n, const Eight& x) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (i + k < n) to[i + k] = from_float<E>(x[k]);
+    for (int k = 0; k < 8; k += 2) {
+        float a, b;
+        x.get(k / 2, a, b);
+        if (k < n) to[k] = from_float<E>(a);
+        if (k + 1 < n) to[k + 1] = from_float<E>(b);
     }
 }
 
-// 8 codes and their scale
-__device__ __forceinline__ void unpack_codes(uint2 b, float scale, float (&x)[8]) {
+// 8 codes
+__device__ __forceinline__ Eight unpack_codes(uint2 b) {
+    Eight x;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const uint32_t w = k < 2 ? b.x : b.y;
         const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(k & 1 ? w >> 16 : w), __NV_E4M3);
         const float2 f = __half22float2(__half2(h));
-        x[2 * k] = f.x * scale;
-        x[2 * k + 1] = f.y * scale;
+        x.set(k, f.x, f.y);
     }
+    return x;
 }
-__device__ __forceinline__ void load8_codes(const uint8_t* from, int64_t i, int64_t n, float scale, float (&x)[8]) {
+__device__ __forceinline__ uint2 load_some_codes(const uint8_t* from, int64_t n) {
     uint32_t b[2] = {0, 0};
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-        if (i + k < n) b[k / 4] |= (uint32_t)from[i + k] << (k % 4 * 8);
-    unpack_codes(make_uint2(b[0], b[1]), scale, x);
+        if (k < n) b[k / 4] |= (uint32_t)from[k] << (k % 4 * 8);
+    return make_uint2(b[0], b[1]);
 }
+__device__ __forceinline__ void store_some_codes(uint8_t* to, int64_t n, uint2 b) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (k < n) to[k] = (uint8_t)((k < 4 ? b.x : b.y) >> (k % 4 * 8));
+}
+
 __device__ __forceinline__ float max_size(float a, float b) {   // max of |a| and |b|, sign aside; NaN as soon as one is
     float y;
     asm("max.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
     return y;
 }
-// The codes of the warp's 256 values and their scale, largest / 448.  What is not finite stays so in its own element (NaN).
+// The largest |x| of the warp, as bits: a NaN stands above all.
 template <bool kPositive>
-__device__ __forceinline__ uint2 to_codes(float* scale, int lane, const float (&x)[8]) {
-    float most = x[0];
+__device__ __forceinline__ float largest(const Eight& x) {
+    float a, b;
+    x.get(0, a, b);
+    float most = kPositive ? max_nan(a, b) : max_size(a, b);
 #pragma unroll
-    for (int k = 1; k < 8; ++k) most = kPositive ? max_nan(most, x[k]) : max_size(most, x[k]);
-    most = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(fabsf(most))));   // a NaN's bits stand above all
-    const bool finite = most < CUDART_INF_F;
-    if (!finite) {
-        most = 0.0f;
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (fabsf(x[k]) < CUDART_INF_F) most = fmaxf(most, fabsf(x[k]));
-        most = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(most)));
+    for (int k = 1; k < 4; ++k) {
+        x.get(k, a, b);
+        most = kPositive ? max_nan(most, max_nan(a, b)) : max_size(most, max_size(a, b));
     }
-    const bool kept = most >= kTiny;
-    const float inverse = kept ? __fdiv_rn(kE4m3Max, most) : 0.0f;
-    if (lane == 0) *scale = kept ? __fdiv_rn(most, kE4m3Max) : 0.0f;
-    float y[8];
+    return __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(fabsf(most))));
+}
+__device__ __forceinline__ float largest_finite(const Eight& x) {
+    float most = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) y[k] = x[k] * inverse;
-    if (kPositive && kept) {
+    for (int k = 0; k < 4; ++k) {
+        float a, b;
+        x.get(k, a, b);
+        if (fabsf(a) < CUDART_INF_F) most = fmaxf(most, fabsf(a));
+        if (fabsf(b) < CUDART_INF_F) most = fmaxf(most, fabsf(b));
+    }
+    return __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(most)));
+}
+template <bool kPositive>
+__device__ __forceinline__ uint2 codes_of(const Eight& x, float inverse, bool finite) {
+    Eight y;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) y.at[k] = x.at[k] * pair_of(inverse, inverse);
+    if (kPositive) {
         constexpr float kLeast = 0.001953125f;   // 2^-9, the smallest code
-        float least = y[0];
+        float least = kLeast;
 #pragma unroll
-        for (int k = 1; k < 8; ++k) least = fminf(least, y[k]);
-        if (least < kLeast)
+        for (int k = 0; k < 4; ++k) {
+            float a, b;
+            y.get(k, a, b);
+            least = fminf(least, fminf(a, b));
+        }
+        if (least < kLeast && inverse > 0.0f)
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (x[k] > 0.0f) y[k] = fmaxf(y[k], kLeast);
+            for (int k = 0; k < 4; ++k) {
+                float a, b, p, q;
+                x.get(k, a, b);
+                y.get(k, p, q);
+                y.set(k, a > 0.0f ? fmaxf(p, kLeast) : p, b > 0.0f ? fmaxf(q, kLeast) : q);
+            }
     }
     uint32_t b[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
+        float p, q;
+        y.get(k, p, q);
         uint16_t two;
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(y[2 * k + 1]), "f"(y[2 * k]));
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(q), "f"(p));
         b[k] = two;
         if (!finite) {
-            if (!(fabsf(x[2 * k]) < CUDART_INF_F)) b[k] = (b[k] & 0xFF00u) | 0x7F;
-            if (!(fabsf(x[2 * k + 1]) < CUDART_INF_F)) b[k] = (b[k] & 0xFFu) | 0x7F00;
+            x.get(k, p, q);
+            if (!(fabsf(p) < CUDART_INF_F)) b[k] = (b[k] & 0xFF00u) | 0x7F;
+            if (!(fabsf(q) < CUDART_INF_F)) b[k] = (b[k] & 0xFFu) | 0x7F00;
         }
     }
     return make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410));
 }
-__device__ __forceinline__ void store8_codes(uint8_t* to, int64_t i, int64_t n, bool whole, uint2 b) {
-    if (whole) {
-        *reinterpret_cast<uint2*>(to + i) = b;
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (i + k < n) to[i + k] = (uint8_t)((k < 4 ? b.x : b.y) >> (k % 4 * 8));
-    }
+// Both states of the warp's 256 elements as codes, and their scales, largest / 448.  What is not finite stays so in its own
+// element (NaN).
+struct Codes {
+    uint2 m, r;
+    float m_scale, r_scale;
+};
+__device__ __forceinline__ Codes encode(const Eight& m, const Eight& r, int lane) {
+    float most_m = largest<false>(m), most_r = largest<true>(r);
+    const bool finite = most_m < CUDART_INF_F && most_r < CUDART_INF_F;
+    if (!finite) most_m = largest_finite(m), most_r = largest_finite(r);
+    // lanes 0 and 1 divide for the scales of m and r, lanes 2 and 3 for their inverses; nothing is kept of what is too small
+    const float most = lane & 1 ? most_r : most_m;
+    float q = __fdiv_rn(lane & 2 ? kE4m3Max : most, lane & 2 ? most : kE4m3Max);
+    q = most >= kTiny ? q : 0.0f;
+    return {codes_of<false>(m, __shfl_sync(~0u, q, 2), finite), codes_of<true>(r, __shfl_sync(~0u, q, 3), finite), __shfl_sync(~0u, q, 0),
+            __shfl_sync(~0u, q, 1)};
 }
 
 // sqrt and 1/x to 1 ulp or two, denormal arguments of the root included
@@ -223,120 +259,27 @@ __device__ __forceinline__ float reciprocal(float x) {
 struct Numbers {
     float b1, a1, b2, a2, correct, eps, keep, size, grad_scale;
 };
-// 8 elements' step: new weights, first moments, and second moments (their roots, if kRoot)
+// The step of 8 elements: new weights, first moments, and second moments (their roots, if kRoot).  m and v come in units:
+// b1 and b2 hold the units' values.
 template <bool kRoot>
-__device__ __forceinline__ void step8(const Numbers& c, float (&p)[8], const float (&g)[8], float (&m)[8], float (&v)[8]) {
+__device__ __forceinline__ void step8(const Numbers& c, float b1, float b2, Eight& p, const Eight& g, Eight& m, Eight& v) {
+    auto two = [](float x) { return pair_of(x, x); };
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float x = g[j] * c.grad_scale;
-        m[j] = fmaf(c.b1, m[j], c.a1 * x);
-        v[j] = fmaf(c.b2, v[j], c.a2 * (x * x));
-        const float r = root(v[j]);
-        p[j] = fmaf(-c.size, m[j] * reciprocal(fmaf(r, c.correct, c.eps)), p[j] * c.keep);
-        if (kRoot) v[j] = r;
+    for (int k = 0; k < 4; ++k) {
+        const Pair x = g.at[k] * two(c.grad_scale);
+        m.at[k] = fma2(two(b1), m.at[k], two(c.a1) * x);
+        v.at[k] = fma2(two(c.a2) * x, x, two(b2) * v.at[k]);
+        float a, b;
+        v.get(k, a, b);
+        const Pair r = pair_of(root(a), root(b));
+        split(fma2(r, two(c.correct), two(c.eps)), a, b);
+        p.at[k] = fma2(two(-c.size), m.at[k] * pair_of(reciprocal(a), reciprocal(b)), p.at[k] * two(c.keep));
+        if (kRoot) v.at[k] = r;
     }
 }
 
-template <bool kEight>
-struct RawState : Raw<float> {
-    __device__ __forceinline__ void load(const void* from, const float*, int64_t, int64_t i) { Raw<float>::load(static_cast<const float*>(from) + i); }
-};
-template <>
-struct RawState<true> {
-    uint2 w;
-    float scale;
-    __device__ __forceinline__ void load(const void* from, const float* scales, int64_t block, int64_t i) {
-        w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(from) + i);
-        scale = scales[block];
-    }
-    __device__ __forceinline__ void unpack(float (&x)[8]) const { unpack_codes(w, scale, x); }
-};
-
-// Warp w of W takes blocks w, w + W, .. of all tensors' blocks in a row: the GPU's warps pass through a tensor side by side, which
-// DRAM likes best (with a run of blocks for each warp it gave a sixth less), and what a tensor's blocks have in common is fetched
-// again only when the tensor changes.
-template <class P, class G, bool kMaster, bool kEight>
-__global__ void __launch_bounds__(kThreads) step_kernel(StepArgs a) {
-    using W = std::conditional_t<kMaster, float, P>;      // what the step works on
-    const int lane = threadIdx.x & 31;
-    const int warps = gridDim.x * (kThreads / 32);
-    int at = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-    auto tensor_of = [&](int b) { return (unsigned)b < (unsigned)a.n_blocks ? a.tensor_of[b] : -1; };   // n_blocks + 2 warps < 2^32
-    int current = -1, tensor = tensor_of(at), next = tensor_of(at + warps);
-    TensorRef t = {};
-    const G* grad = nullptr;
-    W* weights = nullptr;
-    Numbers c = {};
-    bool on = false, wide = false, fetched = false;
-    Raw<G> rg;
-    Raw<W> rw;
-    RawState<kEight> ra, rs;
-    float p[8], g[8], m[8], v[8];
-    for (; tensor >= 0; at += warps) {
-        const int after = tensor_of(at + 2 * warps);
-        if (tensor != current) {
-            current = tensor;
-            t = a.tensors[tensor];
-            on = !a.active || a.active[t.group] > 0;
-            grad = static_cast<const G*>(a.grads[tensor]);
-            weights = kMaster ? reinterpret_cast<W*>(t.master) : static_cast<W*>(t.param);
-            const Group& group = a.groups[t.group];
-            c = {group.b1, group.a1, group.b2, group.a2, group.correct, group.eps, group.keep, group.size, group.grad_scale};
-            uintptr_t low = (uintptr_t)t.param | (uintptr_t)grad | (uintptr_t)weights;
-            if (!kEight) low |= (uintptr_t)t.avg | (uintptr_t)t.sq;
-            wide = (low & 15) == 0 && (!kEight || (((uintptr_t)t.avg | (uintptr_t)t.sq) & 7) == 0);
-        }
-        const bool more = next == current;
-        tensor = next;
-        next = after;
-        if (!on) continue;
-        const int64_t block = at - t.first, i = block * kBlock + lane * 8;
-        const bool full = wide && (block + 1) * kBlock <= t.n;
-        if (full) {
-            auto load = [&](int64_t b) {
-                const int64_t i = b * kBlock + lane * 8;
-                rg.load(grad + i);
-                rw.load(weights + i);
-                ra.load(t.avg, t.avg_scale, b, i);
-                rs.load(t.sq, t.sq_scale, b, i);
-            };
-            if (!fetched) load(block);
-            rg.unpack(g);
-            rw.unpack(p);
-            ra.unpack(m);
-            rs.unpack(v);
-            fetched = kAhead && more && (block + warps + 1) * kBlock <= t.n;
-            if (fetched) load(block + warps);             // on its way while this one is computed
-            if (kEight)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] *= v[j];
-        } else {                                          // a tensor's last block, or tensors that are not aligned
-            const bool whole = wide && i + 8 <= t.n;
-            load8(grad, i, t.n, whole, g);
-            load8(weights, i, t.n, whole, p);
-            if (kEight) {
-                load8_codes(static_cast<const uint8_t*>(t.avg), i, t.n, t.avg_scale[block], m);
-                load8_codes(static_cast<const uint8_t*>(t.sq), i, t.n, t.sq_scale[block], v);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] *= v[j];
-            } else {
-                load8(static_cast<const float*>(t.avg), i, t.n, whole, m);
-                load8(static_cast<const float*>(t.sq), i, t.n, whole, v);
-            }
-        }
-        const bool whole = full || (wide && i + 8 <= t.n);
-        step8<kEight>(c, p, g, m, v);
-        if (kMaster) store8(t.master, i, t.n, whole, p);
-        store8(static_cast<P*>(t.param), i, t.n, whole, p);
-        if (kEight) {
-            store8_codes(static_cast<uint8_t*>(t.avg), i, t.n, whole, to_codes<false>(t.avg_scale + block, lane, m));
-            store8_codes(static_cast<uint8_t*>(t.sq), i, t.n, whole, to_codes<true>(t.sq_scale + block, lane, v));
-        } else {
-            store8(static_cast<float*>(t.avg), i, t.n, whole, m);
-            store8(static_cast<float*>(t.sq), i, t.n, whole, v);
-        }
-    }
-    // the last block moves the groups on to their next step
+// The block that finishes a step last moves the groups on.
+__device__ __forceinline__ void finish_step(const StepArgs& a) {
     __shared__ unsigned int arrived;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -354,22 +297,305 @@ __global__ void __launch_bounds__(kThreads) step_kernel(StepArgs a) {
     if (threadIdx.x == 0) *a.ticket = 0;
 }
 
+template <bool kEight>
+struct RawState : Raw<float> {
+    __device__ __forceinline__ void load(const char* from, int block) { Raw<float>::load(from + (int64_t)block * (kBlock * 4)); }
+};
+template <>
+struct RawState<true> {
+    uint2 w;
+    __device__ __forceinline__ void load(const char* from, int block) { w = *reinterpret_cast<const uint2*>(from + (int64_t)block * kBlock); }
+};
+
+// Warp w of W takes units w, w + W, .. of all tensors' units in a row, so that the GPU's warps pass through a tensor side by side, and
+// what a tensor's blocks have in common is fetched again only when the tensor changes.  A lane's share of the next block, 48 to 128
+// bytes, is on its way in registers while a block is computed.
+//
+// DRAM decides.  In 32 bits a unit is a block: with runs of four or eight blocks for each warp the step took a sixth longer
+// (209 M bf16 weights with masters: 886 us; 1040).  The wait for the number of the tensor after next, once a unit, keeps the
+// warps in step; without it 990.  Four thread blocks of four warps an SM are as many as the registers allow; more warps,
+// with spills, were slower.
+template <class P, class G, bool kMaster, bool kEight>
+__global__ void __launch_bounds__(kThreads) step_kernel(StepArgs a) {
+    using W = std::conditional_t<kMaster, float, P>;      // what the step works on
+    constexpr int kState = kEight ? 1 : 4;
+    const int lane = threadIdx.x & 31, unit = kEight ? a.unit : 1;
+    const int warps = gridDim.x * (kThreads / 32);
+    int at = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    auto tensor_of = [&](int u) { return (unsigned)u < (unsigned)a.n_units ? a.tensor_of[u] : -1; };   // n_units + 2 warps < 2^31
+    int current = -1, tensor = tensor_of(at), next = tensor_of(at + warps);
+    // of the current tensor; the addresses are those of the lane's 8 elements of block 0
+    int first = 0, whole_blocks = 0, all_blocks = 0;
+    int64_t n = 0;
+    char *param = nullptr, *master = nullptr, *avg = nullptr, *sq = nullptr;
+    const char* grad = nullptr;
+    float *avg_scale = nullptr, *sq_scale = nullptr;
+    Numbers c = {};
+    bool on = false, fetched = false, have_scales = false;
+    float scale_m = 0.0f, scale_r = 0.0f;                 // lane j: of the unit's j-th block
+    Raw<G> rg;
+    Raw<W> rw;
+    RawState<kEight> ra, rs;
+    auto load = [&](int b) {
+        rg.load(grad + (int64_t)b * (kBlock * (int)sizeof(G)));
+        rw.load((kMaster ? master : param) + (int64_t)b * (kBlock * (int)sizeof(W)));
+        ra.load(avg, b);
+        rs.load(sq, b);
+    };
+    for (; tensor >= 0; at += warps) {
+        const int after = tensor_of(at + 2 * warps);
+        if (tensor != current) {
+            current = tensor;
+            const TensorRef t = a.tensors[tensor];
+            on = !a.active || a.active[t.group] > 0;
+            first = t.first;
+            n = t.n;
+            const char* const g = static_cast<const char*>(a.grads[tensor]);
+            uintptr_t low = (uintptr_t)t.param | (uintptr_t)g | (uintptr_t)t.master;
+            if (!kEight) low |= (uintptr_t)t.avg | (uintptr_t)t.sq;
+            const bool wide = (low & 15) == 0 && (!kEight || (((uintptr_t)t.avg | (uintptr_t)t.sq) & 7) == 0);
+            whole_blocks = wide ? (int)(n / kBlock) : 0;
+            all_blocks = (int)((n + kBlock - 1) / kBlock);
+            grad = g + lane * 8 * sizeof(G);
+            param = static_cast<char*>(t.param) + lane * 8 * sizeof(P);
+            master = reinterpret_cast<char*>(t.master) + lane * 8 * 4;
+            avg = static_cast<char*>(t.avg) + lane * 8 * kState;
+            sq = static_cast<char*>(t.sq) + lane * 8 * kState;
+            avg_scale = t.avg_scale + lane;
+            sq_scale = t.sq_scale + lane;
+            const Group& group = a.groups[t.group];
+            c = {group.b1, group.a1, group.b2, group.a2, group.correct, group.eps, group.keep, group.size, group.grad_scale};
+        }
+        const bool more = next == current;
+        tensor = next;
+        next = after;
+        if (!on) continue;
+        const int begin = (at - first) * unit, end = min(begin + unit, all_blocks), following = begin + warps * unit;
+        float old_m = scale_m, old_r = scale_r, new_m = 0.0f, new_r = 0.0f;
+        if constexpr (kEight) {
+            if (!have_scales && begin + lane < end) old_m = avg_scale[begin], old_r = sq_scale[begin];
+            have_scales = more;
+            if (more && lane < unit && following + lane < all_blocks) scale_m = avg_scale[following], scale_r = sq_scale[following];
+        }
+        for (int block = begin; block < end; ++block) {
+            P* const to = reinterpret_cast<P*>(param + (int64_t)block * (kBlock * (int)sizeof(P)));
+            float* const to_master = reinterpret_cast<float*>(master + (int64_t)block * (kBlock * 4));
+            char* const to_avg = avg + (int64_t)block * (kBlock * kState);
+            char* const to_sq = sq + (int64_t)block * (kBlock * kState);
+            Eight p, g, m, v;
+            float b1 = c.b1, b2 = c.b2;
+            if constexpr (kEight) {
+                const float by = __shfl_sync(~0u, old_r, block - begin);
+                b1 *= __shfl_sync(~0u, old_m, block - begin);
+                b2 *= by * by;
+            }
+            auto from_codes = [&](uint2 codes_m, uint2 codes_r) {
+                m = unpack_codes(codes_m);
+                v = unpack_codes(codes_r);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v.at[k] = v.at[k] * v.at[k];
+            };
+            Codes codes = {};
+            if (block < whole_blocks) {
+                if (!fetched) load(block);
+                g = rg.unpack();
+                p = rw.unpack();
+                if constexpr (kEight) {
+                    from_codes(ra.w, rs.w);
+                } else {
+                    m = ra.unpack();
+                    v = rs.unpack();
+                }
+                const int ahead = block + 1 < end ? block + 1 : more ? following : whole_blocks;
+                fetched = ahead < whole_blocks;
+                if (fetched) load(ahead);                 // on its way while this one is computed
+                step8<kEight>(c, b1, b2, p, g, m, v);
+                if (kMaster) store_whole8(to_master, p);
+                store_whole8(to, p);
+                if constexpr (kEight) {
+                    codes = encode(m, v, lane);
+                    *reinterpret_cast<uint2*>(to_avg) = codes.m;
+                    *reinterpret_cast<uint2*>(to_sq) = codes.r;
+                } else {
+                    store_whole8(reinterpret_cast<float*>(to_avg), m);
+                    store_whole8(reinterpret_cast<float*>(to_sq), v);
+                }
+            } else {                                      // a tensor's last block, or tensors that are not aligned
+                const int64_t left = n - ((int64_t)block * kBlock + lane * 8);
+                g = load_some(reinterpret_cast<const G*>(grad + (int64_t)block * (kBlock * (int)sizeof(G))), left);
+                p = kMaster ? load_some(to_master, left) : load_some(to, left);
+                if constexpr (kEight) {
+                    from_codes(load_some_codes(reinterpret_cast<const uint8_t*>(to_avg), left), load_some_codes(reinterpret_cast<const uint8_t*>(to_sq), left));
+                } else {
+                    m = load_some(reinterpret_cast<const float*>(to_avg), left);
+                    v = load_some(reinterpret_cast<const float*>(to_sq), left);
+                }
+                step8<kEight>(c, b1, b2, p, g, m, v);
+                if (kMaster) store_some(to_master, left, p);
+                store_some(to, left, p);
+                if constexpr (kEight) {
+                    codes = encode(m, v, lane);
+                    store_some_codes(reinterpret_cast<uint8_t*>(to_avg), left, codes.m);
+                    store_some_codes(reinterpret_cast<uint8_t*>(to_sq), left, codes.r);
+                } else {
+                    store_some(reinterpret_cast<float*>(to_avg), left, m);
+                    store_some(reinterpret_cast<float*>(to_sq), left, v);
+                }
+            }
+            if (kEight && lane == block - begin) new_m = codes.m_scale, new_r = codes.r_scale;
+        }
+        if (kEight && begin + lane < end) avg_scale[begin] = new_m, sq_scale[begin] = new_r;
+    }
+    finish_step(a);
+}
+
+template <int kBytes>
+__device__ __forceinline__ void copy(void* to, const char* from) {
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
+    if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(kBytes) : "memory");
+}
+// Blocks of a tensor on their way to a warp, each lane having its own 8 elements: the next three, in shared memory.  A lane waits
+// for its own copies only.
+template <class W, class G>
+struct Ahead {
+    static constexpr int kDepth = 3, kSlots = kDepth + 1;     // the slot of the block before is free: its values have been used
+    struct Slot {
+        uint4 g[sizeof(G) / 2][32], w[sizeof(W) / 2][32];
+        uint2 m[32], r[32];
+    };
+    struct Shared {
+        Slot slot[kSlots];
+    };
+    Shared* const shared;
+    const int lane;
+    __device__ __forceinline__ Ahead(Shared* s) : shared(s), lane(threadIdx.x & 31) {}
+    __device__ __forceinline__ void fetch(int n, bool there, const char* grad, const char* weights, const char* avg, const char* sq, int block) {
+        if (there) {
+            Slot& s = shared->slot[n % kSlots];
+#pragma unroll
+            for (int k = 0; k < (int)sizeof(G) / 2; ++k) copy<16>(&s.g[k][lane], grad + (int64_t)block * (kBlock * (int)sizeof(G)) + 16 * k);
+#pragma unroll
+            for (int k = 0; k < (int)sizeof(W) / 2; ++k) copy<16>(&s.w[k][lane], weights + (int64_t)block * (kBlock * (int)sizeof(W)) + 16 * k);
+            copy<8>(&s.m[lane], avg + (int64_t)block * kBlock);
+            copy<8>(&s.r[lane], sq + (int64_t)block * kBlock);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    // with the block's codes as they are: their scales are not in these numbers
+    __device__ __forceinline__ void take(int n, Eight& grad, Eight& weights, Eight& avg, Eight& root) const {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+        const Slot& s = shared->slot[n % kSlots];
+        Raw<G> rg;
+        Raw<W> rw;
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(G) / 2; ++k) rg.w[k] = s.g[k][lane];
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(W) / 2; ++k) rw.w[k] = s.w[k][lane];
+        grad = rg.unpack(), weights = rw.unpack(), avg = unpack_codes(s.m[lane]), root = unpack_codes(s.r[lane]);
+    }
+};
+
+// The same with 8-bit states where weights and gradients are of 16 bits and there is no master copy: a block is then 48 bytes a lane, and one ahead leaves 25 KB
+// on their way to an SM where 40 are wanted.  Three ahead, and 32 blocks in a row, whose scales fill a line of each state:
+// 519 us for 304 M elements, against 604 with one.  With more bytes a block it is the other way round (fp32: 1110 us against 790).
+template <class P>
+__global__ void __launch_bounds__(kThreads) deep_step_kernel(StepArgs a) {
+    using Blocks = Ahead<P, P>;
+    __shared__ typename Blocks::Shared shared[kThreads / 32];
+    const int lane = threadIdx.x & 31, unit = a.unit;
+    const int warps = gridDim.x * (kThreads / 32);
+    for (int at = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); at < a.n_units;) {   // n_units + warps < 2^31
+        const int tensor = a.tensor_of[at];
+        const TensorRef t = a.tensors[tensor];
+        const char* grad = static_cast<const char*>(a.grads[tensor]);
+        const int all = (int)((t.n + kBlock - 1) / kBlock), unit0 = at - t.first;
+        at += (((all + unit - 1) / unit - unit0 + warps - 1) / warps) * warps;            // behind all of the warp's units in this tensor
+        if (a.active && a.active[t.group] <= 0) continue;
+        const uintptr_t low = (uintptr_t)t.param | (uintptr_t)grad;
+        const bool wide = (low & 15) == 0 && (((uintptr_t)t.avg | (uintptr_t)t.sq) & 7) == 0;
+        const int whole = wide ? (int)(t.n / kBlock) : 0;
+        // the addresses of the lane's 8 elements of block 0
+        grad += lane * 8 * sizeof(P);
+        char* const param = static_cast<char*>(t.param) + lane * 8 * sizeof(P);
+        char* const avg = static_cast<char*>(t.avg) + lane * 8;
+        char* const sq = static_cast<char*>(t.sq) + lane * 8;
+        const Group& group = a.groups[t.group];
+        const Numbers c = {group.b1, group.a1, group.b2, group.a2, group.correct, group.eps, group.keep, group.size, group.grad_scale};
+        Blocks blocks(shared + (threadIdx.x >> 5));
+        auto after = [&](int b) { return ((b + 1) & (unit - 1)) && b + 1 < all ? b + 1 : (b & -unit) + warps * unit; };
+        int ahead = unit0 * unit;
+        for (int k = 0; k < Blocks::kDepth; ++k, ahead = after(ahead)) blocks.fetch(k, ahead < whole, grad, param, avg, sq, ahead);
+        float scale_m = 0.0f, scale_r = 0.0f, old_m = 0.0f, old_r = 0.0f, new_m = 0.0f, new_r = 0.0f;   // lane j: of the unit's j-th block
+        if (lane < unit && unit0 * unit + lane < all) scale_m = t.avg_scale[unit0 * unit + lane], scale_r = t.sq_scale[unit0 * unit + lane];
+        int n = 0;
+        for (int block = unit0 * unit; block < all; block = after(block), ++n) {
+            const int place = block & (unit - 1);
+            if (place == 0) {
+                old_m = scale_m, old_r = scale_r;
+                const int following = block + warps * unit + lane;
+                if (lane < unit && following < all) scale_m = t.avg_scale[following], scale_r = t.sq_scale[following];
+            }
+            P* const to = reinterpret_cast<P*>(param + (int64_t)block * (kBlock * (int)sizeof(P)));
+            char* const to_avg = avg + (int64_t)block * kBlock;
+            char* const to_sq = sq + (int64_t)block * kBlock;
+            const int64_t left = t.n - ((int64_t)block * kBlock + lane * 8);
+            const float by = __shfl_sync(~0u, old_r, place), b1 = c.b1 * __shfl_sync(~0u, old_m, place), b2 = c.b2 * (by * by);
+            Eight p, g, m, v;
+            Codes codes = {};
+            auto step = [&] {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v.at[k] = v.at[k] * v.at[k];
+                step8<true>(c, b1, b2, p, g, m, v);
+                codes = encode(m, v, lane);
+            };
+            if (block < whole) {
+                blocks.take(n, g, p, m, v);
+                blocks.fetch(n + Blocks::kDepth, ahead < whole, grad, param, avg, sq, ahead);
+                step();
+                store_whole8(to, p);
+                *reinterpret_cast<uint2*>(to_avg) = codes.m;
+                *reinterpret_cast<uint2*>(to_sq) = codes.r;
+            } else {                                      // a tensor's last block, or tensors that are not aligned: nothing is ahead
+                g = load_some(reinterpret_cast<const P*>(grad + (int64_t)block * (kBlock * (int)sizeof(P))), left);
+                p = load_some(to, left);
+                m = unpack_codes(load_some_codes(reinterpret_cast<const uint8_t*>(to_avg), left));
+                v = unpack_codes(load_some_codes(reinterpret_cast<const uint8_t*>(to_sq), left));
+                step();
+                store_some(to, left, p);
+                store_some_codes(reinterpret_cast<uint8_t*>(to_avg), left, codes.m);
+                store_some_codes(reinterpret_cast<uint8_t*>(to_sq), left, codes.r);
+            }
+            ahead = after(ahead);
+            if (lane == place) new_m = codes.m_scale, new_r = codes.r_scale;
+            if ((place == unit - 1 || block == all - 1) && lane <= place) t.avg_scale[block - place + lane] = new_m, t.sq_scale[block - place + lane] = new_r;
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");   // nothing of this tensor's is on its way to the slots any more
+    }
+    finish_step(a);
+}
+
 __global__ void set_group_kernel(Group* groups, int32_t k, Group g, bool keep_step) {
     if (keep_step) set_step(g, groups[k].step);
     groups[k] = g;
 }
 
-__global__ void fill_blocks_kernel(const TensorRef* tensors, int32_t* tensor_of) {
+__global__ void fill_units_kernel(const TensorRef* tensors, int unit, int32_t* tensor_of) {
     const TensorRef t = tensors[blockIdx.x];
-    const int n = (int)((t.n + kBlock - 1) / kBlock);
+    const int64_t blocks = (t.n + kBlock - 1) / kBlock;
+    const int n = (int)((blocks + unit - 1) / unit);
     for (int i = threadIdx.x; i < n; i += blockDim.x) tensor_of[t.first + i] = blockIdx.x;
 }
 
 using StepFn = void (*)(StepArgs);
 template <class P, class G>
+constexpr bool deep() { return sizeof(P) == 2 && sizeof(G) == 2; }
+template <class P, class G>
 StepFn pick(bool master, bool eight) {
     if (master) return eight ? step_kernel<P, G, true, true> : step_kernel<P, G, true, false>;
-    return eight ? step_kernel<P, G, false, true> : step_kernel<P, G, false, false>;
+    if (!eight) return step_kernel<P, G, false, false>;
+    if constexpr (deep<P, G>()) return deep_step_kernel<P>;
+    else return step_kernel<P, G, false, true>;
 }
 
 size_t up(size_t n) { return (n + 255) & ~size_t(255); }
@@ -380,7 +606,7 @@ size_t up(size_t n) { return (n + 255) & ~size_t(255); }
 struct slaq_adamw_handle {
     int device = 0;
     int32_t n_tensors = 0, n_groups = 0;
-    int32_t n_blocks = 0;
+    int32_t n_units = 0, unit = 1;
     bool owns_ws = false;
     void* ws = nullptr;
     slaq::TensorRef* tensors = nullptr;
@@ -423,7 +649,7 @@ Group device_group(const slaq_adamw_group& g) {
 size_t size_of(int type) { return type == SLAQ_F32 ? 4 : 2; }
 int64_t blocks_of(int64_t n) { return (n + kBlock - 1) / kBlock; }
 // bytes of the plan's device memory, and with `h` where its parts lie
-size_t layout(slaq_adamw_handle* h, char* base, int32_t n_tensors, int64_t n_blocks, int32_t n_groups) {
+size_t layout(slaq_adamw_handle* h, char* base, int32_t n_tensors, int64_t n_units, int32_t n_groups) {
     size_t at = 0;
     auto part = [&](auto*& p, size_t bytes) {
         if (h) p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(base + at);
@@ -433,7 +659,7 @@ size_t layout(slaq_adamw_handle* h, char* base, int32_t n_tensors, int64_t n_blo
     slaq_adamw_handle& o = h ? *h : none;
     part(o.tensors, sizeof(TensorRef) * (size_t)n_tensors);
     part(o.grads, sizeof(void*) * (size_t)n_tensors);
-    part(o.tensor_of, sizeof(int32_t) * (size_t)n_blocks);
+    part(o.tensor_of, sizeof(int32_t) * (size_t)n_units);
     part(o.groups, sizeof(Group) * (size_t)n_groups);
     part(o.ticket, sizeof(unsigned int));
     return at;
@@ -463,16 +689,25 @@ int create(slaq_adamw_handle* h, void* dev_ws, size_t bytes, int32_t n_tensors, 
     std::vector<TensorRef> refs((size_t)n_tensors);
     std::vector<const void*> grads((size_t)n_tensors);
     h->numel.resize((size_t)n_tensors);
-    int64_t blocks = 0;
+    int64_t blocks = 0, units = 0;
+    for (int32_t t = 0; t < n_tensors; ++t)
+        if (tensors[t].n > 0 && tensors[t].n <= kMostElements) blocks += blocks_of(tensors[t].n);
+    if (blocks > kMostElements / kBlock) return SLAQ_E_RANGE;
+    // With 8-bit states a warp works on 8 blocks in a row (32 in the deep kernel), so that it reads and writes their scales at
+    // once: where warps of several SMs wrote to one line of scales, these waited for one another (304 M elements in units of one
+    // block: 774 us).  As far as there is a unit for every warp.
+    bool any_master = false;
+    for (int32_t t = 0; t < n_tensors; ++t) any_master |= tensors[t].n > 0 && tensors[t].master;
+    int unit = !eight ? 1 : param_type != SLAQ_F32 && grad_type != SLAQ_F32 && !any_master ? 32 : 8;
+    while (unit > 1 && blocks < (int64_t)unit * 148 * 16) unit /= 2;
     for (int32_t t = 0; t < n_tensors; ++t) {
         const slaq_adamw_tensor& x = tensors[t];
         if (x.n < 0 || x.group < 0 || x.group >= n_groups) return SLAQ_E_ARG;
         if (x.n > kMostElements) return SLAQ_E_RANGE;
-        refs[t] = {x.param, x.master, x.exp_avg, x.exp_avg_sq, x.exp_avg_scale, x.exp_avg_sq_scale, x.n, x.group, (int32_t)blocks};
+        refs[t] = {x.param, x.master, x.exp_avg, x.exp_avg_sq, x.exp_avg_scale, x.exp_avg_sq_scale, x.n, x.group, (int32_t)units};
         grads[t] = x.grad;
         h->numel[t] = x.n;
-        blocks += blocks_of(x.n);
-        if (blocks > kMostElements / kBlock) return SLAQ_E_RANGE;
+        units += (blocks_of(x.n) + unit - 1) / unit;
         if (!x.n) continue;
         if (!x.param || !x.exp_avg || !x.exp_avg_sq || (eight && (!x.exp_avg_scale || !x.exp_avg_sq_scale))) return SLAQ_E_ARG;
         masters |= x.master != nullptr;
@@ -494,14 +729,15 @@ int create(slaq_adamw_handle* h, void* dev_ws, size_t bytes, int32_t n_tensors, 
         if (h->written[k].first < h->written[k - 1].second) return SLAQ_E_ARG;   // a tensor listed twice, or overlapping ones
     h->n_tensors = n_tensors;
     h->n_groups = n_groups;
-    h->n_blocks = (int32_t)blocks;
+    h->n_units = (int32_t)units;
+    h->unit = unit;
     h->grad_size = size_of(grad_type);
     if (const int rc = check_grads(h, grads.data())) return rc;
     if (param_type == SLAQ_F32) h->step = pick<float, float>(masters, eight);
     else if (param_type == SLAQ_BF16) h->step = grad_type == SLAQ_F32 ? pick<__nv_bfloat16, float>(masters, eight) : pick<__nv_bfloat16, __nv_bfloat16>(masters, eight);
     else h->step = grad_type == SLAQ_F32 ? pick<__half, float>(masters, eight) : pick<__half, __half>(masters, eight);
     if (cudaGetDevice(&h->device) != cudaSuccess) return SLAQ_E_CUDA;
-    const size_t need = layout(nullptr, nullptr, n_tensors, blocks, n_groups);
+    const size_t need = layout(nullptr, nullptr, n_tensors, blocks, n_groups);   // as many units as blocks: the size does not depend on the states
     if (dev_ws) {
         if (((uintptr_t)dev_ws & 255) || bytes < need) return SLAQ_E_NOMEM;
         h->ws = dev_ws;
@@ -523,9 +759,9 @@ int create(slaq_adamw_handle* h, void* dev_ws, size_t bytes, int32_t n_tensors, 
         cudaDeviceGetAttribute(&sm, cudaDevAttrMultiProcessorCount, h->device) != cudaSuccess ||
         cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, h->step, kThreads, 0) != cudaSuccess)
         return SLAQ_E_CUDA;
-    if (n_tensors) fill_blocks_kernel<<<n_tensors, 256, 0, st>>>(h->tensors, h->tensor_of);
+    if (n_tensors) fill_units_kernel<<<n_tensors, 256, 0, st>>>(h->tensors, h->unit, h->tensor_of);
     if (cudaGetLastError() != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return SLAQ_E_CUDA;   // the lists above end here
-    const int64_t wanted = (blocks + kThreads / 32 - 1) / (kThreads / 32);
+    const int64_t wanted = (units + kThreads / 32 - 1) / (kThreads / 32);
     h->grid = (int)std::max<int64_t>(1, std::min<int64_t>(wanted, (int64_t)sm * std::max(per_sm, 1)));
     return SLAQ_OK;
 }
@@ -583,7 +819,7 @@ const char* slaq_adamw_last_error(const slaq_adamw_t* h) { return h ? h->err : "
 int slaq_adamw_step(slaq_adamw_t* h, const int32_t* d_active, void* cuda_stream) {
     if (!h) return SLAQ_E_ARG;
     if (!slaq::on_device(h)) return slaq::fail(h, SLAQ_E_ARG, "the plan's device is not the current one");
-    slaq::StepArgs a = {h->tensors, h->grads, h->tensor_of, h->n_blocks, h->n_groups, h->groups, d_active, h->ticket};
+    slaq::StepArgs a = {h->tensors, h->grads, h->tensor_of, h->n_units, h->n_groups, h->unit, h->groups, d_active, h->ticket};
     h->step<<<h->grid, slaq::kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(a);
     return cudaGetLastError() == cudaSuccess ? SLAQ_OK : slaq::fail(h, SLAQ_E_CUDA, "the step could not be launched");
 }

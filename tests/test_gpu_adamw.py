@@ -220,6 +220,37 @@ def test_other_gradients_and_another_stream(slaq):
     assert all(torch.equal(x, y) for x, y in zip(p, q))
 
 
+@pytest.mark.parametrize("pt,shift", [(torch.bfloat16, 0), (torch.bfloat16, 3), (torch.float32, 0)])
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_large_plan_is_the_sum_of_small_ones(slaq, bits, pt, shift):
+    """Blocks do not know of one another: tensors cut at block boundaries into plans of their own give the same bits."""
+    gen = torch.Generator().manual_seed(13)
+    sizes = [5_000_003, 700, 256 * 32, 900_001, 1, 256 * 33 - 1]
+    p, g = _cut(sizes, pt, gen, 0.5, shift), _cut(sizes, pt, gen, 0.1, shift)
+    blocks = lambda n: -(-n // 256)   # noqa: E731
+    state = torch.float8_e4m3fn if bits == 8 else torch.float32
+    make = lambda xs: (dict(exp_avg=[torch.zeros(x.numel(), device="cuda").to(state) for x in xs], exp_avg_sq=[torch.zeros(x.numel(), device="cuda").to(state) for x in xs])   # noqa: E731
+                       | (dict(exp_avg_scale=[torch.zeros(blocks(x.numel()), device="cuda") for x in xs], exp_avg_sq_scale=[torch.zeros(blocks(x.numel()), device="cuda") for x in xs]) if bits == 8 else {}))
+    whole, q = make(p), [x.clone() for x in p]
+    plan = slaq.AdamW(p, g, state_bits=bits, **whole)
+    pieces = make(q)
+    plans = []
+    for k, n in enumerate(sizes):
+        for lo in range(0, n, 256 * 4000):
+            hi = min(n, lo + 256 * 4000)
+            part = {name: [v[k][lo // 256: blocks(hi)] if "scale" in name else v[k][lo:hi]] for name, v in pieces.items()}
+            plans.append(slaq.AdamW([q[k][lo:hi]], [g[k][lo:hi]], state_bits=bits, **part))
+    for _ in range(3):
+        plan.step()
+        for x in plans:
+            x.step()
+    for a, b in zip(p, q):
+        assert torch.equal(a, b)
+    for name in whole:
+        for a, b in zip(whole[name], pieces[name]):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), name
+
+
 def test_many_small_tensors(slaq):
     gen = torch.Generator().manual_seed(9)
     sizes = [1 + k % 40 for k in range(5000)]
