@@ -549,12 +549,13 @@ int slaq_token_loss(const void* d_logits, int type, int64_t rows, int32_t vocab,
  * a row counts with d_weights[r] (NULL: 1), and not at all if its target is negative (d_targets may be NULL) or its weight 0.
  * slaq_job_losses: d_out_losses[j] = -sum w logprob / sum w, in 64 bits, always summed in the same order.
  * slaq_job_row_grad: d_out_row_grad[r] = -w_r / sum w of the row's job: the loss's derivative by the row's log
- * probability.  Rows that belong to no job are left as they were.
+ * probability.  Rows before the first job and behind the last are left as they were, or set to 0 if zero_rest is not 0 (it
+ * takes a job then: SLAQ_E_ARG without).
  * A job without a row that counts has loss NaN, and so has one whose offsets leave 0 .. rows or fall (its rows are not
  * touched).  Errors: SLAQ_E_ARG, SLAQ_E_CUDA.
  */
 int slaq_job_row_grad(int32_t n_jobs, const int64_t* d_offsets, int64_t rows, const int64_t* d_targets, const float* d_weights,
-                      float* d_out_row_grad, void* cuda_stream);
+                      float* d_out_row_grad, int32_t zero_rest, void* cuda_stream);
 int slaq_job_losses(int32_t n_jobs, const int64_t* d_offsets, int64_t rows, const int64_t* d_targets, const float* d_logprob,
                     const float* d_weights, double* d_out_losses, void* cuda_stream);
 /*

@@ -3,89 +3,224 @@
 // Job j owns rows offsets[j] .. offsets[j+1).  A row counts with its weight (1 without weights), and not at all if its target is
 // negative or its weight 0:  loss_j = -sum w_r logprob_r / sum w_r, in 64 bits: the scheduler works on differences of losses
 // that a converged job reports at 1e-4 of their size and less.
+//
+// 12 to 20 bytes are read per row and little else happens, so what counts is that short jobs do not leave threads idle and
+// that a long one is not left to a single SM: a warp, a block or a cluster of eight blocks works on a job, by the mean number of
+// its rows, and every sum is taken in an order that the sizes alone decide.
+#include <cooperative_groups.h>
+
 #include "slaq_internal.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace slaq {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kCluster = 8;
 
-__device__ double block_sum(double v, double* shared) {
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
-    __syncthreads();
+struct JobArgs {
+    int32_t n_jobs;
+    const int64_t* offsets;
+    int64_t rows;
+    const int64_t* targets;
+    const float *logprob, *weights;
+    float* row_grad;
+    double* losses;
+    bool zero_rest;
+};
+
+struct Two {
+    double w, s;
+};
+
+// The sums of a job's T threads, or of its cluster's blocks of T threads, in each of them.
+template <int T, bool kClustered>
+__device__ Two team_sum(Two v, Two* shared, Two* from_blocks) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        v.w += __shfl_xor_sync(~0u, v.w, o);
+        v.s += __shfl_xor_sync(~0u, v.s, o);
+    }
+    if constexpr (T == 32) return v;
     if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = 0.0;
-    for (int w = 0; w < kThreads / 32; ++w) v += shared[w];
+    v = {0.0, 0.0};
+    for (int w = 0; w < T / 32; ++w) v.w += shared[w].w, v.s += shared[w].s;
+    if constexpr (kClustered) {
+        cg::cluster_group cluster = cg::this_cluster();
+        cluster.sync();                                     // every block has begun
+        if (threadIdx.x < kCluster) cluster.map_shared_rank(from_blocks, threadIdx.x)[cluster.block_rank()] = v;
+        cluster.sync();
+        v = {0.0, 0.0};
+        for (int b = 0; b < kCluster; ++b) v.w += from_blocks[b].w, v.s += from_blocks[b].s;
+    }
     return v;
 }
 
-__device__ __forceinline__ float weight_of(const int64_t* targets, const float* weights, int64_t r) {
-    return targets && targets[r] < 0 ? 0.0f : weights ? weights[r] : 1.0f;
+// Eight rows of a thread, kStep apart, all loaded before the first is used: each(r, w, lp) with their weights (0 behind the end)
+// and, if kLosses, their log probabilities.
+constexpr int kBatch = 8;
+template <bool kWhole, class T>
+__device__ __forceinline__ void load_batch(T (&x)[kBatch], const T* from, int64_t r, int64_t end, int step) {
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) x[k] = kWhole || r + k * step < end ? __ldg(from + r + k * step) : T(0);
+}
+template <bool kWhole, bool kLosses, int kStep, class Each>
+__device__ __forceinline__ void batch(const JobArgs& a, int64_t r, int64_t end, Each&& each) {
+    long long t[kBatch] = {};
+    float w[kBatch], lp[kBatch];
+    if (a.targets) load_batch<kWhole>(t, reinterpret_cast<const long long*>(a.targets), r, end, kStep);
+    if (kLosses) load_batch<kWhole>(lp, a.logprob, r, end, kStep);
+    if (a.weights) {
+        load_batch<kWhole>(w, a.weights, r, end, kStep);
+    } else {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) w[k] = kWhole || r + k * kStep < end ? 1.0f : 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k)
+        if (t[k] < 0) w[k] = 0.0f;
+    each(r, w, lp);
+}
+template <bool kLosses, int kStep, class Each>
+__device__ __forceinline__ void for_rows(const JobArgs& a, int64_t first, int64_t end, Each&& each) {
+    int64_t r = first;
+    for (; r + (kBatch - 1) * kStep < end; r += kStep * kBatch) batch<true, kLosses, kStep>(a, r, end, each);
+    if (r + kStep < end) {
+        batch<false, kLosses, kStep>(a, r, end, each);
+    } else if (r < end) {   // one row: most of what the threads of a short job have
+        float w[kBatch] = {a.weights ? __ldg(a.weights + r) : 1.0f}, lp[kBatch] = {kLosses ? __ldg(a.logprob + r) : 0.0f};
+        if (a.targets && __ldg(a.targets + r) < 0) w[0] = 0.0f;
+        each(r, w, lp);
+    }
 }
 
-// The rows of job j; offsets that leave the array or run backwards give `bad`, and no row.
+// The rows of job j; offsets that leave the array or run backwards give none: the job's loss is then NaN, and its rows are not touched.
 struct Rows {
     int64_t lo, hi;
-    bool bad;
 };
-__device__ Rows rows_of(const int64_t* offsets, int64_t rows, int j) {
-    const int64_t lo = offsets[j], hi = offsets[j + 1];
-    if (lo < 0 || hi < lo || hi > rows) return {0, 0, true};
-    return {lo, hi, false};
+__device__ __forceinline__ Rows rows_of(const JobArgs& a, int64_t j) {
+    const int64_t lo = a.offsets[j], hi = a.offsets[j + 1];
+    return lo < 0 || hi < lo || hi > a.rows ? Rows{0, 0} : Rows{lo, hi};
 }
 
-__global__ void __launch_bounds__(kThreads)
-    row_grad_kernel(const int64_t* offsets, int64_t rows, const int64_t* targets, const float* weights, float* out) {
-    __shared__ double shared[kThreads / 32];
-    const auto [lo, hi, bad] = rows_of(offsets, rows, blockIdx.x);
-    double w = 0.0;
-    for (int64_t r = lo + threadIdx.x; r < hi; r += kThreads) w += weight_of(targets, weights, r);
-    w = block_sum(w, shared);
-    for (int64_t r = lo + threadIdx.x; r < hi; r += kThreads) {
-        const float mine = weight_of(targets, weights, r);
-        out[r] = mine == 0.0f ? 0.0f : (float)(-mine / w);
-    }
-}
-
-__global__ void __launch_bounds__(kThreads)
-    job_losses_kernel(const int64_t* offsets, int64_t rows, const int64_t* targets, const float* logprob, const float* weights, double* out) {
-    __shared__ double shared[kThreads / 32];
-    const auto [lo, hi, bad] = rows_of(offsets, rows, blockIdx.x);
-    double w = 0.0, s = 0.0;
-    for (int64_t r = lo + threadIdx.x; r < hi; r += kThreads) {
-        const float mine = weight_of(targets, weights, r);
-        if (mine != 0.0f) {
-            w += mine;
-            s += (double)mine * logprob[r];
+// Job j by T threads (numbered `tid`), or by the blocks of a cluster.
+template <int T, bool kClustered, bool kLosses>
+__device__ __forceinline__ void work_on(const JobArgs& a, int64_t j, Rows rows, int tid, int rank, Two* shared, Two* from_blocks) {
+    constexpr int kStep = T * (kClustered ? kCluster : 1);
+    const int64_t first = rows.lo + (int64_t)rank * T + tid;
+    Two sum = {0.0, 0.0};
+    for_rows<kLosses, kStep>(a, first, rows.hi, [&](int64_t, const float (&w)[kBatch], const float (&lp)[kBatch]) {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            sum.w += w[k];
+            if (kLosses) sum.s += w[k] != 0.0f ? (double)w[k] * lp[k] : 0.0;      // what does not count may be infinite or NaN
         }
+    });
+    sum = team_sum<T, kClustered>(sum, shared, from_blocks);
+    if (kLosses) {
+        if (tid == 0 && rank == 0) a.losses[j] = -sum.s / sum.w;   // NaN for a job without a row that counts
+        return;
     }
-    w = block_sum(w, shared);
-    s = block_sum(s, shared);
-    if (threadIdx.x == 0) out[blockIdx.x] = -s / w;   // NaN for a job without a row that counts
+    const double by = -1.0 / sum.w;
+    for_rows<false, kStep>(a, first, rows.hi, [&](int64_t r, const float (&w)[kBatch], const float (&)[kBatch]) {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+            if (r + k * kStep < rows.hi) a.row_grad[r + k * kStep] = w[k] != 0.0f ? (float)(w[k] * by) : 0.0f;
+    });
 }
 
-int done() { return cudaGetLastError() == cudaSuccess ? SLAQ_OK : SLAQ_E_CUDA; }
+// Rows before the first job and behind the last.
+__device__ void zero_rest(const JobArgs& a) {
+    const int64_t n = (int64_t)gridDim.x * blockDim.x, at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    const int64_t lo = min(a.offsets[0], a.rows), hi = max(a.offsets[a.n_jobs], (int64_t)0);
+    for (int64_t r = at; r < lo; r += n) a.row_grad[r] = 0.0f;
+    for (int64_t r = hi + at; r < a.rows; r += n) a.row_grad[r] = 0.0f;
+}
+
+// A block, or a cluster of blocks, for each job.
+template <int T, bool kClustered, bool kLosses>
+__global__ void __launch_bounds__(T) jobs_kernel(JobArgs a) {
+    __shared__ Two shared[T / 32], from_blocks[kCluster];
+    if (!kLosses && a.zero_rest) zero_rest(a);
+    const int64_t j = kClustered ? blockIdx.x / kCluster : blockIdx.x;
+    work_on<T, kClustered, kLosses>(a, j, rows_of(a, j), threadIdx.x, kClustered ? (int)cg::this_cluster().block_rank() : 0, shared, from_blocks);
+}
+
+// Short jobs: a warp for each; what is long among them is then done by all warps of its block.
+constexpr int kShort = 2048, kBlockJobs = 16;
+template <bool kLosses>
+__global__ void __launch_bounds__(32 * kBlockJobs) short_jobs_kernel(JobArgs a) {
+    __shared__ Two shared[kBlockJobs];
+    if (!kLosses && a.zero_rest) zero_rest(a);
+    const int64_t first = (int64_t)blockIdx.x * kBlockJobs, mine = first + (threadIdx.x >> 5);
+    bool is_long = false;
+    if (mine < a.n_jobs) {
+        const Rows rows = rows_of(a, mine);
+        is_long = rows.hi - rows.lo > kShort;
+        if (!is_long) work_on<32, false, kLosses>(a, mine, rows, threadIdx.x & 31, 0, nullptr, nullptr);
+    }
+    if (!__syncthreads_or(is_long)) return;
+    for (int64_t j = first; j < min(first + kBlockJobs, (int64_t)a.n_jobs); ++j) {
+        const Rows rows = rows_of(a, j);
+        if (rows.hi - rows.lo <= kShort) continue;
+        work_on<32 * kBlockJobs, false, kLosses>(a, j, rows, threadIdx.x, 0, shared, nullptr);
+        __syncthreads();
+    }
+}
+
+template <bool kLosses>
+int launch_jobs(const JobArgs& a, cudaStream_t st) {
+    const int64_t mean = a.rows / a.n_jobs;
+    cudaLaunchConfig_t cfg = {};
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1] = {};
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kCluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cudaError_t e;
+    if (mean <= 256) {
+        cfg.gridDim = dim3((unsigned)((a.n_jobs + kBlockJobs - 1) / kBlockJobs));
+        cfg.blockDim = dim3(32 * kBlockJobs);
+        e = cudaLaunchKernelEx(&cfg, short_jobs_kernel<kLosses>, a);
+    } else if (mean <= 2048) {
+        cfg.gridDim = dim3((unsigned)a.n_jobs);
+        cfg.blockDim = dim3(128);
+        e = cudaLaunchKernelEx(&cfg, jobs_kernel<128, false, kLosses>, a);
+    } else if (mean < 16384 || a.n_jobs > 296) {
+        cfg.gridDim = dim3((unsigned)a.n_jobs);
+        cfg.blockDim = dim3(512);
+        e = cudaLaunchKernelEx(&cfg, jobs_kernel<512, false, kLosses>, a);
+    } else {
+        cfg.gridDim = dim3((unsigned)a.n_jobs * kCluster);
+        cfg.blockDim = dim3(1024);
+        cfg.numAttrs = 1;
+        e = cudaLaunchKernelEx(&cfg, jobs_kernel<1024, true, kLosses>, a);
+    }
+    if (e != cudaSuccess) (void)cudaGetLastError();
+    return e == cudaSuccess ? SLAQ_OK : SLAQ_E_CUDA;
+}
 
 }  // namespace
 }  // namespace slaq
 
 extern "C" int slaq_job_row_grad(int32_t n_jobs, const int64_t* d_offsets, int64_t rows, const int64_t* d_targets, const float* d_weights,
-                                 float* d_out_row_grad, void* cuda_stream) {
+                                 float* d_out_row_grad, int32_t zero_rest, void* cuda_stream) {
     using namespace slaq;
-    if (n_jobs < 0 || rows < 0 || (n_jobs && (!d_offsets || !d_out_row_grad))) return SLAQ_E_ARG;
-    if (n_jobs == 0) return SLAQ_OK;
-    row_grad_kernel<<<n_jobs, kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(d_offsets, rows, d_targets, d_weights, d_out_row_grad);
-    return done();
+    if (n_jobs < 0 || rows < 0 || (n_jobs && (!d_offsets || (rows && !d_out_row_grad)))) return SLAQ_E_ARG;
+    if (n_jobs == 0 || rows == 0) return n_jobs == 0 && rows && zero_rest ? SLAQ_E_ARG : SLAQ_OK;
+    JobArgs a = {n_jobs, d_offsets, rows, d_targets, nullptr, d_weights, d_out_row_grad, nullptr, zero_rest != 0};
+    return launch_jobs<false>(a, static_cast<cudaStream_t>(cuda_stream));
 }
 
 extern "C" int slaq_job_losses(int32_t n_jobs, const int64_t* d_offsets, int64_t rows, const int64_t* d_targets, const float* d_logprob,
                                const float* d_weights, double* d_out_losses, void* cuda_stream) {
     using namespace slaq;
-    if (n_jobs < 0 || rows < 0 || (n_jobs && (!d_offsets || !d_logprob || !d_out_losses))) return SLAQ_E_ARG;
+    if (n_jobs < 0 || rows < 0 || (n_jobs && (!d_offsets || (rows && !d_logprob) || !d_out_losses))) return SLAQ_E_ARG;
     if (n_jobs == 0) return SLAQ_OK;
-    job_losses_kernel<<<n_jobs, kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(d_offsets, rows, d_targets, d_logprob, d_weights, d_out_losses);
-    return done();
+    JobArgs a = {n_jobs, d_offsets, rows, d_targets, d_logprob, d_weights, nullptr, d_out_losses, false};
+    return launch_jobs<true>(a, static_cast<cudaStream_t>(cuda_stream));
 }
 
 extern "C" int slaq_append_token_losses(slaq_t* h, int32_t n, const int32_t* d_job_ids, const int64_t* d_offsets, int64_t rows,

@@ -186,7 +186,7 @@ def token_loss(logits, targets, row_grad, scale: float = 1.0, out=None, stream=N
 
 def job_row_grad(offsets, targets=None, weights=None, out=None, stream=None):
     """slaq_job_row_grad: the derivative of each job's mean loss by the log probability of each of its rows (float32 [rows]).
-    ``offsets`` int64 [jobs + 1]; rows of no job keep what ``out`` holds (zeros without ``out``)."""
+    ``offsets`` int64 [jobs + 1]; rows before the first job and behind the last keep what ``out`` holds (without ``out``: 0)."""
     torch = _load()
     known = next((t for t in (targets, weights, out) if t is not None), None)
     if known is None:
@@ -198,9 +198,10 @@ def job_row_grad(offsets, targets=None, weights=None, out=None, stream=None):
     n = offsets.numel() - 1
     off = _vector(offsets, "offsets", torch.int64, max(n, 0) + 1, gpu)
     with _on(stream, gpu) as raw:
-        if out is None:
-            out = torch.zeros(rows, dtype=torch.float32, device=offsets.device)
-        _check(_lib().slaq_job_row_grad(n, off, rows, t, w, _vector(out, "out", torch.float32, rows, gpu), raw))
+        fresh = out is None
+        if fresh:
+            out = torch.empty(rows, dtype=torch.float32, device=offsets.device)
+        _check(_lib().slaq_job_row_grad(n, off, rows, t, w, _vector(out, "out", torch.float32, rows, gpu), fresh, raw))
     return out
 
 

@@ -31,7 +31,7 @@ def _inputs(lengths, seed, weighted, missing, behind=3):
     return off, t, lp, w
 
 
-CASES = [[1], [0], [3, 0, 0, 5], [1] * 700, [31, 32, 33, 255, 256, 257, 0, 1023, 1025], [70001], [5, 200003, 0, 1, 4096], [9] * 3000, [120] * 148]
+CASES = [[1], [0], [300_001], [140_000, 3, 130_000], [4] * 200 + [2049, 0, 30_000, 2048] + [3] * 300, [3, 0, 0, 5], [1] * 700, [31, 32, 33, 255, 256, 257, 0, 1023, 1025], [70001], [5, 200003, 0, 1, 4096], [9] * 3000, [120] * 148]
 
 
 @pytest.mark.parametrize("weighted", [False, True])
@@ -51,6 +51,10 @@ def test_losses_and_factors(slaq, lengths, weighted):
     end = int(off[-1])
     assert bool((got[end:] == 9.0).all())                                  # rows behind the last job stay as they were
     assert bool(((got[:end] - factors[:end]).abs() <= (2.0 ** -24 + 1e-12) * factors[:end].abs()).all())
+    off2 = off + 3                                                          # rows in front as well: zeros in a result of its own
+    pad = lambda v, x: None if v is None else torch.cat([torch.full((3,), x, dtype=v.dtype), v]).cuda()   # noqa: E731
+    fresh = slaq.job_row_grad(off2.cuda(), pad(t, 5), pad(w, 1.0)).cpu().double()
+    assert not fresh[:3].any() and not fresh[3 + end:].any() and torch.equal(fresh[3:3 + end], got[:end])
     again = slaq.job_losses(cuda(off), cuda(t), cuda(lp), cuda(w)).cpu()
     assert torch.equal(torch.nan_to_num(again), torch.nan_to_num(slaq.job_losses(cuda(off), cuda(t), cuda(lp), cuda(w)).cpu()))
 

@@ -46,8 +46,9 @@ def test_job_losses(lib):
     assert lib.slaq_job_losses(2, None, 5, None, P, None, P, None) == -1
     assert lib.slaq_job_losses(2, P, 5, None, None, None, P, None) == -1
     assert lib.slaq_job_losses(0, None, 0, None, None, None, None, None) == 0
-    assert lib.slaq_job_row_grad(2, P, 5, None, None, None, None) == -1
-    assert lib.slaq_job_row_grad(0, None, 0, None, None, None, None) == 0
+    assert lib.slaq_job_row_grad(2, P, 5, None, None, None, 0, None) == -1
+    assert lib.slaq_job_row_grad(0, None, 0, None, None, None, 0, None) == 0
+    assert lib.slaq_job_row_grad(0, P, 5, None, None, P, 1, None) == -1
     assert lib.slaq_append_token_losses(None, 1, P, P, 5, None, P, None, None, None, P) == -1
 
 
