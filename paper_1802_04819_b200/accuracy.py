@@ -7,6 +7,9 @@ families (parameter ranges of the benchmark workloads, multiplicative lognormal 
 history is cut `ahead` iterations short, fitted by the library on the GPU, and the fitted curve is evaluated
 `ahead` iterations past the cut against the noise-free generating curve.
 
+The last row is measured on jobs that really train (``trainers.SoftmaxJobs``, one of the paper's algorithms on drawn
+data), against the loss that they report ten iterations later.
+
     python -m paper_1802_04819_b200.accuracy            # needs a GPU; prints a table
 """
 
@@ -77,8 +80,34 @@ def measure(n_jobs=2000, ahead=10, sigmas=SIGMAS, seed=0):
     return rows
 
 
+def measure_trained(n_jobs=500, ahead=10, hmin=30, hmax=200, seed=0):
+    """The same on training jobs, each cut at an iteration drawn from [hmin, hmax] less `ahead`: (jobs fitted, median relative error,
+    share of jobs under 5 %, share won by the sublinear family)."""
+    import paper_1802_04819_b200 as slaq
+    from .trainers import SoftmaxJobs
+    losses = SoftmaxJobs(n_jobs, seed=seed).histories(hmax)
+    cut = np.random.default_rng(seed).integers(hmin, hmax + 1, n_jobs).astype(np.int64) - ahead
+    off = np.zeros(n_jobs + 1, np.int64)
+    np.cumsum(cut, out=off[1:])
+    ids = np.arange(n_jobs, dtype=np.int32)
+    with slaq.Scheduler(n_jobs, int(cut.max()), 4) as sched:
+        sched.load_histories(ids, off, np.concatenate([losses[j, :cut[j]] for j in range(n_jobs)]), cut - 1)
+        sched.set_time_model(ids, np.full(n_jobs, 0.1), np.full(n_jobs, 10.0))
+        sched.schedule(1.0, n_jobs)
+        pred = sched.get_predictions(want_gain=False)
+    ok, q, x = pred["status"] == slaq.JOB_FITTED, pred["params"], ahead / (cut - 1.0)
+    with np.errstate(all="ignore"):
+        f = np.where(pred["family"] == 0, 1.0 / (q[:, 0] * x * x + q[:, 1] * x + q[:, 2]) + q[:, 3], np.exp(q[:, 0] - q[:, 1] * x) + q[:, 2]) * pred["M"]
+    truth = losses[ids, cut - 1 + ahead]
+    err = (np.abs(f - truth) / truth)[ok]
+    return dict(fitted=int(ok.sum()), median_error=float(np.median(err)), under_5_percent=float(np.mean(err < 0.05)),
+                sublinear_wins=float(np.mean(pred["family"][ok] == 0)))
+
+
 if __name__ == "__main__":
     print(f"{'family':12s} {'sigma':>6s} {'fitted':>7s} {'median error':>13s} {'under 5 %':>10s} {'own family wins':>16s}")
     for r in measure():
         print(f"{r['family']:12s} {r['sigma']:6.2f} {r['fitted']:7d} {r['median_error']:13.4f} {r['under_5_percent']:10.3f} "
               f"{r['generating_family_wins']:16.3f}")
+    r = measure_trained()
+    print(f"{'trained':12s} {'':6s} {r['fitted']:7d} {r['median_error']:13.4f} {r['under_5_percent']:10.3f}   (sublinear wins {r['sublinear_wins']:.3f})")

@@ -573,7 +573,8 @@ __device__ __forceinline__ Gradient gradient_from_norm(const RowArgs& a, int64_t
     return gradient_of(a, a.targets[row], n.x, n.y, a.g_entropy ? logf(n.y) : 0.0f, a.g_entropy ? a.in_entropy[row] : 0.0f, a.g_logprob[row], h);
 }
 
-// L lanes take L kUnroll vectors of a row.
+// L lanes take L kUnroll vectors of a row.  Nothing is shared and nothing waited for, so this runs at the copy's rate: 4,096 x
+// 128,000 bf16 326 us (98 %), 2,048 x 50,001 with rows at every alignment 72 us (87 %).
 template <class E, bool kEntropy, int L>
 __global__ void __launch_bounds__(256) grad_kernel(RowArgs a, int segments) {
     const int sub = threadIdx.x % L;
@@ -684,7 +685,7 @@ cudaError_t launch(void (*kernel)(Params...), int64_t blocks, int threads, size_
 }
 
 constexpr int kSms = 148;
-constexpr size_t kSliceBytes = 64 * 1024, kMostSlice = 200 * 1024;   // per block of the loss: three blocks on an SM, or one
+constexpr size_t kSliceBytes = 72 * 1024, kMostSlice = 200 * 1024;   // per block of the loss: three blocks on an SM, or one
 
 // Vectors a row may touch, whatever its alignment.
 template <class E>
@@ -710,6 +711,11 @@ cudaError_t launch_stream(RowArgs a, int cluster, cudaStream_t st) {
     return launch(a.top ? stream_kernel<E, T, true> : stream_kernel<E, T, false>, blocks, T < 128 ? 128 : T, 0, cluster, st, a);
 }
 
+// A warp to a row while there are rows for all warps and a row is not too long for one (2,400 x 5,000 with 5 alternatives: 14.3 us, a
+// block of 128 threads 18.5; 30,000 x 3,000: 39 and 68; but 2,000 x 16,000: 20.5 and 17.3).  With few rows a cluster shares one, as many
+// blocks as make two on every SM (64 x 130,001 fp32: 11.0 us; four on every SM 12.1).  More threads where a block has the SM for
+// itself (there 512 threads 12.0 us, 128 threads 17); with many rows several small blocks hide one another's ends better than one
+// large one (8,192 x 65,536 bf16: 128 threads 166 us, 512 threads 242).
 template <class E>
 cudaError_t launch_logprobs(const RowArgs& a, cudaStream_t st) {
     if (a.vocab <= kNarrow) return launch_narrow<E, false>(a, st);
@@ -718,11 +724,17 @@ cudaError_t launch_logprobs(const RowArgs& a, cudaStream_t st) {
     int cluster = 1;
     while (cluster < kMaxCluster && a.rows * cluster * 2 <= 2 * kSms && vectors / (2 * cluster) >= 256) cluster *= 2;
     const int each = vectors / cluster;
-    if (each <= 1024) return launch_stream<E, 128>(a, cluster, st);
-    if (each <= 4096 || a.rows * cluster > 2 * kSms) return launch_stream<E, 256>(a, cluster, st);
+    const bool many = a.rows * cluster > 2 * kSms;
+    if (each <= (many ? 8192 : 1024)) return launch_stream<E, 128>(a, cluster, st);
+    if (each <= 4096 || many) return launch_stream<E, 256>(a, cluster, st);
     return launch_stream<E, 512>(a, cluster, st);
 }
 
+// A block's part of a row stays in shared memory; three blocks of 72 KB on an SM work in turn on loading, summing up and storing.
+// 4,096 x 128,000 bf16 in clusters of four: 403 us, 79 % of the copy bandwidth (a step read twice from memory: 495 us; parts of 32 KB in
+// clusters of eight 445; blocks of 512 threads 507).  What bounds it is the special function unit, two exponentials an element keep
+// it busy 63 % of the time, and the turns: a block waits for its cluster once a row.  Exponentials by a polynomial in a quarter
+// or half of the places gained nothing: 393 and 408 us.
 template <class E>
 cudaError_t launch_loss(RowArgs a, cudaStream_t st) {
     if (a.vocab <= kNarrow) return launch_narrow<E, true>(a, st);
@@ -734,6 +746,8 @@ cudaError_t launch_loss(RowArgs a, cudaStream_t st) {
     a.slice = slice_of(vectors, cluster);
     const size_t bytes = (size_t)a.slice * 16;
     if (bytes > kMostSlice) return launch(loss_kernel<E, 512, false>, a.rows * cluster, 512, 0, cluster, st, a);
+    if (a.slice <= 1536)   // 20,000 x 5,000 bf16: 88 us, with 256 threads 125; 8,000 x 16,000: 91 and 92
+        return launch(loss_kernel<E, 128, true>, a.rows * cluster, 128, bytes, cluster, st, a);
     return launch(loss_kernel<E, 256, true>, a.rows * cluster, 256, bytes, cluster, st, a);
 }
 
