@@ -59,10 +59,11 @@ class SoftmaxJobs:
         return out.t().contiguous().cpu().numpy()
 
 
-def run(policy="slaq", n_jobs=64, epochs=60, cores_per_job=2, max_cores_per_job=16, epoch_seconds=3.0, max_hist=64, seed=0):
-    """A cluster of such jobs for some epochs: in each, a job on n cores finishes the iterations that its law t(n) = s + w/n allows
-    (drawn laws; the jobs themselves run on this GPU).  Returns the mean over epochs and jobs of the loss, normalised by the first
-    and the lowest loss that the job reaches when it is trained to the end."""
+def run(policy="slaq", n_jobs=64, epochs=80, total_cores=64, max_cores_per_job=16, epoch_seconds=3.0, max_hist=64, seed=0):
+    """A cluster of such jobs, which arrive one after the other over three quarters of the epochs.  In an epoch a job on n cores finishes
+    the iterations that its law t(n) = s + w/n allows (drawn laws; the jobs themselves run on this GPU).  "fair": the cores in
+    equal parts.  Returns the loss averaged over the running jobs and the epochs, each job's normalised by its first loss and the
+    lowest that it reaches when it is trained to the end, and the jobs."""
     import torch
 
     import paper_1802_04819_b200 as slaq
@@ -70,33 +71,34 @@ def run(policy="slaq", n_jobs=64, epochs=60, cores_per_job=2, max_cores_per_job=
     s, w = rng.uniform(0.05, 0.5, n_jobs), rng.uniform(1.0, 20.0, n_jobs)
     last = SoftmaxJobs(n_jobs, seed=seed).histories(400).min(axis=1)
     jobs = SoftmaxJobs(n_jobs, seed=seed)
-    ids, total = np.arange(n_jobs, dtype=np.int32), cores_per_job * n_jobs
-    everyone = torch.arange(n_jobs, dtype=torch.int32, device="cuda")
-    now = jobs.step(active=torch.zeros_like(everyone)).cpu().numpy()
-    first, credit, mean = now.copy(), np.zeros(n_jobs), []
+    nobody = torch.zeros(n_jobs, dtype=torch.int32, device="cuda")
+    first = jobs.step(active=nobody).cpu().numpy()
+    arrives = np.arange(n_jobs) * (0.75 * epochs) / n_jobs
+    credit, mean = np.zeros(n_jobs), []
     with slaq.Scheduler(n_jobs, max_hist, max_cores_per_job) as sched:
-        sched.append_losses(ids, now)
-        sched.set_time_model(ids, s, w)
-        for _ in range(epochs):
+        for epoch in range(epochs):
+            new = np.nonzero(np.ceil(arrives) == epoch)[0]
+            if new.size:
+                sched.append_losses(new, first[new])
+                sched.set_time_model(new, s[new], w[new])
+            running = arrives <= epoch
             if policy == "slaq":
-                alloc, _ = sched.schedule(epoch_seconds, total)
+                alloc, _ = sched.schedule(epoch_seconds, total_cores)
             else:
-                alloc = np.full(n_jobs, cores_per_job, np.int32)
+                alloc = np.where(running, min(max_cores_per_job, total_cores // int(running.sum())), 0)
+                alloc[np.nonzero(running)[0][: max(0, total_cores - int(alloc.sum()))]] += int(alloc.max()) < max_cores_per_job
             progress = np.where(alloc > 0, epoch_seconds / (s + w / np.maximum(alloc, 1)), 0.0) + credit
             todo = np.floor(progress).astype(np.int32)
             credit = progress - todo
             left = torch.from_numpy(todo).cuda()
-            for k in range(int(todo.max())):
-                losses = jobs.step(active=left)       # the losses before this iteration: the last iteration's result ..
-                if k:                                 # .. of the jobs that had one
-                    ran = torch.nonzero(left >= 0).flatten().to(torch.int32)
-                    sched.append_losses_device(ran, losses[ran.long()])
+            for k in range(1, int(todo.max()) + 1):
+                jobs.step(active=left)
                 left -= 1
-            losses = jobs.step(active=torch.zeros_like(left))
-            ran = torch.nonzero(left == 0).flatten().to(torch.int32) if todo.max() else everyone[:0]
-            if ran.numel():
+                losses = jobs.step(active=nobody)
+                ran = torch.nonzero((left >= 0) & (torch.from_numpy(todo).cuda() > 0)).flatten().to(torch.int32)
                 sched.append_losses_device(ran, losses[ran.long()])
-            mean.append(float(np.mean((losses.cpu().numpy() - last) / (first - last))))
+            now = jobs.step(active=nobody).cpu().numpy()
+            mean.append(float(np.mean(((now - last) / (first - last))[running])))
     return float(np.mean(mean)), jobs
 
 
