@@ -516,7 +516,8 @@ enum {
  * A logit of -inf is a masked token (probability 0).  A row of nothing else has log probability -inf, entropy 0 and norm
  * (-inf, 0).  A target of vocab or more gives the log probability NaN; a row with a NaN or +inf gives NaN throughout, its
  * top_ids excepted.
- * Errors: SLAQ_E_ARG (null, negative counts, vocab < 1, scale not positive and finite, unknown type, unaligned element),
+ * Errors: SLAQ_E_ARG (null, negative counts, vocab < 1, scale not in (0, 1e30], unknown type, an address that its
+ * elements' size, or 8 bytes for a norm, does not divide),
  * SLAQ_E_RANGE (vocab > 2^22, top > 32, 2^31 rows or more), SLAQ_E_CUDA.
  */
 int slaq_token_logprobs(const void* d_logits, int type, int64_t rows, int32_t vocab, int64_t row_stride, const int64_t* d_targets,

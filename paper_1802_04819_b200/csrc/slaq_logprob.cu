@@ -16,6 +16,7 @@ namespace {
 
 constexpr int kMaxVocab = 1 << 22;
 constexpr int kMaxTop = 32;
+constexpr float kMostScale = 1e30f;   // beyond, a scale times log2 e would not be finite
 constexpr int kMaxCluster = 8;
 constexpr int kUnroll = 4;         // vectors that a thread has in flight
 
@@ -642,7 +643,7 @@ bool overlap(const RowArgs& a, int64_t es) {
 }
 
 int check_rows(const RowArgs& a, int type) {
-    if (!type_ok(type) || a.rows < 0 || a.vocab < 1 || !(a.scale > 0.0f) || a.scale > 3.0e38f) return SLAQ_E_ARG;
+    if (!type_ok(type) || a.rows < 0 || a.vocab < 1 || !(a.scale > 0.0f) || a.scale > kMostScale) return SLAQ_E_ARG;
     if (a.vocab > kMaxVocab || a.rows > 0x7FFFFFFF) return SLAQ_E_RANGE;
     if (a.rows && (!a.logits || (a.rows > 1 && a.stride < 0))) return SLAQ_E_ARG;
     if (reinterpret_cast<uintptr_t>(a.logits) % size_of(type)) return SLAQ_E_ARG;

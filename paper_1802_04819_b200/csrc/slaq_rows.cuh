@@ -40,9 +40,10 @@ __device__ __forceinline__ float warp_max_nan(float x) {
     return y;
 }
 
-// Unsigned integers in the order of the values, -0 equal to +0, NaN above everything.  No value maps to 0.
+// Unsigned integers in the order of the values, -0 equal to +0, NaN above everything.  No value maps to 0 or to
+// 0xFFFFFFFF, so that a key of value and position can be told from "nothing" and from "nothing taken yet".
 __device__ __forceinline__ uint32_t order_of(float x) {
-    if (x != x) return 0xFFFFFFFFu;
+    if (x != x) return 0xFFFFFFFEu;
     const uint32_t b = __float_as_uint(x + 0.0f);
     return b ^ (b >> 31 ? 0xFFFFFFFFu : 0x80000000u);
 }

@@ -9,7 +9,8 @@ A training step of many jobs whose logits lie in one matrix, job j's rows being 
     adamw.step(active=alloc)                                          # only the jobs that were given cores
 
 Every call is asynchronous on ``stream`` (a torch stream or a raw cudaStream_t; default: torch's current stream of the
-tensors' device).  Results that are not given as ``out`` are allocated by torch.  Refusals raise ``SlaqError``.
+tensors' device).  Results that are not given as ``out`` are allocated by torch for that stream; inputs must stay alive until it
+has passed the call.  No call records anything for autograd.  Refusals raise ``SlaqError``.
 """
 
 from __future__ import annotations
@@ -318,6 +319,7 @@ class AdamW:
                                              _types[kind], _types[grad_kind], state_bits, raw, ctypes.byref(self._h))
         _check(rc, {-1: "a group out of range, betas outside [0, 1), a tensor listed twice, or tensors that overlap"}.get(rc))
         self._gpu, self._n_groups = gpu, len(groups)
+        self._streams = {raw}                       # those that use the plan's memory: torch gives it away when they have passed
 
     def _ok(self, rc):
         return _check(rc, self._lib.slaq_adamw_last_error(self._h).decode() if rc < 0 else None)
@@ -327,6 +329,9 @@ class AdamW:
         ``schedule_device``) is above 0; None: of all."""
         a = None if active is None else _vector(active, "active", _load().int32, self._n_groups, self._gpu)
         with _on(stream, self._gpu) as raw:
+            if raw not in self._streams:
+                self._streams.add(raw)
+                self._ws.record_stream(_load().cuda.ExternalStream(raw, device=self._gpu))
             self._ok(self._lib.slaq_adamw_step(self._h, a, raw))
 
     def set_group(self, group: int, stream=None, **values):

@@ -266,6 +266,46 @@ def test_many_small_tensors(slaq):
         at += n
 
 
+@pytest.mark.parametrize("given", [False, True])
+def test_memory_of_the_librarys_own_or_of_the_caller(slaq, given):
+    import ctypes
+
+    from paper_1802_04819_b200.training import _group, _Tensor
+    lib = slaq.load_library()
+    p, g, m, v = (torch.full((700,), x, device="cuda") for x in (1.0, 0.5, 0.0, 0.0))
+    table, groups, numels = (_Tensor * 1)(), (type(_group()) * 1)(_group(lr=0.25, weight_decay=0.0)), (ctypes.c_int64 * 1)(700)
+    for name, t in (("param", p), ("grad", g), ("exp_avg", m), ("exp_avg_sq", v)):
+        setattr(table[0], name, t.data_ptr())
+    table[0].n = 700
+    need = lib.slaq_adamw_workspace_bytes(1, ctypes.addressof(numels), 1)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    h = ctypes.c_void_p()
+    assert lib.slaq_adamw_create(ws.data_ptr(), need - 1, 1, table, 1, groups, 0, 0, 32, None, ctypes.byref(h)) == -4 and not h.value
+    assert lib.slaq_adamw_create(ws.data_ptr() if given else None, need if given else 0, 1, table, 1, groups, 0, 0, 32, None, ctypes.byref(h)) == 0
+    assert lib.slaq_adamw_step(h, None, None) == 0
+    torch.cuda.synchronize()
+    torch.testing.assert_close(p, torch.full_like(p, 0.75), rtol=1e-6, atol=0)
+    assert lib.slaq_adamw_destroy(h) == 0
+
+
+def test_a_plan_that_is_dropped_while_another_stream_steps(slaq):
+    """Its memory is not given to anybody before that stream has passed the steps."""
+    side = torch.cuda.Stream()
+    n = 3_000_000
+    p, g = torch.ones(n, device="cuda"), torch.ones(n, device="cuda")
+    torch.cuda.synchronize()
+    plan = slaq.AdamW([p], [g], groups=[dict(lr=0.01, weight_decay=0.0)])
+    torch.cuda.synchronize()
+    for _ in range(20):
+        plan.step(stream=side)
+    m, v = plan.exp_avg, plan.exp_avg_sq           # the states are the caller's to keep
+    del plan
+    junk = [torch.full((300_000,), 255, dtype=torch.uint8, device="cuda") for _ in range(20)]
+    torch.cuda.synchronize()
+    torch.testing.assert_close(p, torch.full_like(p, 0.8), rtol=0, atol=1e-4)
+    del junk, m, v
+
+
 def test_refusals(slaq):
     flat, g = torch.zeros(100, device="cuda"), torch.zeros(50, device="cuda")
     a, b = flat[:50], flat[50:]

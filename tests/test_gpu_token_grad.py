@@ -105,7 +105,7 @@ def test_a_factor_of_zero_leaves_zeros(slaq, vocab):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("vocab,pad", [(10, 0), (777, 0), (777, 3), (8192, 0), (50001, 0), (50001, 7), (200000, 8)])
+@pytest.mark.parametrize("vocab,pad", [(10, 0), (777, 0), (777, 3), (8192, 0), (50001, 0), (50001, 7), (200000, 8), (900001, 0)])
 def test_in_the_place_of_the_logits(slaq, vocab, pad, dtype):  # noqa: F811
     x, t, gen = _rows(6, vocab, dtype, pad, 2)
     g, h = _grads(6, gen)

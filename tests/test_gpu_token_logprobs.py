@@ -126,6 +126,26 @@ def test_alternatives_in_awkward_orders(slaq, vocab, order):
         _check(slaq.token_logprobs(x, t, top=top), ref.logprobs(x, t, 1.0, top), vocab, x, 1.0, top)
 
 
+@pytest.mark.parametrize("vocab", [20, 900, 6000, 200000])
+def test_rows_of_nan(slaq, vocab):
+    x = torch.full((3, vocab), math.nan, dtype=torch.bfloat16, device="cuda")
+    x[1, ::2] = 1.0
+    x[2, : vocab - 3] = -math.inf
+    t = torch.zeros(3, dtype=torch.int64, device="cuda")
+    for top in (2, 7):
+        got = slaq.token_logprobs(x, t, top=top)
+        assert bool(got.logprob.isnan().all()) and bool(got.entropy.isnan().all()) and bool(got.top_logprobs.isnan().all())
+        want = [list(range(top)), [2 * k + 1 for k in range(top)], ([vocab - 3, vocab - 2, vocab - 1] + list(range(top)))[:top]]
+        assert got.top_ids.tolist() == want
+
+
+@pytest.mark.parametrize("scale", [1e-38, 1e-6, 1e6, 1e30])
+def test_extreme_temperatures(slaq, scale):
+    """At a scale of 1e30 only the largest logit counts; at 1e-38 all are alike."""
+    x, t, _ = _rows(5, 3000, torch.float32, 0, 3)
+    _check(slaq.token_logprobs(x, t, top=4, scale=scale), ref.logprobs(x, t, scale, 4), 3000, x, scale, 4)
+
+
 def test_without_targets_only_the_rows_themselves_are_described(slaq):
     x, t, _ = _rows(9, 1234, torch.bfloat16, 2, 1)
     got = slaq.token_logprobs(x, top=4)

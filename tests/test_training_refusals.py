@@ -19,7 +19,7 @@ def lib():
 
 @pytest.mark.parametrize("change,code", [
     ({"type": 3}, -1), ({"type": -1}, -1), ({"rows": -1}, -1), ({"vocab": 0}, -1), ({"scale": 0.0}, -1), ({"scale": math.nan}, -1),
-    ({"scale": math.inf}, -1), ({"x": None}, -1), ({"stride": -4}, -1), ({"top": -1}, -1), ({"top": 3}, -1), ({"top": 33, "ids": P, "best": P}, -2),
+    ({"scale": math.inf}, -1), ({"scale": 2e30}, -1), ({"x": None}, -1), ({"stride": -4}, -1), ({"top": -1}, -1), ({"top": 3}, -1), ({"top": 33, "ids": P, "best": P}, -2),
     ({"vocab": (1 << 22) + 1}, -2), ({"rows": 1 << 31}, -2), ({"x": P + 2}, -1), ({"x": P + 1, "type": 1}, -1), ({"t": None}, -1),
     ({"rows": 0, "x": None, "t": None}, 0)])
 def test_log_probabilities(lib, change, code):
