@@ -38,30 +38,24 @@ struct TensorRef {
     int32_t group, first;            // the number of its first unit among all tensors' units
 };
 
-// What a step needs of a group, ready for its next step: the block that finishes a step last moves it on.
+// A group's numbers for its next step; the block that finishes a step last moves them on.
 struct Group {
-    double lr, beta1, beta2, power1, power2;   // power: beta to the number of the next step
+    double power1, power2;           // beta to the number of the next step
+    double beta1, beta2;
     int64_t step;                    // steps taken
-    float b1, a1, b2, a2, correct, eps, keep, size, grad_scale;
-    int32_t pad;
+    float b1, a1, b2, a2, eps, keep, lr, grad_scale;
 };
 
-__host__ __device__ inline void corrections(Group& g) {
-    g.correct = (float)(1.0 / sqrt(1.0 - g.power2));
-    g.size = (float)(g.lr / (1.0 - g.power1));
-}
 __host__ __device__ inline void set_step(Group& g, int64_t step) {
     g.step = step;
     g.power1 = pow(g.beta1, (double)(step + 1));
     g.power2 = pow(g.beta2, (double)(step + 1));
-    corrections(g);
 }
 // One product a step: a million steps put 1e-10 of their relative error into a power, which is 0 long before that.
 __device__ inline void advance(Group& g) {
     ++g.step;
     g.power1 *= g.beta1;
     g.power2 *= g.beta2;
-    corrections(g);
 }
 
 struct StepArgs {
@@ -255,10 +249,13 @@ __device__ __forceinline__ float reciprocal(float x) {
     return y;
 }
 
-// What a step needs of a group.
+// What a step needs of a group.  1 - beta^t is a difference of 64-bit numbers (1e-3 at the first step for beta2 = 0.999).
 struct Numbers {
     float b1, a1, b2, a2, correct, eps, keep, size, grad_scale;
 };
+__device__ __forceinline__ Numbers numbers_of(const Group& g) {
+    return {g.b1, g.a1, g.b2, g.a2, __frsqrt_rn((float)(1.0 - g.power2)), g.eps, g.keep, __fdiv_rn(g.lr, (float)(1.0 - g.power1)), g.grad_scale};
+}
 // The step of 8 elements: new weights, first moments, and second moments (their roots, if kRoot).  m and v come in units:
 // b1 and b2 hold the units' values.
 template <bool kRoot>
@@ -290,9 +287,7 @@ __device__ __forceinline__ void finish_step(const StepArgs& a) {
     if (arrived != gridDim.x - 1) return;
     for (int k = threadIdx.x; k < a.n_groups; k += kThreads)
         if (!a.active || a.active[k] > 0) {
-            Group g = a.groups[k];
-            advance(g);
-            a.groups[k] = g;
+            advance(a.groups[k]);
         }
     if (threadIdx.x == 0) *a.ticket = 0;
 }
@@ -309,12 +304,13 @@ struct RawState<true> {
 
 // Warp w of W takes units w, w + W, .. of all tensors' units in a row, so that the GPU's warps pass through a tensor side by side, and
 // what a tensor's blocks have in common is fetched again only when the tensor changes.  A lane's share of the next block, 48 to 128
-// bytes, is on its way in registers while a block is computed.
+// bytes, is asked for a block ahead, into registers.
 //
-// DRAM decides.  In 32 bits a unit is a block: with runs of four or eight blocks for each warp the step took a sixth longer
-// (209 M bf16 weights with masters: 886 us; 1040).  The wait for the number of the tensor after next, once a unit, keeps the
-// warps in step; without it 990.  Four thread blocks of four warps an SM are as many as the registers allow; more warps,
-// with spills, were slower.
+// DRAM decides.  In 32 bits a unit is a block: with runs of four or eight blocks for each warp the step took a sixth longer (209 M
+// bf16 weights with masters: 1040 us instead of 885, 6.60 TB/s).  And the next block is asked for behind this one's stores: asked
+// for before them, while the block is computed, its loads come between the stores of other warps (967 us).  In 8 bits,
+// where there is more to compute for a byte, it is the other way round (304 M fp32 weights: 783 us; behind the stores 875).
+// Four thread blocks of four warps an SM are as many as the registers allow; more warps, with spills, were slower.
 template <class P, class G, bool kMaster, bool kEight>
 __global__ void __launch_bounds__(kThreads) step_kernel(StepArgs a) {
     using W = std::conditional_t<kMaster, float, P>;      // what the step works on
@@ -363,8 +359,7 @@ __global__ void __launch_bounds__(kThreads) step_kernel(StepArgs a) {
             sq = static_cast<char*>(t.sq) + lane * 8 * kState;
             avg_scale = t.avg_scale + lane;
             sq_scale = t.sq_scale + lane;
-            const Group& group = a.groups[t.group];
-            c = {group.b1, group.a1, group.b2, group.a2, group.correct, group.eps, group.keep, group.size, group.grad_scale};
+            c = numbers_of(a.groups[t.group]);
         }
         const bool more = next == current;
         tensor = next;
@@ -408,7 +403,7 @@ __global__ void __launch_bounds__(kThreads) step_kernel(StepArgs a) {
                 }
                 const int ahead = block + 1 < end ? block + 1 : more ? following : whole_blocks;
                 fetched = ahead < whole_blocks;
-                if (fetched) load(ahead);                 // on its way while this one is computed
+                if (kEight && fetched) load(ahead);
                 step8<kEight>(c, b1, b2, p, g, m, v);
                 if (kMaster) store_whole8(to_master, p);
                 store_whole8(to, p);
@@ -419,6 +414,7 @@ __global__ void __launch_bounds__(kThreads) step_kernel(StepArgs a) {
                 } else {
                     store_whole8(reinterpret_cast<float*>(to_avg), m);
                     store_whole8(reinterpret_cast<float*>(to_sq), v);
+                    if (fetched) load(ahead);
                 }
             } else {                                      // a tensor's last block, or tensors that are not aligned
                 const int64_t left = n - ((int64_t)block * kBlock + lane * 8);
@@ -498,7 +494,7 @@ struct Ahead {
 
 // The same with 8-bit states where weights and gradients are of 16 bits and there is no master copy: a block is then 48 bytes a lane, and one ahead leaves 25 KB
 // on their way to an SM where 40 are wanted.  Three ahead, and 32 blocks in a row, whose scales fill a line of each state:
-// 519 us for 304 M elements, against 604 with one.  With more bytes a block it is the other way round (fp32: 1110 us against 790).
+// 528 us for 304 M elements (5.76 TB/s), against 604 with one; instructions bound it, 44 an element.  With more bytes a block it is the other way round (fp32: 1110 us against 790).
 template <class P>
 __global__ void __launch_bounds__(kThreads) deep_step_kernel(StepArgs a) {
     using Blocks = Ahead<P, P>;
@@ -520,8 +516,7 @@ __global__ void __launch_bounds__(kThreads) deep_step_kernel(StepArgs a) {
         char* const param = static_cast<char*>(t.param) + lane * 8 * sizeof(P);
         char* const avg = static_cast<char*>(t.avg) + lane * 8;
         char* const sq = static_cast<char*>(t.sq) + lane * 8;
-        const Group& group = a.groups[t.group];
-        const Numbers c = {group.b1, group.a1, group.b2, group.a2, group.correct, group.eps, group.keep, group.size, group.grad_scale};
+        const Numbers c = numbers_of(a.groups[t.group]);
         Blocks blocks(shared + (threadIdx.x >> 5));
         auto after = [&](int b) { return ((b + 1) & (unit - 1)) && b + 1 < all ? b + 1 : (b & -unit) + warps * unit; };
         int ahead = unit0 * unit;
@@ -640,7 +635,7 @@ bool group_ok(const slaq_adamw_group& g) {
 }
 Group device_group(const slaq_adamw_group& g) {
     Group d = {};
-    d.lr = g.lr, d.beta1 = g.beta1, d.beta2 = g.beta2;
+    d.lr = (float)g.lr, d.beta1 = g.beta1, d.beta2 = g.beta2;
     d.b1 = (float)g.beta1, d.a1 = (float)(1.0 - g.beta1), d.b2 = (float)g.beta2, d.a2 = (float)(1.0 - g.beta2);
     d.eps = (float)g.eps, d.keep = (float)(1.0 - g.lr * g.weight_decay), d.grad_scale = (float)g.grad_scale;
     set_step(d, g.step);
@@ -700,6 +695,7 @@ int create(slaq_adamw_handle* h, void* dev_ws, size_t bytes, int32_t n_tensors, 
     for (int32_t t = 0; t < n_tensors; ++t) any_master |= tensors[t].n > 0 && tensors[t].master;
     int unit = !eight ? 1 : param_type != SLAQ_F32 && grad_type != SLAQ_F32 && !any_master ? 32 : 8;
     while (unit > 1 && blocks < (int64_t)unit * 148 * 16) unit /= 2;
+    while (unit > 8 && blocks < (int64_t)unit * 8 * n_tensors) unit /= 2;   // short tensors end inside a unit (3,000 of 80 blocks: 120 us with 8, 134 with 32)
     for (int32_t t = 0; t < n_tensors; ++t) {
         const slaq_adamw_tensor& x = tensors[t];
         if (x.n < 0 || x.group < 0 || x.group >= n_groups) return SLAQ_E_ARG;
