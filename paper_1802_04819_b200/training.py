@@ -22,24 +22,24 @@ from typing import NamedTuple
 
 import numpy as np
 
-from .binding import SlaqError, load_library
+from .binding import SlaqError, _marshal, load_library
 
 F32, BF16, F16 = 0, 1, 2
 MAX_VOCAB, MAX_TOP = 1 << 22, 32
 STATE_BLOCK = 256
 
-_torch = _current_stream = _current_device = None
-_types = {}
-
-
-def _lib():
-    return load_library()
+_torch = _calls = _address = _current_stream = _current_device = None
+_types, _at = {}, {}          # element types; the addresses of the C functions
 
 
 def _load():
-    global _torch, _current_stream, _current_device
+    global _torch, _calls, _address, _current_stream, _current_device
     if _torch is None:
         import torch
+        lib, _calls = load_library(), _marshal()
+        for name in ("token_logprobs", "token_logprobs_grad", "token_loss", "job_row_grad", "job_losses", "adamw_step"):
+            _at[name] = ctypes.cast(getattr(lib, "slaq_" + name), c_void_p).value
+        _address = _calls.address
         _types.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
         # the address alone: torch.cuda.current_stream() makes an object, 3 of the 8 us of a call
         _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
@@ -64,11 +64,10 @@ def _check(rc, message=None):
 
 def _vector(t, name, dtype, n, device):
     """The address of a contiguous tensor of n entries on GPU `device`; None passes."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.get_device() != device or t.numel() != n or not t.is_contiguous():
+    at = _address(t, dtype, n, device)
+    if at is False:
         _refuse(f"{name} is not a contiguous {dtype} tensor of {n} entries on GPU {device}")
-    return t.data_ptr()
+    return at
 
 
 def _matrix(t, name):
@@ -85,36 +84,20 @@ def _matrix(t, name):
     return t.data_ptr(), kind, rows, vocab, pitch, t.get_device()
 
 
-class _Here:
-    """The current stream of the current device: the common case, without a context to enter."""
-    __slots__ = ("raw",)
-
-    def __init__(self, raw):
-        self.raw = raw
-
-    def __enter__(self):
-        return self.raw
-
-    def __exit__(self, *exc):
-        return False
-
-
 @contextlib.contextmanager
 def _elsewhere(stream, device):
-    """Another stream than torch's current one, or another device: what is allocated there belongs there."""
+    """Another stream than torch's current one, or another device, as the current ones: what is allocated there belongs there."""
     torch = _load()
     with torch.cuda.device(device):
         if stream is None:
-            yield torch.cuda.current_stream().cuda_stream
+            yield
         else:
             with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream):
-                yield getattr(stream, "cuda_stream", stream)
+                yield
 
 
-def _on(stream, device):
-    if stream is None and device == _current_device():
-        return _Here(_current_stream(device))
-    return _elsewhere(stream, device)
+def _is_here(stream, device):
+    return stream is None and device == _current_device()
 
 
 class TokenLogprobs(NamedTuple):
@@ -130,31 +113,37 @@ def token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, strea
     the row is not asked for) or None, ``top`` alternatives (0 .. 32), ``scale`` the inverse temperature."""
     torch = _load()
     x, kind, rows, vocab, pitch, gpu = _matrix(logits, "logits")
+    if not _is_here(stream, gpu):
+        with _elsewhere(stream, gpu):
+            return token_logprobs(logits, targets, top, scale)
     t = _vector(targets, "targets", torch.int64, rows, gpu)
     if not 0 <= top <= MAX_TOP:
         raise SlaqError(-1 if top < 0 else -2, f"top is 0 .. {MAX_TOP}")
-    device = logits.device
-    with _on(stream, gpu) as raw:
-        logprob = None if t is None else torch.empty(rows, device=device, dtype=torch.float32)
-        entropy = torch.empty(rows, device=device, dtype=torch.float32)
-        norm = torch.empty((rows, 2), device=device, dtype=torch.float32)
-        ids = best = None
-        if top:
-            ids = torch.empty((rows, top), device=device, dtype=torch.int32)
-            best = torch.empty((rows, top), device=device, dtype=torch.float32)
-        rc = _lib().slaq_token_logprobs(x, kind, rows, vocab, pitch, t, scale, None if t is None else logprob.data_ptr(), entropy.data_ptr(),
-                                        norm.data_ptr(), top, ids.data_ptr() if top else None, best.data_ptr() if top else None, raw)
+    empty, device, f32 = torch.empty, logits.device, torch.float32
+    logprob = None if t is None else empty(rows, device=device, dtype=f32)
+    entropy, norm = empty(rows, device=device, dtype=f32), empty((rows, 2), device=device, dtype=f32)
+    ids = best = to_ids = to_best = None
+    if top:
+        ids, best = empty((rows, top), device=device, dtype=torch.int32), empty((rows, top), device=device, dtype=f32)
+        to_ids, to_best = ids.data_ptr(), best.data_ptr()
+    rc = _calls.token_logprobs(_at["token_logprobs"], x, kind, rows, vocab, pitch, t, scale, None if t is None else logprob.data_ptr(),
+                               entropy.data_ptr(), norm.data_ptr(), top, to_ids, to_best, _current_stream(gpu))
     if rc < 0:
         _check(rc)
     return TokenLogprobs(logprob, entropy, norm, ids, best)
 
 
 def _gradient(out, logits):
+    """(the gradient's tensor, its address, its row stride)"""
     if out is None:
-        return _load().empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    if out.shape != logits.shape or out.dtype is not logits.dtype or out.get_device() != logits.get_device() or (out.stride(1) != 1 and out.shape[1] > 1):
-        _refuse("out is not a matrix like logits with its rows' elements next to one another")
-    return out
+        out = _load().empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    elif out is not logits:
+        if out.shape != logits.shape or out.dtype is not logits.dtype or out.get_device() != logits.get_device() or (out.stride(1) != 1 and out.shape[1] > 1):
+            _refuse("out is not a matrix like logits with its rows' elements next to one another")
+    return out, out.data_ptr(), out.stride(0)
+
+
+_GRADIENT = "bad argument: a missing input, a scale that is not positive, or a gradient that overlaps the logits otherwise than row for row"
 
 
 def token_logprobs_grad(logits, targets, norm, grad_logprob, entropy=None, grad_entropy=None, scale: float = 1.0, out=None, stream=None):
@@ -162,13 +151,17 @@ def token_logprobs_grad(logits, targets, norm, grad_logprob, entropy=None, grad_
     ``token_logprobs`` returned.  ``out`` may be ``logits`` itself."""
     torch = _load()
     x, kind, rows, vocab, pitch, gpu = _matrix(logits, "logits")
+    if not _is_here(stream, gpu):
+        with _elsewhere(stream, gpu):
+            return token_logprobs_grad(logits, targets, norm, grad_logprob, entropy, grad_entropy, scale, out)
+    f32 = torch.float32
     t = _vector(targets, "targets", torch.int64, rows, gpu)
-    n, g = _vector(norm, "norm", torch.float32, 2 * rows, gpu), _vector(grad_logprob, "grad_logprob", torch.float32, rows, gpu)
-    e, h = _vector(entropy, "entropy", torch.float32, rows, gpu), _vector(grad_entropy, "grad_entropy", torch.float32, rows, gpu)
-    with _on(stream, gpu) as raw:
-        out = _gradient(out, logits)
-        _check(_lib().slaq_token_logprobs_grad(x, kind, rows, vocab, pitch, t, scale, n, e, g, h, out.data_ptr(), out.stride(0), raw),
-               "bad argument: a missing input, a scale that is not positive, or a gradient that overlaps the logits otherwise than row for row")
+    n, g = _vector(norm, "norm", f32, 2 * rows, gpu), _vector(grad_logprob, "grad_logprob", f32, rows, gpu)
+    e, h = _vector(entropy, "entropy", f32, rows, gpu), _vector(grad_entropy, "grad_entropy", f32, rows, gpu)
+    out, to, to_pitch = _gradient(out, logits)
+    rc = _calls.token_logprobs_grad(_at["token_logprobs_grad"], x, kind, rows, vocab, pitch, t, scale, n, e, g, h, to, to_pitch, _current_stream(gpu))
+    if rc < 0:
+        _check(rc, _GRADIENT if rc == -1 else None)
     return out
 
 
@@ -176,59 +169,77 @@ def token_loss(logits, targets, row_grad, scale: float = 1.0, out=None, stream=N
     """slaq_token_loss: (log probabilities, gradient of sum(row_grad x logprob) by the logits) in one call."""
     torch = _load()
     x, kind, rows, vocab, pitch, gpu = _matrix(logits, "logits")
+    if not _is_here(stream, gpu):
+        with _elsewhere(stream, gpu):
+            return token_loss(logits, targets, row_grad, scale, out)
     t, g = _vector(targets, "targets", torch.int64, rows, gpu), _vector(row_grad, "row_grad", torch.float32, rows, gpu)
-    with _on(stream, gpu) as raw:
-        out = _gradient(out, logits)
-        logprob = torch.empty(rows, device=out.device, dtype=torch.float32)
-        _check(_lib().slaq_token_loss(x, kind, rows, vocab, pitch, t, scale, g, logprob.data_ptr(), out.data_ptr(), out.stride(0), raw),
-               "bad argument: a missing input, a scale that is not positive, or a gradient that overlaps the logits otherwise than row for row")
+    out, to, to_pitch = _gradient(out, logits)
+    logprob = torch.empty(rows, device=out.device, dtype=torch.float32)
+    rc = _calls.token_loss(_at["token_loss"], x, kind, rows, vocab, pitch, t, scale, g, logprob.data_ptr(), to, to_pitch, _current_stream(gpu))
+    if rc < 0:
+        _check(rc, _GRADIENT if rc == -1 else None)
     return logprob, out
+
+
+def _job_offsets(offsets, gpu):
+    """(jobs, address): at least one entry on the GPU that the rows are on."""
+    if gpu < 0:
+        _refuse("the rows are not on a GPU")
+    n = offsets.numel() - 1
+    if n < 0:
+        _refuse("offsets has no entry")
+    return n, _vector(offsets, "offsets", _load().int64, n + 1, gpu)
 
 
 def job_row_grad(offsets, targets=None, weights=None, out=None, stream=None):
     """slaq_job_row_grad: the derivative of each job's mean loss by the log probability of each of its rows (float32 [rows]).
     ``offsets`` int64 [jobs + 1]; rows before the first job and behind the last keep what ``out`` holds (without ``out``: 0)."""
     torch = _load()
-    known = next((t for t in (targets, weights, out) if t is not None), None)
+    known = targets if targets is not None else weights if weights is not None else out
     if known is None:
         _refuse("the number of rows follows from targets, weights or out: one of them is wanted")
-    rows, gpu = known.numel(), offsets.get_device()
-    if gpu < 0:
-        _refuse("offsets lies not on a GPU")
-    t, w = _vector(targets, "targets", torch.int64, rows, gpu), _vector(weights, "weights", torch.float32, rows, gpu)
-    n = offsets.numel() - 1
-    off = _vector(offsets, "offsets", torch.int64, max(n, 0) + 1, gpu)
-    with _on(stream, gpu) as raw:
-        fresh = out is None
-        if fresh:
-            out = torch.empty(rows, dtype=torch.float32, device=offsets.device)
-        _check(_lib().slaq_job_row_grad(n, off, rows, t, w, _vector(out, "out", torch.float32, rows, gpu), fresh, raw))
+    rows, gpu = known.numel(), known.get_device()
+    n, off = _job_offsets(offsets, gpu)
+    if not _is_here(stream, gpu):
+        with _elsewhere(stream, gpu):
+            return job_row_grad(offsets, targets, weights, out)
+    t, w, fresh = _vector(targets, "targets", torch.int64, rows, gpu), _vector(weights, "weights", torch.float32, rows, gpu), out is None
+    if fresh:
+        out = (torch.empty if n else torch.zeros)(rows, device=known.device, dtype=torch.float32)
+    to = _vector(out, "out", torch.float32, rows, gpu)
+    rc = _calls.job_row_grad(_at["job_row_grad"], n, off, rows, t, w, to, fresh and n > 0, _current_stream(gpu))
+    if rc < 0:
+        _check(rc)
     return out
-
-
-def _job_inputs(offsets, targets, logprob, weights):
-    torch = _load()
-    rows, gpu, n = logprob.numel(), logprob.get_device(), offsets.numel() - 1
-    if gpu < 0:
-        _refuse("logprob lies not on a GPU")
-    return (n, gpu, _vector(offsets, "offsets", torch.int64, max(n, 0) + 1, gpu), rows, _vector(targets, "targets", torch.int64, rows, gpu),
-            _vector(logprob, "logprob", torch.float32, rows, gpu), _vector(weights, "weights", torch.float32, rows, gpu))
 
 
 def job_losses(offsets, targets, logprob, weights=None, out=None, stream=None):
     """slaq_job_losses: float64 [jobs], the weighted mean of -logprob over each job's rows that count."""
     torch = _load()
-    n, gpu, off, rows, t, lp, w = _job_inputs(offsets, targets, logprob, weights)
-    with _on(stream, gpu) as raw:
-        if out is None:
-            out = torch.empty(n, dtype=torch.float64, device=logprob.device)
-        _check(_lib().slaq_job_losses(n, off, rows, t, lp, w, _vector(out, "out", torch.float64, n, gpu), raw))
+    rows, gpu = logprob.numel(), logprob.get_device()
+    n, off = _job_offsets(offsets, gpu)
+    if not _is_here(stream, gpu):
+        with _elsewhere(stream, gpu):
+            return job_losses(offsets, targets, logprob, weights, out)
+    t, lp = _vector(targets, "targets", torch.int64, rows, gpu), _vector(logprob, "logprob", torch.float32, rows, gpu)
+    w = _vector(weights, "weights", torch.float32, rows, gpu)
+    if out is None:
+        out = torch.empty(n, device=logprob.device, dtype=torch.float64)
+    to = _vector(out, "out", torch.float64, n, gpu)
+    rc = _calls.job_losses(_at["job_losses"], n, off, rows, t, lp, w, to, _current_stream(gpu))
+    if rc < 0:
+        _check(rc)
     return out
 
 
 def append_token_losses(sched, d_job_ids, offsets, targets, logprob, weights, d_iter_times, d_cores_used, out):
     torch = _load()
-    n, gpu, off, rows, t, lp, w = _job_inputs(offsets, targets, logprob, weights)
+    rows, gpu, n = logprob.numel(), logprob.get_device(), d_job_ids.numel()
+    jobs, off = _job_offsets(offsets, gpu)
+    if jobs != n:
+        _refuse("offsets has one entry more than there are jobs")
+    t, lp = _vector(targets, "targets", torch.int64, rows, gpu), _vector(logprob, "logprob", torch.float32, rows, gpu)
+    w = _vector(weights, "weights", torch.float32, rows, gpu)
     if out is None:
         out = torch.empty(n, dtype=torch.float64, device=logprob.device)
     sched._check(sched._lib.slaq_append_token_losses(
@@ -282,7 +293,8 @@ class AdamW:
             _refuse("parameters are fp32, bf16 or fp16 tensors on a GPU, with a gradient and a group each")
 
         gpu = device.index
-        with _on(stream, gpu) as raw:
+        with contextlib.nullcontext() if _is_here(stream, gpu) else _elsewhere(stream, gpu):
+            raw = _current_stream(gpu)
             def states(given, dtype, count):
                 return [torch.zeros(count(p), device=device).to(dtype) for p in params] if given is None else list(given)
             blocks = lambda p: -(-p.numel() // STATE_BLOCK)   # noqa: E731
@@ -296,23 +308,23 @@ class AdamW:
                 _refuse("gradients are of the parameters' type or fp32")
             lists = [("params", params, kind), ("grads", grads, grad_kind), ("masters", self.masters, torch.float32),
                      ("exp_avg", self.exp_avg, state), ("exp_avg_sq", self.exp_avg_sq, state)]
-            table = (_Tensor * n)()
+            table, sizes = (_Tensor * n)(), [p.numel() for p in params]
             for name, field, tensors, dtype in [(f, {"params": "param", "grads": "grad", "masters": "master"}.get(f, f), ts, d) for f, ts, d in lists]:
                 if tensors is None:
                     continue
                 if len(tensors) != n:
                     _refuse(f"{name} has another length than params")
-                for row, p, t in zip(table, params, tensors):
-                    setattr(row, field, _vector(t, name, dtype, p.numel(), gpu))
+                for row, size, t in zip(table, sizes, tensors):
+                    setattr(row, field, _vector(t, name, dtype, size, gpu))
             if eight:
                 for name, tensors in (("exp_avg_scale", self.exp_avg_scale), ("exp_avg_sq_scale", self.exp_avg_sq_scale)):
                     if len(tensors) != n:
                         _refuse(f"{name} has another length than params")
-                    for row, p, t in zip(table, params, tensors):
-                        setattr(row, name, _vector(t, name, torch.float32, blocks(p), gpu))
-            for row, p, k in zip(table, params, group_of):
-                row.n, row.group = p.numel(), k
-            numels = np.array([p.numel() for p in params], np.int64)
+                    for row, size, t in zip(table, sizes, tensors):
+                        setattr(row, name, _vector(t, name, torch.float32, -(-size // STATE_BLOCK), gpu))
+            for row, size, k in zip(table, sizes, group_of):
+                row.n, row.group = size, k
+            numels = np.array(sizes, np.int64)
             need = self._lib.slaq_adamw_workspace_bytes(n, numels.ctypes.data, len(groups))
             self._ws = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
             rc = self._lib.slaq_adamw_create(self._ws.data_ptr(), need, n, table, len(groups), (_Group * len(groups))(*groups),
@@ -324,23 +336,32 @@ class AdamW:
     def _ok(self, rc):
         return _check(rc, self._lib.slaq_adamw_last_error(self._h).decode() if rc < 0 else None)
 
+    def _run(self, stream, call):
+        with contextlib.nullcontext() if _is_here(stream, self._gpu) else _elsewhere(stream, self._gpu):
+            self._ok(call(_current_stream(self._gpu)))
+
     def step(self, active=None, stream=None):
         """One step of the groups whose entry of ``active`` (int32 CUDA tensor [groups], for instance the allocation of
         ``schedule_device``) is above 0; None: of all."""
-        a = None if active is None else _vector(active, "active", _load().int32, self._n_groups, self._gpu)
-        with _on(stream, self._gpu) as raw:
-            if raw not in self._streams:
-                self._streams.add(raw)
-                self._ws.record_stream(_load().cuda.ExternalStream(raw, device=self._gpu))
-            self._ok(self._lib.slaq_adamw_step(self._h, a, raw))
+        if not _is_here(stream, self._gpu):
+            with _elsewhere(stream, self._gpu):
+                return self.step(active)
+        a = _vector(active, "active", _torch.int32, self._n_groups, self._gpu)
+        raw = _current_stream(self._gpu)
+        if raw not in self._streams:
+            self._streams.add(raw)
+            self._ws.record_stream(_torch.cuda.ExternalStream(raw, device=self._gpu))
+        rc = _calls.adamw_step(_at["adamw_step"], self._h.value, a, raw)
+        if rc < 0:
+            self._ok(rc)
 
     def set_group(self, group: int, stream=None, **values):
         """New numbers of a group from the next step on; what is not named stays as it is, the count of steps too."""
         if not 0 <= group < self._n_groups:
             raise SlaqError(-2, "no such group")
         merged = {**self._groups[group], **values}
-        with _on(stream, self._gpu) as raw:
-            self._ok(self._lib.slaq_adamw_set_group(self._h, group, ctypes.byref(_group(**{"step": -1, **{k: v for k, v in merged.items() if k != "step"}, **values})), raw))
+        numbers = _group(**{"step": -1, **{k: v for k, v in merged.items() if k != "step"}, **values})
+        self._run(stream, lambda raw: self._lib.slaq_adamw_set_group(self._h, group, ctypes.byref(numbers), raw))
         self._groups[group] = merged
 
     def set_grads(self, grads, stream=None):
@@ -348,18 +369,14 @@ class AdamW:
         grads = list(grads)
         if len(grads) != len(self.params):
             _refuse("grads has another length than params")
-        for g, old in zip(grads, self.grads):
-            _vector(g, "grads", old.dtype, old.numel(), self._gpu)
-        rows = (c_void_p * len(grads))(*[g.data_ptr() for g in grads])
-        with _on(stream, self._gpu) as raw:
-            self._ok(self._lib.slaq_adamw_set_grads(self._h, rows, raw))
+        rows = (c_void_p * len(grads))(*[_vector(g, "grads", old.dtype, old.numel(), self._gpu) for g, old in zip(grads, self.grads)])
+        self._run(stream, lambda raw: self._lib.slaq_adamw_set_grads(self._h, rows, raw))
         self.grads = grads
 
     def get_steps(self, stream=None) -> np.ndarray:
         """Steps taken per group; waits for the stream."""
         out = np.empty(self._n_groups, np.int64)
-        with _on(stream, self._gpu) as raw:
-            self._ok(self._lib.slaq_adamw_get_steps(self._h, out.ctypes.data, raw))
+        self._run(stream, lambda raw: self._lib.slaq_adamw_get_steps(self._h, out.ctypes.data, raw))
         return out
 
     def close(self):
