@@ -121,10 +121,10 @@ def token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, strea
         raise SlaqError(-1 if top < 0 else -2, f"top is 0 .. {MAX_TOP}")
     empty, device, f32 = torch.empty, logits.device, torch.float32
     logprob = None if t is None else empty(rows, device=device, dtype=f32)
-    entropy, norm = empty(rows, device=device, dtype=f32), empty((rows, 2), device=device, dtype=f32)
+    entropy, norm = empty(rows, device=device, dtype=f32), empty(rows, 2, device=device, dtype=f32)
     ids = best = to_ids = to_best = None
     if top:
-        ids, best = empty((rows, top), device=device, dtype=torch.int32), empty((rows, top), device=device, dtype=f32)
+        ids, best = empty(rows, top, device=device, dtype=torch.int32), empty(rows, top, device=device, dtype=f32)
         to_ids, to_best = ids.data_ptr(), best.data_ptr()
     rc = _calls.token_logprobs(_at["token_logprobs"], x, kind, rows, vocab, pitch, t, scale, None if t is None else logprob.data_ptr(),
                                entropy.data_ptr(), norm.data_ptr(), top, to_ids, to_best, _current_stream(gpu))
