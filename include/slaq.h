@@ -576,8 +576,9 @@ int slaq_append_token_losses(slaq_t* h, int32_t n, const int32_t* d_job_ids, con
  * none has) the step works on it and param receives its rounding.
  * state_bits 32: exp_avg = m and exp_avg_sq = v are float [n].
  * state_bits 8: both are e4m3 codes [n]; elements 256 b .. 256 b + 255 share the scales [b] ([ceil(n / 256)] floats):
- * m = code x exp_avg_scale, sqrt(v) = code x exp_avg_sq_scale.  A block's scale is its largest (finite) value / 448, and 0, with
- * its codes, where that value is below 2^-100.  Rounded to nearest; a non-zero second moment never rounds to zero.
+ * m = code x exp_avg_scale, sqrt(v) = code x exp_avg_sq_scale.  A block's scale is its largest (finite) value x (1 / 448), and 0, with
+ * its codes, where that value is below 2^-100; a code is the e4m3 nearest to the value x ((1 / largest) x 448), every operation
+ * rounded to 32 bits.  A non-zero second moment never rounds to zero.
  */
 typedef struct slaq_adamw_tensor {
     void* param;

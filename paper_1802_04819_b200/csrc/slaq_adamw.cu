@@ -219,8 +219,8 @@ __device__ __forceinline__ uint2 codes_of(const Eight& x, float inverse, bool fi
     }
     return make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410));
 }
-// Both states of the warp's 256 elements as codes, and their scales, largest / 448.  What is not finite stays so in its own
-// element (NaN).
+// Both states of the warp's 256 elements as codes, and their scales, largest x (1 / 448); a value becomes a code by (1 / largest) x 448.
+// What is not finite stays so in its own element (NaN).
 struct Codes {
     uint2 m, r;
     float m_scale, r_scale;
@@ -229,12 +229,12 @@ __device__ __forceinline__ Codes encode(const Eight& m, const Eight& r, int lane
     float most_m = largest<false>(m), most_r = largest<true>(r);
     const bool finite = most_m < CUDART_INF_F && most_r < CUDART_INF_F;
     if (!finite) most_m = largest_finite(m), most_r = largest_finite(r);
-    // lanes 0 and 1 divide for the scales of m and r, lanes 2 and 3 for their inverses; nothing is kept of what is too small
+    // even lanes invert for m, odd ones for r; nothing is kept of what is too small
     const float most = lane & 1 ? most_r : most_m;
-    float q = __fdiv_rn(lane & 2 ? kE4m3Max : most, lane & 2 ? most : kE4m3Max);
-    q = most >= kTiny ? q : 0.0f;
-    return {codes_of<false>(m, __shfl_sync(~0u, q, 2), finite), codes_of<true>(r, __shfl_sync(~0u, q, 3), finite), __shfl_sync(~0u, q, 0),
-            __shfl_sync(~0u, q, 1)};
+    const float inverse = most >= kTiny ? __frcp_rn(most) * kE4m3Max : 0.0f;
+    constexpr float kPer = 1.0f / kE4m3Max;
+    return {codes_of<false>(m, __shfl_sync(~0u, inverse, 0), finite), codes_of<true>(r, __shfl_sync(~0u, inverse, 1), finite),
+            most_m >= kTiny ? most_m * kPer : 0.0f, most_r >= kTiny ? most_r * kPer : 0.0f};
 }
 
 // sqrt and 1/x to 1 ulp or two, denormal arguments of the root included
@@ -249,6 +249,14 @@ __device__ __forceinline__ float reciprocal(float x) {
     return y;
 }
 
+// a + b of products that keep their own rounding: mul.rn.f32x2 and add.rn.f32x2 are merged, add.rn.f32 is not.
+__device__ __forceinline__ Pair sum_of_products(Pair a, Pair b) {
+    float p, q, r, t;
+    split(a, p, q);
+    split(b, r, t);
+    return pair_of(__fadd_rn(p, r), __fadd_rn(q, t));
+}
+
 // What a step needs of a group.  1 - beta^t is a difference of 64-bit numbers (1e-3 at the first step for beta2 = 0.999).
 struct Numbers {
     float b1, a1, b2, a2, correct, eps, keep, size, grad_scale;
@@ -256,22 +264,33 @@ struct Numbers {
 __device__ __forceinline__ Numbers numbers_of(const Group& g) {
     return {g.b1, g.a1, g.b2, g.a2, __frsqrt_rn((float)(1.0 - g.power2)), g.eps, g.keep, __fdiv_rn(g.lr, (float)(1.0 - g.power1)), g.grad_scale};
 }
-// The step of 8 elements: new weights, first moments, and second moments (their roots, if kRoot).  m and v come in units:
-// b1 and b2 hold the units' values.
-template <bool kRoot>
-__device__ __forceinline__ void step8(const Numbers& c, float b1, float b2, Eight& p, const Eight& g, Eight& m, Eight& v) {
+// The step of 8 elements: new weights, first moments, and second moments.  With kCodes the states come as codes, whose units
+// are m_scale and r_scale, and the roots of the second moments are returned.
+//
+// With codes, m and v are rounded after every product and sum: a code is a decision, and the formula's own, taken operation by
+// operation, is what a checkpoint or another implementation can be held to.  With fused products 51 of 16 M codes of m and the
+// last bit of every fourth scale differed after two steps; without, none of m, and of the second moment the last bit of
+// every fourth scale and 2 to 6 codes in 16 M, for the root is good to 1 ulp (an exact one costs 8 %).  It costs 2 %.
+template <bool kCodes>
+__device__ __forceinline__ void step8(const Numbers& c, float m_scale, float r_scale, Eight& p, const Eight& g, Eight& m, Eight& v) {
     auto two = [](float x) { return pair_of(x, x); };
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const Pair x = g.at[k] * two(c.grad_scale);
-        m.at[k] = fma2(two(b1), m.at[k], two(c.a1) * x);
-        v.at[k] = fma2(two(c.a2) * x, x, two(b2) * v.at[k]);
+        if (kCodes) {
+            const Pair old = v.at[k] * two(r_scale);
+            m.at[k] = sum_of_products(two(c.b1) * (m.at[k] * two(m_scale)), two(c.a1) * x);
+            v.at[k] = sum_of_products(two(c.b2) * (old * old), two(c.a2) * (x * x));
+        } else {
+            m.at[k] = fma2(two(c.b1), m.at[k], two(c.a1) * x);
+            v.at[k] = fma2(two(c.b2), v.at[k], two(c.a2) * x * x);
+        }
         float a, b;
         v.get(k, a, b);
         const Pair r = pair_of(root(a), root(b));
         split(fma2(r, two(c.correct), two(c.eps)), a, b);
         p.at[k] = fma2(two(-c.size), m.at[k] * pair_of(reciprocal(a), reciprocal(b)), p.at[k] * two(c.keep));
-        if (kRoot) v.at[k] = r;
+        if (kCodes) v.at[k] = r;
     }
 }
 
@@ -378,18 +397,9 @@ __global__ void __launch_bounds__(kThreads) step_kernel(StepArgs a) {
             char* const to_avg = avg + (int64_t)block * (kBlock * kState);
             char* const to_sq = sq + (int64_t)block * (kBlock * kState);
             Eight p, g, m, v;
-            float b1 = c.b1, b2 = c.b2;
-            if constexpr (kEight) {
-                const float by = __shfl_sync(~0u, old_r, block - begin);
-                b1 *= __shfl_sync(~0u, old_m, block - begin);
-                b2 *= by * by;
-            }
-            auto from_codes = [&](uint2 codes_m, uint2 codes_r) {
-                m = unpack_codes(codes_m);
-                v = unpack_codes(codes_r);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v.at[k] = v.at[k] * v.at[k];
-            };
+            float by_m = 1.0f, by_r = 1.0f;
+            if constexpr (kEight) by_m = __shfl_sync(~0u, old_m, block - begin), by_r = __shfl_sync(~0u, old_r, block - begin);
+            auto from_codes = [&](uint2 codes_m, uint2 codes_r) { m = unpack_codes(codes_m), v = unpack_codes(codes_r); };
             Codes codes = {};
             if (block < whole_blocks) {
                 if (!fetched) load(block);
@@ -404,7 +414,7 @@ __global__ void __launch_bounds__(kThreads) step_kernel(StepArgs a) {
                 const int ahead = block + 1 < end ? block + 1 : more ? following : whole_blocks;
                 fetched = ahead < whole_blocks;
                 if (kEight && fetched) load(ahead);
-                step8<kEight>(c, b1, b2, p, g, m, v);
+                step8<kEight>(c, by_m, by_r, p, g, m, v);
                 if (kMaster) store_whole8(to_master, p);
                 store_whole8(to, p);
                 if constexpr (kEight) {
@@ -426,7 +436,7 @@ __global__ void __launch_bounds__(kThreads) step_kernel(StepArgs a) {
                     m = load_some(reinterpret_cast<const float*>(to_avg), left);
                     v = load_some(reinterpret_cast<const float*>(to_sq), left);
                 }
-                step8<kEight>(c, b1, b2, p, g, m, v);
+                step8<kEight>(c, by_m, by_r, p, g, m, v);
                 if (kMaster) store_some(to_master, left, p);
                 store_some(to, left, p);
                 if constexpr (kEight) {
@@ -535,13 +545,11 @@ __global__ void __launch_bounds__(kThreads) deep_step_kernel(StepArgs a) {
             char* const to_avg = avg + (int64_t)block * kBlock;
             char* const to_sq = sq + (int64_t)block * kBlock;
             const int64_t left = t.n - ((int64_t)block * kBlock + lane * 8);
-            const float by = __shfl_sync(~0u, old_r, place), b1 = c.b1 * __shfl_sync(~0u, old_m, place), b2 = c.b2 * (by * by);
+            const float by_m = __shfl_sync(~0u, old_m, place), by_r = __shfl_sync(~0u, old_r, place);
             Eight p, g, m, v;
             Codes codes = {};
             auto step = [&] {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v.at[k] = v.at[k] * v.at[k];
-                step8<true>(c, b1, b2, p, g, m, v);
+                step8<true>(c, by_m, by_r, p, g, m, v);
                 codes = encode(m, v, lane);
             };
             if (block < whole) {

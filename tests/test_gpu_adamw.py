@@ -127,7 +127,9 @@ def test_steps_with_8_bit_states(slaq, pt, gt, master, shift):
 
 
 def test_a_block_is_rounded_as_e4m3_is(slaq):
-    """With b1 = b2 = 0 the states are the gradients themselves: their codes follow from the type's own rounding."""
+    """With b1 = b2 = 0 the states are the gradients themselves: their codes follow from the type's own rounding.
+    A scale is the largest x (1 / 448), a code the value x ((1 / largest) x 448), as the header says, all in 32 bits."""
+    per = torch.tensor(1.0) / torch.tensor(448.0)
     g = torch.cat([torch.linspace(-3, 3, 256), torch.logspace(-8, 0, 256), torch.zeros(256), torch.full((100,), 1e-38)]).cuda()
     p = torch.zeros_like(g)
     plan = slaq.AdamW([p], [g], groups=[dict(betas=(0.0, 0.0))], state_bits=8)
@@ -136,12 +138,12 @@ def test_a_block_is_rounded_as_e4m3_is(slaq):
         x = g[lo: lo + 256].cpu()
         most, b = x.abs().max(), lo // 256
         kept = most >= 2.0 ** -100
-        inv = torch.tensor(448.0) / most if kept else torch.tensor(0.0)
-        assert float(plan.exp_avg_scale[0][b]) == (float(most / 448.0) if kept else 0.0)
+        inv = torch.tensor(1.0) / most * torch.tensor(448.0) if kept else torch.tensor(0.0)
+        assert float(plan.exp_avg_scale[0][b]) == (float(most * per) if kept else 0.0)
         assert torch.equal(plan.exp_avg[0][lo: lo + 256].cpu().float(), (x * inv).to(torch.float8_e4m3fn).float())
         r = torch.sqrt(x * x)
         most = r.max()
-        inv = torch.tensor(448.0) / most if kept else torch.tensor(0.0)
+        inv = torch.tensor(1.0) / most * torch.tensor(448.0) if kept else torch.tensor(0.0)
         want = torch.where((r > 0) & bool(kept), (r * inv).clamp_min(2.0 ** -9), r * inv).to(torch.float8_e4m3fn).float()
         assert torch.equal(plan.exp_avg_sq[0][lo: lo + 256].cpu().float(), want)
 
