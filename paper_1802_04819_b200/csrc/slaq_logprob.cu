@@ -147,6 +147,50 @@ __device__ __forceinline__ Vector<E> gradient_of_kind(const Gradient& r) {
     for (int i = 0; i < Vector<E>::N / 2; ++i) out.put(i, p);
     return out;
 }
+// .. and what L lanes write vector by vector: the target's own term comes afterwards, from the thread that wrote its vector
+template <bool kEntropy, class E>
+__device__ __forceinline__ void store_vector(const Row<E>& to, E* row, int v, const Vector<E>& in, const Gradient& y) {
+    if (v >= to.vectors) return;
+    const Vector<E> out = y.kind ? gradient_of_kind<E>(y) : gradient_at<kEntropy>(y, in);
+    if (to.whole(v)) {
+        store_whole(row + to.first(v), out);
+    } else {
+        const E* const e = reinterpret_cast<const E*>(&out.w);
+#pragma unroll
+        for (int k = 0; k < Vector<E>::N; ++k)
+            if ((unsigned)(to.first(v) + k) < (unsigned)to.V) row[to.first(v) + k] = e[k];
+    }
+}
+// Where the gradient's row `to` is not aligned as the logits' row `from` is, each of its vectors begins with element `off` of one of
+// theirs and the rest of it is in the next: lane `sub` of L has vectors sub, sub + L, .. and gets what it lacks from its neighbour.
+__device__ __forceinline__ uint4 shuffled(unsigned int group, uint4 x, int lane, int L) {
+    return {__shfl_sync(group, x.x, lane, L), __shfl_sync(group, x.y, lane, L), __shfl_sync(group, x.z, lane, L), __shfl_sync(group, x.w, lane, L)};
+}
+// vectors w, w + L, .. are here, w + 1, w + 1 + L, .. come; of those, lane L - 1 has its last already
+template <int L, class E>
+__device__ __forceinline__ void join_next(Vector<E> (&in)[kUnroll], const Vector<E>& last, int off, int sub, unsigned int group) {
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+        const Vector<E> next = {shuffled(group, sub == 0 && k + 1 < kUnroll ? in[(k + 1) % kUnroll].w : in[k].w, sub + 1, L)};
+        in[k] = joined(in[k], k + 1 == kUnroll && sub == L - 1 ? last : next, off);
+    }
+}
+// .. and w - 1, w - 1 + L, .. come; of those, lane 0 has its first already
+template <int L, class E>
+__device__ __forceinline__ void join_previous(Vector<E> (&in)[kUnroll], const Vector<E>& first, int off, int sub, unsigned int group) {
+#pragma unroll
+    for (int k = kUnroll - 1; k >= 0; --k) {
+        const Vector<E> previous = {shuffled(group, sub == L - 1 && k ? in[(k + kUnroll - 1) % kUnroll].w : in[k].w, sub + L - 1, L)};
+        in[k] = joined(k == 0 && sub == 0 ? first : previous, in[k], off);
+    }
+}
+template <class E>
+__device__ __forceinline__ int off_of(const Row<E>& from, const Row<E>& to) { return (from.skip - to.skip + Row<E>::N) % Row<E>::N; }
+// the lanes of the L that share a row
+template <int L>
+__device__ __forceinline__ unsigned int group_of_lane() {
+    return L == 32 ? ~0u : ((1u << (L & 31)) - 1) << (threadIdx.x & 31 & ~(L - 1));
+}
 template <class E>
 __device__ __forceinline__ bool aligned_alike(const E* a, const E* b) { return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15) == 0; }
 
@@ -218,48 +262,51 @@ __global__ void __launch_bounds__(256) narrow_kernel(RowArgs a) {
     }
 }
 
-// ---- the loss and gradient of a row that a warp holds in registers: 4 vectors a lane ----
-template <class E>
+// ---- the loss and gradient of a row that L lanes hold in registers: 4 vectors a lane ----
+template <class E, int L>
 __global__ void __launch_bounds__(128) warp_loss_kernel(RowArgs a) {
-    const int lane = threadIdx.x & 31;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    const int sub = threadIdx.x % L;
+    const int64_t row = (int64_t)blockIdx.x * (128 / L) + threadIdx.x / L;
     if (row >= a.rows) return;
+    const unsigned int group = group_of_lane<L>();
     const int64_t t = a.targets[row];
     const Row<E> x(row_of<E>(a, row), a.vocab);
     const float c = a.scale * kLog2E;
     Vector<E> v[kUnroll];
     RowStats r = {0.0f, 1.0f, 0.0f, 0.0f};
+    float given = 0.0f;
     if (t >= 0) {
 #pragma unroll
-        for (int k = 0; k < kUnroll; ++k) v[k] = x.load(k * 32 + lane);
-        const float given = t < a.vocab ? as_float(x.x[t]) : 0.0f;
+        for (int k = 0; k < kUnroll; ++k) v[k] = x.load(k * L + sub);
+        given = t < a.vocab ? as_float(x.x[t]) : 0.0f;
         float most = -CUDART_INF_F;
 #pragma unroll
         for (int k = 0; k < kUnroll; ++k) most = max_nan(most, v[k].max());
-        Sums all = {-CUDART_INF_F, 0.0f, 0.0f};
-        add_vectors<false>(all, v, warp_max_nan(most), c);      // one maximum for all lanes: nothing to rescale
+        if (L == 32) most = warp_max_nan(most);
+        else
 #pragma unroll
-        for (int o = 16; o; o >>= 1) all.s += __shfl_xor_sync(~0u, all.s, o);
+            for (int o = L / 2; o; o >>= 1) most = max_nan(most, __shfl_xor_sync(group, most, o));
+        Sums all = {-CUDART_INF_F, 0.0f, 0.0f};
+        add_vectors<false>(all, v, most, c);      // one maximum for all lanes: nothing to rescale
+#pragma unroll
+        for (int o = L / 2; o; o >>= 1) all.s += __shfl_xor_sync(group, all.s, o);
         r = stats_of(all);
-        if (lane == 0) write_stats(a, row, t, given, r);
+        if (sub == 0) write_stats(a, row, t, given, r);
     } else {
-        write_nothing(a, row, lane, 32);
+        write_nothing(a, row, sub, L);
     }
     const Gradient y = gradient_of(a, t, r.m, r.s, r.log_s, 0.0f, a.g_logprob[row], 0.0f);
-    E* const to = static_cast<E*>(a.grad) + row * a.grad_stride;
-    const bool alike = aligned_alike(to, x.x);
-    // the lane that writes the target's vector adds the target's own term
-    const int at = y.target >= 0 ? (y.target + x.skip) / Row<E>::N : -1;
-    const bool owner = alike && at >= 0 && at % 32 == lane && x.whole(at) && y.kind == 0;
-    const float x_t = owner ? as_float(x.x[y.target]) : 0.0f;
-    __syncwarp();                  // the row's logits have been read by all lanes
-#pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-        const int n = k * 32 + lane;
-        if (alike && x.whole(n)) store_whole(to + x.first(n), y.kind ? gradient_of_kind<E>(y) : gradient_at<false>(y, v[k]));
-        else if (n < x.vectors) store_partial<false>(to, x, n, v[k], y);
+    E* const out = static_cast<E*>(a.grad) + row * a.grad_stride;
+    const Row<E> to(out, a.vocab);
+    if (const int off = off_of(x, to); off && y.kind == 0) {      // no lane has a vector behind the row's last
+        if (x.skip > to.skip) join_next<L>(v, Row<E>::nothing(), off, sub, group);
+        else join_previous<L>(v, Row<E>::nothing(), off, sub, group);
     }
-    if (owner) to[y.target] = from_float<E>(gradient_at<false>(y, x_t, y.target));
+    const int at = y.target >= 0 && y.kind == 0 ? (y.target + to.skip) / Row<E>::N : -1;
+    __syncwarp(group);             // the row's logits have been read by all lanes
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) store_vector<false>(to, out, k * L + sub, v[k], y);
+    if (at >= 0 && at % L == sub) out[y.target] = from_float<E>(gradient_at<false>(y, given, y.target));
 }
 
 // ---- rows that a team of T threads, or a cluster of such blocks, sums up in one pass ----
@@ -558,10 +605,18 @@ __global__ void __launch_bounds__(T) loss_kernel(RowArgs a) {
             for (; i < part.n; i += T) store_whole(out + i * N, gradient_at<false>(y, vector(i)));
             if (owner) to[t] = from_float<E>(gradient_at<false>(y, x_t, (int)t));
         }
-    } else {   // the rows of the gradient are aligned otherwise than the logits': element by element, neighbours by neighbours
+    } else if (part.n > 0) {
+        // The rows of the gradient are aligned otherwise than the logits': each of its vectors comes from two of theirs, and at
+        // the ends of the part up to N elements come one by one.
         const E* const elements = kResident ? reinterpret_cast<const E*>(kept) : reinterpret_cast<const E*>(from);
-        const int first = x.first(part.lo);
-        for (int i = tid; i < part.n * N; i += T) out[i] = from_float<E>(gradient_at<false>(y, as_float(elements[i]), first + i));
+        const int first = x.first(part.lo), off = (x.skip - skip_of(to) + N) % N;
+        auto one = [&](int i) { out[i] = from_float<E>(gradient_at<false>(y, as_float(elements[i]), first + i)); };
+#pragma unroll 4
+        for (int i = tid; i < part.n - 1; i += T)
+            store_whole(out + i * N + off, y.kind ? gradient_of_kind<E>(y) : gradient_at<false>(y, joined(vector(i), vector(i + 1), off)));
+        if (tid < N) one(tid < off ? tid : (part.n - 1) * N + tid);
+        const int i_t = y.target >= 0 ? y.target - first : -1;
+        if (i_t >= off && i_t < (part.n - 1) * N + off && (i_t - off) / N % T == tid) one(i_t);
     }
     if (edge >= 0) store_partial<false>(to, x, edge, at_edge, y);
 }
@@ -574,36 +629,28 @@ __device__ __forceinline__ Gradient gradient_from_norm(const RowArgs& a, int64_t
     return gradient_of(a, a.targets[row], n.x, n.y, a.g_entropy ? logf(n.y) : 0.0f, a.g_entropy ? a.in_entropy[row] : 0.0f, a.g_logprob[row], h);
 }
 
-// L lanes take L kUnroll vectors of a row.  Nothing is shared and nothing waited for, so this runs at the copy's rate: 4,096 x
+// L lanes take L kUnroll vectors of a row, as they lie in the gradient.  Nothing is shared and nothing waited for, so this runs at the copy's rate: 4,096 x
 // 128,000 bf16 326 us (98 %), 2,048 x 50,001 with rows at every alignment 72 us (87 %).
 template <class E, bool kEntropy, int L>
-__global__ void __launch_bounds__(256) grad_kernel(RowArgs a, int segments) {
+__global__ void __launch_bounds__(256, 5) grad_kernel(RowArgs a, int segments) {
     const int sub = threadIdx.x % L;
     const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L, row = item / segments;
     if (row >= a.rows) return;
-    const Row<E> x(row_of<E>(a, row), a.vocab);
+    const Row<E> from(row_of<E>(a, row), a.vocab);
     const int v = (int)(item - row * segments) * L * kUnroll + sub;
     E* const to = static_cast<E*>(a.grad) + row * a.grad_stride;
-    if (!aligned_alike(to, x.x)) {
-        const Gradient y = gradient_from_norm(a, row);
-        const int lo = max(x.first(v - sub), 0), hi = min(x.first(v - sub + L * kUnroll), x.V);
-        for (int i = lo + sub; i < hi; i += L) to[i] = from_float<E>(gradient_at<kEntropy>(y, as_float(x.x[i]), i));
-        return;
-    }
+    const Row<E> x(to, a.vocab);
     Vector<E> in[kUnroll];
+    const int off = off_of(from, x), w = from.skip < x.skip ? v - 1 : v;
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) in[k] = x.load(v + L * k);
+    for (int k = 0; k < kUnroll; ++k) in[k] = from.load(w + L * k);
+    if (off) join_next<L>(in, sub == L - 1 ? from.load(w + L * (kUnroll - 1) + 1) : Row<E>::nothing(), off, sub, group_of_lane<L>());
     const Gradient y = gradient_from_norm(a, row);
-    // the lane that writes the target's vector adds the target's own term
     const int at = y.target >= 0 ? (y.target + x.skip) / Row<E>::N : -1;
-    const bool owner = at >= v && (at - v) % L == 0 && at - v < L * kUnroll && x.whole(at);
-    const float x_t = owner ? as_float(x.x[y.target]) : 0.0f;
+    const bool owner = at >= v && (at - v) % L == 0 && at - v < L * kUnroll && y.kind == 0;
+    const float x_t = owner ? as_float(from.x[y.target]) : 0.0f;
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-        const int n = v + L * k;
-        if (x.whole(n)) store_whole(to + x.first(n), y.kind ? gradient_of_kind<E>(y) : gradient_at<kEntropy>(y, in[k]));
-        else if (n < x.vectors) store_partial<kEntropy>(to, x, n, in[k], y);
-    }
+    for (int k = 0; k < kUnroll; ++k) store_vector<kEntropy>(x, to, v + L * k, in[k], y);
     if (owner) to[y.target] = from_float<E>(gradient_at<kEntropy>(y, x_t, y.target));
 }
 
@@ -739,8 +786,10 @@ cudaError_t launch_logprobs(const RowArgs& a, cudaStream_t st) {
 template <class E>
 cudaError_t launch_loss(RowArgs a, cudaStream_t st) {
     if (a.vocab <= kNarrow) return launch_narrow<E, true>(a, st);
-    if (fits_a_warp<E>(a.vocab)) return launch(warp_loss_kernel<E>, (a.rows + 3) / 4, 128, 0, 1, st, a);
     const int vectors = most_vectors<E>(a.vocab);
+    if (vectors <= 8 * kUnroll) return launch(warp_loss_kernel<E, 8>, (a.rows + 15) / 16, 128, 0, 1, st, a);
+    if (vectors <= 16 * kUnroll) return launch(warp_loss_kernel<E, 16>, (a.rows + 7) / 8, 128, 0, 1, st, a);
+    if (fits_a_warp<E>(a.vocab)) return launch(warp_loss_kernel<E, 32>, (a.rows + 3) / 4, 128, 0, 1, st, a);
     int cluster = 1;
     while (cluster < kMaxCluster && ((a.rows * cluster * 2 <= 2 * kSms && vectors / (2 * cluster) >= 256) || (size_t)slice_of(vectors, cluster) * 16 > kSliceBytes))
         cluster *= 2;
@@ -759,6 +808,7 @@ cudaError_t launch_grad(const RowArgs& a, cudaStream_t st) {
     if (a.vocab <= kNarrow) return launch(narrow_grad_kernel<E, kEntropy, 16, 4>, blocks(256 / 16), 256, 0, 1, st, a);
     const int vectors = most_vectors<E>(a.vocab);
     if (vectors <= 8 * kUnroll) return launch(grad_kernel<E, kEntropy, 8>, blocks(256 / 8), 256, 0, 1, st, a, 1);
+    if (vectors <= 16 * kUnroll) return launch(grad_kernel<E, kEntropy, 16>, blocks(256 / 16), 256, 0, 1, st, a, 1);
     const int segments = (vectors + 32 * kUnroll - 1) / (32 * kUnroll);
     const int64_t n = (a.rows * segments + 7) / 8;
     return n > 0x7FFFFFFF ? cudaErrorInvalidValue : launch(grad_kernel<E, kEntropy, 32>, n, 256, 0, 1, st, a, segments);

@@ -129,6 +129,24 @@ struct Vector {
     __device__ __forceinline__ float one(int e) const { return as_float(reinterpret_cast<const E*>(&w)[e]); }
 };
 
+// Elements off .. off + N - 1 of the 2 N elements of two vectors
+template <class E>
+__device__ __forceinline__ Vector<E> joined(const Vector<E>& a, const Vector<E>& b, int off) {
+    uint32_t w[8] = {a.w.x, a.w.y, a.w.z, a.w.w, b.w.x, b.w.y, b.w.z, b.w.w};
+    const int bytes = off * (int)sizeof(E);
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = bytes & 8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = bytes & 4 ? w[i + 1] : w[i];
+    if constexpr (sizeof(E) == 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bytes & 2 ? 16 : 0);
+    return {{w[0], w[1], w[2], w[3]}};
+}
+// elements by which an address lies behind a multiple of 16 bytes
+template <class E>
+__device__ __forceinline__ int skip_of(const E* p) { return (int)(reinterpret_cast<uintptr_t>(p) & 15) / (int)sizeof(E); }
+
 // The 16-byte vectors that a row of V elements touches: the row begins with element `skip` of vector 0.  The vectors that lie
 // inside the row, [lo, hi), are read and written whole; the others, at most one at each end, element by element, with -inf in
 // the places outside.
@@ -137,7 +155,7 @@ struct Row {
     static constexpr int N = Vector<E>::N;
     const E* x;
     int V, skip, vectors, lo, hi;
-    __device__ __forceinline__ Row(const E* row, int n) : x(row), V(n), skip((int)(reinterpret_cast<uintptr_t>(row) & 15) / (int)sizeof(E)) {
+    __device__ __forceinline__ Row(const E* row, int n) : x(row), V(n), skip(skip_of(row)) {
         vectors = (skip + n + N - 1) / N;
         lo = skip || n < N ? 1 : 0;
         hi = (skip + n) % N ? vectors - 1 : vectors;

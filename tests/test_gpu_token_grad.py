@@ -124,6 +124,40 @@ def test_in_the_place_of_the_logits(slaq, vocab, pad, dtype):  # noqa: F811
     assert torch.equal(y, want)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [65, 66, 125, 126, 171, 249, 250, 253, 254, 505, 506, 509, 510, 1017, 1018, 1025, 2500, 9001, 70003])
+def test_alignments_that_differ(slaq, vocab, dtype):  # noqa: F811
+    """Logits and gradient each at its own distance from 16 bytes: every pair of distances gives the bits of any other."""
+    step = 16 // dtype.itemsize
+    x, t, gen = _rows(7, vocab, dtype, 0, vocab)
+    g, h = _grads(7, gen)
+    t[3], t[4], t[5], t[6] = -1, 0, vocab - 1, vocab
+    x[2, vocab // 3:] = -math.inf
+    pitch = (vocab + 3 * step) // step * step
+    places = torch.full((2, 7, pitch), 5.0, dtype=dtype, device="cuda")
+    where = range(0, step) if vocab < 3000 else (0, 1, step - 1)
+    expected = {}
+    for at in where:
+        y = places[0, :, at:at + vocab].copy_(x)
+        parts = slaq.token_logprobs(y, t)
+        for to in where:
+            for name in ("loss", "grad", "entropy"):
+                places[1] = 5.0
+                out = places[1, :, to:to + vocab]
+                if name == "loss":
+                    slaq.token_loss(y, t, g, out=out)
+                else:
+                    kw = dict(entropy=parts.entropy, grad_entropy=h) if name == "entropy" else {}
+                    slaq.token_logprobs_grad(y, t, parts.norm, g, out=out, **kw)
+                assert bool((places[1, :, :to] == 5.0).all()) and bool((places[1, :, to + vocab:] == 5.0).all())
+                want = expected.setdefault((name, at), out.clone())       # the sums' order is the logits', not the gradient's
+                assert torch.equal(torch.nan_to_num(out), torch.nan_to_num(want)) and bool((out[6] != out[6]).all())
+                if to == at:
+                    rows = slice(0, 6)
+                    with_h = h[rows] if name == "entropy" else None
+                    _near(*_check(out[rows], ref.gradient(y[rows], t[rows], g[rows], with_h), vocab, g[rows], with_h, 1.0), dtype)
+
+
 def test_rows_that_alternate_with_the_logits(slaq):  # noqa: F811
     both = torch.randn(5, 2 * 3000, generator=torch.Generator().manual_seed(1)).cuda()
     x, out = both[:, :3000], both[:, 3000:]
