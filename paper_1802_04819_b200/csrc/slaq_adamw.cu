@@ -267,10 +267,10 @@ __device__ __forceinline__ Numbers numbers_of(const Group& g) {
 // The step of 8 elements: new weights, first moments, and second moments.  With kCodes the states come as codes, whose units
 // are m_scale and r_scale, and the roots of the second moments are returned.
 //
-// With codes, m and v are rounded after every product and sum: a code is a decision, and the formula's own, taken operation by
-// operation, is what a checkpoint or another implementation can be held to.  With fused products 51 of 16 M codes of m and the
-// last bit of every fourth scale differed after two steps; without, none of m, and of the second moment the last bit of
-// every fourth scale and 2 to 6 codes in 16 M, for the root is good to 1 ulp (an exact one costs 8 %).  It costs 2 %.
+// With codes, m, v and the root are rounded after every operation: a code is a decision, and the formula's own, taken operation by
+// operation, is what a checkpoint or another implementation can be held to.  With fused products and a root good to 1 ulp, 51 of 16 M
+// codes of m, 6 of v and the last bit of every fourth scale differed after two steps, and one code of v is 6 % of a weight's next step.
+// It costs 8 %.
 template <bool kCodes>
 __device__ __forceinline__ void step8(const Numbers& c, float m_scale, float r_scale, Eight& p, const Eight& g, Eight& m, Eight& v) {
     auto two = [](float x) { return pair_of(x, x); };
@@ -287,7 +287,7 @@ __device__ __forceinline__ void step8(const Numbers& c, float m_scale, float r_s
         }
         float a, b;
         v.get(k, a, b);
-        const Pair r = pair_of(root(a), root(b));
+        const Pair r = kCodes ? pair_of(__fsqrt_rn(a), __fsqrt_rn(b)) : pair_of(root(a), root(b));
         split(fma2(r, two(c.correct), two(c.eps)), a, b);
         p.at[k] = fma2(two(-c.size), m.at[k] * pair_of(reciprocal(a), reciprocal(b)), p.at[k] * two(c.keep));
         if (kCodes) v.at[k] = r;
