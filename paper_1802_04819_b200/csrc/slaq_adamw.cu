@@ -328,7 +328,7 @@ struct RawState<true> {
 // DRAM decides.  In 32 bits a unit is a block: with runs of four or eight blocks for each warp the step took a sixth longer (209 M
 // bf16 weights with masters: 1040 us instead of 885, 6.60 TB/s).  And the next block is asked for behind this one's stores: asked
 // for before them, while the block is computed, its loads come between the stores of other warps (967 us).  In 8 bits,
-// where there is more to compute for a byte, it is the other way round (304 M fp32 weights: 783 us; behind the stores 875).
+// where there is more to compute for a byte, it is the other way round (304 M fp32 weights: 783 us; behind the stores 875; 803 with the root to the nearest).
 // Four thread blocks of four warps an SM are as many as the registers allow; more warps, with spills, were slower.
 template <class P, class G, bool kMaster, bool kEight>
 __global__ void __launch_bounds__(kThreads) step_kernel(StepArgs a) {
@@ -504,7 +504,8 @@ struct Ahead {
 
 // The same with 8-bit states where weights and gradients are of 16 bits and there is no master copy: a block is then 48 bytes a lane, and one ahead leaves 25 KB
 // on their way to an SM where 40 are wanted.  Three ahead, and 32 blocks in a row, whose scales fill a line of each state:
-// 528 us for 304 M elements (5.76 TB/s), against 604 with one; instructions bound it, 44 an element.  With more bytes a block it is the other way round (fp32: 1110 us against 790).
+// 599 us for 304 M elements (5.1 TB/s); with fused products and a root good to 1 ulp 528, then against 604 with one ahead: instructions
+// bound it.  With more bytes a block it is the other way round (fp32: 1110 us against 790).
 template <class P>
 __global__ void __launch_bounds__(kThreads) deep_step_kernel(StepArgs a) {
     using Blocks = Ahead<P, P>;
