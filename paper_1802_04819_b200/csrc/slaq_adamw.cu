@@ -283,7 +283,7 @@ __device__ __forceinline__ void step8(const Numbers& c, float m_scale, float r_s
             v.at[k] = sum_of_products(two(c.b2) * (old * old), two(c.a2) * (x * x));
         } else {
             m.at[k] = fma2(two(c.b1), m.at[k], two(c.a1) * x);
-            v.at[k] = fma2(two(c.b2), v.at[k], two(c.a2) * x * x);
+            v.at[k] = fma2(two(c.a2) * x, x, two(c.b2) * v.at[k]);
         }
         float a, b;
         v.get(k, a, b);
