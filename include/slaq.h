@@ -593,7 +593,7 @@ typedef struct slaq_adamw_tensor {
     int32_t reserved;
 } slaq_adamw_tensor;
 typedef struct slaq_adamw_group {
-    double lr, beta1, beta2, eps, weight_decay;   /* lr, eps, weight_decay >= 0; betas in [0, 1) */
+    double lr, beta1, beta2, eps, weight_decay;   /* lr, weight_decay in [0, 1e30); betas in [0, 1); eps 0 or in [2^-126, 1e30) */
     double grad_scale;                            /* factor of the gradients, 1 for none */
     int64_t step;                                 /* steps taken so far */
 } slaq_adamw_group;
@@ -603,7 +603,7 @@ typedef struct slaq_adamw_handle slaq_adamw_t;
  * Make a plan.  dev_ws: NULL (the library allocates), or device memory of the caller, 256-byte aligned and
  * slaq_adamw_workspace_bytes() long, that outlives the plan.  Host arrays; the call returns when the plan is on the device and
  * must not be captured.  Any alignment of the tensors that suits their type will do.
- * Errors: SLAQ_E_ARG (null, unknown types, a group out of range, betas outside [0, 1), a tensor listed twice, tensors that
+ * Errors: SLAQ_E_ARG (null, unknown types, a group or its numbers out of range, a tensor listed twice, tensors that
  * overlap one another or a gradient), SLAQ_E_RANGE (more than 2^38 elements), SLAQ_E_NOMEM, SLAQ_E_CUDA.
  */
 int slaq_adamw_create(void* dev_ws, size_t bytes, int32_t n_tensors, const slaq_adamw_tensor* tensors, int32_t n_groups,

@@ -268,7 +268,8 @@ class AdamW:
 
     ``params`` and ``grads``: lists of contiguous CUDA tensors (fp32, bf16 or fp16; gradients of the weights' type or fp32);
     ``group_of``: the group of each tensor (default: all 0); ``groups``: a list of dicts with ``lr``, ``betas``, ``eps``,
-    ``weight_decay``, ``grad_scale``, ``step`` (any may be left out).  ``masters``: fp32 copies that the step works on, the
+    ``weight_decay``, ``grad_scale``, ``step`` (any may be left out; ``eps`` is 0 or at least 2^-126, and with 0 an element whose
+    second moment is 0 becomes NaN, as the formula says).  ``masters``: fp32 copies that the step works on, the
     weights being their rounding.  ``state_bits`` 32 (fp32 states) or 8 (float8_e4m3fn codes with a float32 scale per 256
     elements, the second moment as its square root).  States are made as zeros, or taken over as lists: ``exp_avg``,
     ``exp_avg_sq`` and, in 8 bits, ``exp_avg_scale``, ``exp_avg_sq_scale``; they are attributes of the same names."""
@@ -329,7 +330,7 @@ class AdamW:
             self._ws = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
             rc = self._lib.slaq_adamw_create(self._ws.data_ptr(), need, n, table, len(groups), (_Group * len(groups))(*groups),
                                              _types[kind], _types[grad_kind], state_bits, raw, ctypes.byref(self._h))
-        _check(rc, {-1: "a group out of range, betas outside [0, 1), a tensor listed twice, or tensors that overlap"}.get(rc))
+        _check(rc, {-1: "a group or its numbers out of range, a tensor listed twice, or tensors that overlap"}.get(rc))
         self._gpu, self._n_groups = gpu, len(groups)
         self._streams = {raw}                       # those that use the plan's memory: torch gives it away when they have passed
 
