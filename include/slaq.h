@@ -595,7 +595,8 @@ typedef struct slaq_adamw_tensor {
 typedef struct slaq_adamw_group {
     double lr, beta1, beta2, eps, weight_decay;   /* lr, weight_decay in [0, 1e30); betas in [0, 1); eps 0 or in [2^-126, 1e30) */
     double grad_scale;                            /* factor of the gradients, 1 for none */
-    int64_t step;                                 /* steps taken so far */
+    int64_t step;                                 /* steps taken so far, at most 2^53 */
+    /* grad_scale, lr x weight_decay and lr / (1 - beta1) are below 3.4e38 */
 } slaq_adamw_group;
 typedef struct slaq_adamw_handle slaq_adamw_t;
 

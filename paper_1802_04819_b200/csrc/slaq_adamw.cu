@@ -637,13 +637,15 @@ bool on_device(const slaq_adamw_handle* h) {
     int d = -1;
     return cudaGetDevice(&d) == cudaSuccess && d == h->device;
 }
-// eps is 0 or a normal number of 32 bits: the step's reciprocal takes what lies between for 0, and 0 x infinity would be the step of an
-// element whose gradient and states are 0, which is 0 / eps = 0.
+// What the step computes with is finite in 32 bits, so that elements that are 0 stay so: the factor of the gradients, the decay, and the
+// learning rate over 1 - beta1^t, which is largest at the first step.  eps is 0 or a normal number: the step's reciprocal takes what lies
+// between for 0, and 0 x infinity would be the step of an element whose gradient and states are 0, which is 0 / eps = 0.
 bool group_ok(const slaq_adamw_group& g) {
-    constexpr double kLeastEps = 1.1754943508222875e-38;   // 2^-126
+    constexpr double kLeastEps = 1.1754943508222875e-38, kMost = 3.4e38;   // 2^-126; 32 bits end at 3.4028e38
     auto in = [](double x, double lo, double hi) { return x >= lo && x < hi; };
     return in(g.lr, 0.0, 1e30) && in(g.beta1, 0.0, 1.0) && in(g.beta2, 0.0, 1.0) && (g.eps == 0.0 || in(g.eps, kLeastEps, 1e30)) &&
-           in(g.weight_decay, 0.0, 1e30) && std::isfinite(g.grad_scale);
+           in(g.weight_decay, 0.0, 1e30) && std::fabs(g.grad_scale) < kMost && g.lr * g.weight_decay < kMost && g.lr / (1.0 - g.beta1) < kMost &&
+           g.step <= (int64_t)1 << 53;
 }
 Group device_group(const slaq_adamw_group& g) {
     Group d = {};

@@ -70,3 +70,15 @@ def test_an_epsilon_below_the_normal_numbers_is_refused(fake, plan, eps, code):
     assert plan([_group(eps=eps)])[0] == code
     _, h = plan()
     assert fake.slaq_adamw_set_group(h, 0, byref(_group(eps=eps, step=-1)), None) == code
+
+
+@pytest.mark.parametrize("numbers,code", [
+    (dict(grad_scale=3e38), 0), (dict(grad_scale=-3e38), 0), (dict(grad_scale=1e39), -1), (dict(grad_scale=-1e300), -1), (dict(lr=1e20, weight_decay=1e18), 0),
+    (dict(lr=1e20, weight_decay=1e20), -1), (dict(lr=1e25, betas=(1 - 1e-12, 0.9)), 0), (dict(lr=1e25, betas=(1 - 1e-15, 0.9)), -1), (dict(step=2 ** 53), 0),
+    (dict(step=2 ** 53 + 1), -1), (dict(step=2 ** 63 - 1), -1)])
+def test_numbers_that_a_step_in_32_bits_does_not_hold_are_refused(fake, plan, numbers, code):
+    """An infinite factor makes NaN of elements that are 0; a count of 2^63 - 1 overflows with the next step."""
+    from paper_1802_04819_b200.training import _group
+    assert plan([_group(**numbers)])[0] == code
+    _, h = plan()
+    assert fake.slaq_adamw_set_group(h, 0, byref(_group(**{"step": -1, **numbers})), None) == code
