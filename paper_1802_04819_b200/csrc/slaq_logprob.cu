@@ -715,10 +715,12 @@ int by_type(int type, F&& f) {
     return e == cudaSuccess ? SLAQ_OK : SLAQ_E_CUDA;
 }
 
+constexpr size_t kSliceBytes = 72 * 1024, kMostSlice = 200 * 1024;   // per block of the loss: three blocks on an SM, or one
+
 template <class... Params, class... Args>
 cudaError_t launch(void (*kernel)(Params...), int64_t blocks, int threads, size_t smem, int cluster, cudaStream_t st, Args... args) {
-    if (smem > 40 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (smem > 40 * 1024) {   // what a kernel may use is state that all host threads share: never what this call needs, always the most
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSlice);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg = {};
@@ -736,7 +738,6 @@ cudaError_t launch(void (*kernel)(Params...), int64_t blocks, int threads, size_
 }
 
 constexpr int kSms = 148;
-constexpr size_t kSliceBytes = 72 * 1024, kMostSlice = 200 * 1024;   // per block of the loss: three blocks on an SM, or one
 
 // Vectors a row may touch, whatever its alignment.
 template <class E>

@@ -82,3 +82,18 @@ def test_numbers_that_a_step_in_32_bits_does_not_hold_are_refused(fake, plan, nu
     assert plan([_group(**numbers)])[0] == code
     _, h = plan()
     assert fake.slaq_adamw_set_group(h, 0, byref(_group(**{"step": -1, **numbers})), None) == code
+
+
+def test_a_call_takes_no_shared_memory_from_another_threads(fake):
+    """Rows of both sizes are kept by one kernel, in different amounts of shared memory.  What it may use belongs to the kernel, not to the
+    call: a call between another thread's request and launch must not lower it."""
+    def call(rows, vocab):
+        assert fake.slaq_token_loss(P, 1, rows, vocab, vocab, Q, 1.0, Q, Q, 1 << 44, vocab, None) == 0
+        return _last(fake)
+
+    def _last(lib):
+        return c_void_p.in_dll(lib, "fake_last_kernel").value, c_size_t.in_dll(lib, "fake_last_bytes").value
+    calls = [call(*shape) for shape in ((4096, 147_000), (4096, 128_000), (2048, 50_001), (4096, 151_936))]
+    assert len({kernel for kernel, _ in calls[:3]}) == 1 and len({size for _, size in calls}) == 4
+    for kernel, size in calls:
+        assert fake.fake_limit(kernel) >= size
