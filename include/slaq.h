@@ -550,8 +550,8 @@ int slaq_token_loss(const void* d_logits, int type, int64_t rows, int32_t vocab,
  * a row counts with d_weights[r] (NULL: 1), and not at all if its target is negative (d_targets may be NULL) or its weight 0.
  * slaq_job_losses: d_out_losses[j] = -sum w logprob / sum w, in 64 bits, always summed in the same order.
  * slaq_job_row_grad: d_out_row_grad[r] = -w_r / sum w of the row's job: the loss's derivative by the row's log
- * probability.  Rows before the first job and behind the last are left as they were, or set to 0 if zero_rest is not 0 (it
- * takes a job then: SLAQ_E_ARG without).
+ * probability.  Rows that are no job's (before the first, behind the last, a refused job's) are left as they were, or set to 0 if zero_rest
+ * is not 0 (it takes a job then: SLAQ_E_ARG without).  d_out_row_grad overlaps none of the inputs.
  * A job without a row that counts has loss NaN, and so has one whose offsets leave 0 .. rows or fall (its rows are not
  * touched).  Errors: SLAQ_E_ARG, SLAQ_E_CUDA.
  */

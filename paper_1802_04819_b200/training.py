@@ -193,7 +193,8 @@ def _job_offsets(offsets, gpu):
 
 def job_row_grad(offsets, targets=None, weights=None, out=None, stream=None):
     """slaq_job_row_grad: the derivative of each job's mean loss by the log probability of each of its rows (float32 [rows]).
-    ``offsets`` int64 [jobs + 1]; rows before the first job and behind the last keep what ``out`` holds (without ``out``: 0)."""
+    ``offsets`` int64 [jobs + 1]; rows that are no job's (before the first, behind the last, or a job's whose offsets fall or leave the
+    rows) keep what ``out`` holds (without ``out``: 0)."""
     torch = _load()
     known = targets if targets is not None else weights if weights is not None else out
     if known is None:
