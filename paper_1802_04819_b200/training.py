@@ -84,15 +84,23 @@ def _matrix(t, name):
     return t.data_ptr(), kind, rows, vocab, pitch, t.get_device()
 
 
+def _torch_stream(stream, device):
+    """A torch stream from one or from a raw cudaStream_t.  0 is the device's default stream; torch would make a new one of it."""
+    cuda = _load().cuda
+    if not isinstance(stream, int):
+        return stream
+    return cuda.ExternalStream(stream, device=device) if stream else cuda.default_stream(device)
+
+
 @contextlib.contextmanager
 def _elsewhere(stream, device):
     """Another stream than torch's current one, or another device, as the current ones: what is allocated there belongs there."""
-    torch = _load()
-    with torch.cuda.device(device):
+    cuda = _load().cuda
+    with cuda.device(device):
         if stream is None:
             yield
         else:
-            with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream):
+            with cuda.stream(_torch_stream(stream, device)):
                 yield
 
 
@@ -352,7 +360,7 @@ class AdamW:
         raw = _current_stream(self._gpu)
         if raw not in self._streams:
             self._streams.add(raw)
-            self._ws.record_stream(_torch.cuda.ExternalStream(raw, device=self._gpu))
+            self._ws.record_stream(_torch_stream(raw, self._gpu))
         rc = _calls.adamw_step(_at["adamw_step"], self._h.value, a, raw)
         if rc < 0:
             self._ok(rc)
