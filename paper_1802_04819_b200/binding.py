@@ -230,6 +230,7 @@ class Scheduler:
         self._h = c_void_p()
         self.max_jobs, self.max_hist, self.max_cores_per_job = int(max_jobs), int(max_hist), int(max_cores_per_job)
         self._workspace = workspace
+        self._stream = 0                         # the raw stream that the handle's work is on
         self._calls = _marshal()
         addr = lambda f: ctypes.cast(f, c_void_p).value   # noqa: E731
         self._addr = (addr(self._lib.slaq_append_losses), addr(self._lib.slaq_append_losses_ex), addr(self._lib.slaq_schedule))
@@ -269,7 +270,9 @@ class Scheduler:
     # -- the C calls --
     def set_stream(self, stream):
         raw = getattr(stream, "cuda_stream", stream)
-        return self._check(self._lib.slaq_set_stream(self._h, c_void_p(raw)))
+        rc = self._check(self._lib.slaq_set_stream(self._h, c_void_p(raw)))
+        self._stream = raw or 0
+        return rc
 
     def set_param(self, key: int, value: float):
         rc = self._check(self._lib.slaq_set_param(self._h, key, float(value)))
@@ -303,7 +306,9 @@ class Scheduler:
     def append_token_losses(self, d_job_ids, offsets, targets, logprob, weights=None, d_iter_times=None, d_cores_used=None,
                             out=None):
         """The mean loss of each listed job over its rows (see ``job_losses``) as its new iteration, from torch CUDA
-        tensors, asynchronous on the handle's stream; returns the losses (float64, ``out`` if given)."""
+        tensors, asynchronous on the handle's stream; returns the losses (float64, ``out`` if given).  Where the handle's stream is not
+        the one that the tensors were made on, that stream waits for what made them first, the tensors stay alive until it has
+        passed the call, and whoever reads the losses waits for it; they are allocated for the handle's stream, so they may be dropped."""
         from .training import append_token_losses
         return append_token_losses(self, d_job_ids, offsets, targets, logprob, weights, d_iter_times, d_cores_used, out)
 

@@ -9,8 +9,8 @@ A training step of many jobs whose logits lie in one matrix, job j's rows being 
     adamw.step(active=alloc)                                          # only the jobs that were given cores
 
 Every call is asynchronous on ``stream`` (a torch stream or a raw cudaStream_t; default: torch's current stream of the
-tensors' device).  Results that are not given as ``out`` are allocated by torch for that stream; inputs must stay alive until it
-has passed the call.  No call records anything for autograd.  Refusals raise ``SlaqError``.
+tensors' device; ``append_token_losses`` is on the handle's).  Results that are not given as ``out`` are allocated by torch for
+that stream; inputs must be ready on it, and stay alive until it has passed the call.  No call records anything for autograd.  Refusals raise ``SlaqError``.
 """
 
 from __future__ import annotations
@@ -249,8 +249,9 @@ def append_token_losses(sched, d_job_ids, offsets, targets, logprob, weights, d_
         _refuse("offsets has one entry more than there are jobs")
     t, lp = _vector(targets, "targets", torch.int64, rows, gpu), _vector(logprob, "logprob", torch.float32, rows, gpu)
     w = _vector(weights, "weights", torch.float32, rows, gpu)
-    if out is None:
-        out = torch.empty(n, dtype=torch.float64, device=logprob.device)
+    if out is None:      # its memory is the handle's stream's: not in use by earlier work of torch's, nor given to later work too early
+        with contextlib.nullcontext() if sched._stream == _current_stream(gpu) else _elsewhere(sched._stream, gpu):
+            out = torch.empty(n, dtype=torch.float64, device=logprob.device)
     sched._check(sched._lib.slaq_append_token_losses(
         sched._h, n, _vector(d_job_ids, "job ids", torch.int32, n, gpu), off, rows, t, lp, w,
         _vector(d_iter_times, "iteration times", torch.float64, n, gpu), _vector(d_cores_used, "cores", torch.int32, n, gpu),

@@ -33,3 +33,37 @@ def test_a_raw_stream_of_0_is_the_default_stream(slaq, monkeypatch):
         assert seen and set(seen) == {raw}
         seen.clear()
         torch.cuda.synchronize()
+
+
+def test_appends_on_a_stream_that_lags_behind(slaq):
+    """The losses are dropped at once and their size of memory is taken and written on the current stream, while the handle's stream has
+    the append still before it: the histories are those of the same losses through the host."""
+    jobs, rows_each = 50, 7
+    rng = np.random.default_rng(2)
+    ids = np.arange(jobs, dtype=np.int32)
+    side = torch.cuda.Stream()
+    d_ids, off = torch.arange(jobs, dtype=torch.int32, device="cuda"), torch.arange(jobs + 1, device="cuda") * rows_each
+    targets = torch.zeros(jobs * rows_each, dtype=torch.int64, device="cuda")
+    with slaq.Scheduler(jobs, 32, 8, stream=side) as a, slaq.Scheduler(jobs, 32, 8) as b:
+        for s in (a, b):
+            s.append_losses(ids, np.full(jobs, 5.0))
+            s.set_time_model(ids, np.full(jobs, 0.1), np.full(jobs, 2.0))
+        kept, want = [], []
+        for k in range(10):
+            lp = torch.from_numpy((-4.0 * 0.8 ** k * rng.uniform(0.9, 1.1, jobs * rows_each)).astype(np.float32)).cuda()
+            want.append(slaq.job_losses(off, targets, lp).cpu().numpy())
+            kept.append(lp)                                  # the inputs are the caller's to keep
+        side.wait_stream(torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)                    # some ten milliseconds
+        junk = []
+        for lp in kept:
+            a.append_token_losses(d_ids, off, targets, lp)
+            junk.append(torch.full((jobs,), -1e9, dtype=torch.float64, device="cuda"))
+        torch.cuda.synchronize()
+        for losses in want:
+            b.append_losses(ids, losses)
+        np.testing.assert_array_equal(a.schedule(1.0, 100)[0], b.schedule(1.0, 100)[0])
+        np.testing.assert_array_equal(a.get_predictions()["gain"], b.get_predictions()["gain"])
+        assert all(bool((x == -1e9).all()) for x in junk)
