@@ -338,18 +338,31 @@ class AdamW:
             numels = np.array(sizes, np.int64)
             need = self._lib.slaq_adamw_workspace_bytes(n, numels.ctypes.data, len(groups))
             self._ws = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
+            # what is the plan's own memory: torch gives it away when the streams that use it have passed
+            self._own = [self._ws] + [t for given, made in ((exp_avg, self.exp_avg), (exp_avg_sq, self.exp_avg_sq), (exp_avg_scale, self.exp_avg_scale),
+                                                             (exp_avg_sq_scale, self.exp_avg_sq_scale)) if given is None and made is not None for t in made]
             rc = self._lib.slaq_adamw_create(self._ws.data_ptr(), need, n, table, len(groups), (_Group * len(groups))(*groups),
                                              _types[kind], _types[grad_kind], state_bits, raw, ctypes.byref(self._h))
         _check(rc, {-1: "a group or its numbers out of range, a tensor listed twice, or tensors that overlap"}.get(rc))
         self._gpu, self._n_groups = gpu, len(groups)
-        self._streams = {raw}                       # those that use the plan's memory: torch gives it away when they have passed
+        self._streams = {raw}                       # those that it is kept for
 
     def _ok(self, rc):
         return _check(rc, self._lib.slaq_adamw_last_error(self._h).decode() if rc < 0 else None)
 
+    def _here(self):
+        """The raw current stream, for which the plan's memory is kept from now on."""
+        raw = _current_stream(self._gpu)
+        if raw not in self._streams:
+            stream = _torch_stream(raw, self._gpu)
+            for t in self._own:
+                t.record_stream(stream)
+            self._streams.add(raw)
+        return raw
+
     def _run(self, stream, call):
         with contextlib.nullcontext() if _is_here(stream, self._gpu) else _elsewhere(stream, self._gpu):
-            self._ok(call(_current_stream(self._gpu)))
+            self._ok(call(self._here()))
 
     def step(self, active=None, stream=None):
         """One step of the groups whose entry of ``active`` (int32 CUDA tensor [groups], for instance the allocation of
@@ -358,11 +371,7 @@ class AdamW:
             with _elsewhere(stream, self._gpu):
                 return self.step(active)
         a = _vector(active, "active", _torch.int32, self._n_groups, self._gpu)
-        raw = _current_stream(self._gpu)
-        if raw not in self._streams:
-            self._streams.add(raw)
-            self._ws.record_stream(_torch_stream(raw, self._gpu))
-        rc = _calls.adamw_step(_at["adamw_step"], self._h.value, a, raw)
+        rc = _calls.adamw_step(_at["adamw_step"], self._h.value, a, self._here())
         if rc < 0:
             self._ok(rc)
 

@@ -67,3 +67,24 @@ def test_appends_on_a_stream_that_lags_behind(slaq):
         np.testing.assert_array_equal(a.schedule(1.0, 100)[0], b.schedule(1.0, 100)[0])
         np.testing.assert_array_equal(a.get_predictions()["gain"], b.get_predictions()["gain"])
         assert all(bool((x == -1e9).all()) for x in junk)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_plan_and_its_states_are_dropped_while_another_stream_steps(slaq, bits):
+    """What is allocated in their place afterwards keeps its pattern, and the steps come out as if nothing had been dropped."""
+    n = 3_000_000
+    p, g = torch.ones(n, device="cuda"), torch.ones(n, device="cuda")
+    plan = slaq.AdamW([p], [g], groups=[dict(lr=0.01, weight_decay=0.0)], state_bits=bits)
+    sizes = [x.numel() * x.element_size() for xs in (plan.exp_avg, plan.exp_avg_sq, plan.exp_avg_scale or [], plan.exp_avg_sq_scale or [], [plan._ws]) for x in xs]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+    for _ in range(20):
+        plan.step(stream=side)
+    del plan
+    junk = [torch.full((size,), 85, dtype=torch.uint8, device="cuda") for size in sizes for _ in range(2)]
+    torch.cuda.synchronize()
+    assert all(bool((x == 85).all()) for x in junk)
+    # 20 steps of lr, each off by the roundings of a step; 8-bit states: a constant gradient is the largest of its block, and kept exactly
+    torch.testing.assert_close(p, torch.full_like(p, 0.8), rtol=0, atol=1e-4)

@@ -10,7 +10,11 @@ class Tensor:
     """What the calls ask of a tensor.  `stream` is the one that was current when it was made."""
 
     def __init__(self, dtype, n, stream):
-        self.dtype, self.n, self.stream, self.device, self.recorded = dtype, n, stream, "cuda:0", []
+        self.dtype, self.n, self.stream, self.recorded, self.is_cuda = dtype, n, stream, [], True
+        self.device = SimpleNamespace(index=0)
+
+    def to(self, dtype):
+        return Tensor(dtype, self.n, self.stream)
 
     def numel(self):
         return self.n
@@ -52,7 +56,7 @@ def world(monkeypatch):
         w.made.append(Tensor(dtype, n, w.stream))
         return w.made[-1]
     cuda = SimpleNamespace(device=lambda d: contextlib.nullcontext(), stream=current, default_stream=lambda d: 0, ExternalStream=lambda raw, device: raw)
-    fake = SimpleNamespace(cuda=cuda, empty=make, zeros=make, int64=torch.int64, int32=torch.int32, float32=torch.float32, float64=torch.float64)
+    fake = SimpleNamespace(cuda=cuda, empty=make, zeros=make, **{t: getattr(torch, t) for t in ("int64", "int32", "float32", "float64", "uint8", "float8_e4m3fn")})
     monkeypatch.setattr(training, "_torch", fake)
     monkeypatch.setattr(training, "_current_stream", lambda gpu: w.stream)
     monkeypatch.setattr(training, "_current_device", lambda: 0)
@@ -84,3 +88,30 @@ def test_a_scheduler_knows_the_stream_it_was_given(world):
     with pytest.raises(world.slaq.SlaqError):
         sched.set_stream(99)
     assert sched._stream == 0
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("call", ["step", "set_group", "set_grads", "get_steps"])
+def test_a_plans_memory_is_kept_for_every_stream_that_uses_it(world, monkeypatch, bits, call):
+    """Dropped after a call on another stream, it must not go back to the one it was made on before the other has passed the call: its
+    tables, and the states that it made."""
+    t = world.torch
+    lib = SimpleNamespace(**{"slaq_adamw_" + name: lambda *a: 0 for name in ("create", "destroy", "set_group", "set_grads", "get_steps")},
+                          slaq_adamw_workspace_bytes=lambda *a: 4096)
+    monkeypatch.setattr(world.training, "load_library", lambda: lib)
+    monkeypatch.setattr(world.training, "_calls", SimpleNamespace(adamw_step=lambda *a: 0))
+    weights, grads = [Tensor(t.float32, n, 5) for n in (300, 7)], [Tensor(t.float32, n, 5) for n in (300, 7)]
+    plan = world.slaq.AdamW(weights, grads, state_bits=bits)
+    own = [plan._ws, *plan.exp_avg, *plan.exp_avg_sq, *(plan.exp_avg_scale or []), *(plan.exp_avg_sq_scale or [])]
+    assert len(own) == (9 if bits == 8 else 5)
+
+    def use(stream):
+        {"step": plan.step, "set_group": lambda stream: plan.set_group(0, stream=stream, lr=0.1), "set_grads": lambda stream: plan.set_grads(grads, stream=stream),
+         "get_steps": plan.get_steps}[call](stream=stream)
+    use(None)
+    assert not any(x.recorded for x in own)                  # the stream that it was made on
+    for _ in range(2):
+        use(9)
+        use(0)
+    assert all(x.recorded == [9, 0] for x in own)            # once for each
+    assert not any(x.recorded for x in weights + grads)      # the caller's
