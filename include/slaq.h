@@ -553,7 +553,7 @@ int slaq_token_loss(const void* d_logits, int type, int64_t rows, int32_t vocab,
  * probability.  Rows that are no job's (before the first, behind the last, a refused job's) are left as they were, or set to 0 if zero_rest
  * is not 0 (it takes a job then: SLAQ_E_ARG without).  d_out_row_grad overlaps none of the inputs.
  * A job without a row that counts has loss NaN, and so has one whose offsets leave 0 .. rows or fall (its rows are not
- * touched).  Errors: SLAQ_E_ARG, SLAQ_E_CUDA.
+ * touched).  Errors: SLAQ_E_ARG (null, negative counts, an address that its elements' size does not divide), SLAQ_E_CUDA.
  */
 int slaq_job_row_grad(int32_t n_jobs, const int64_t* d_offsets, int64_t rows, const int64_t* d_targets, const float* d_weights,
                       float* d_out_row_grad, int32_t zero_rest, void* cuda_stream);

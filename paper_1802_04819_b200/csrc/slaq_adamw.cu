@@ -829,6 +829,7 @@ const char* slaq_adamw_last_error(const slaq_adamw_t* h) { return h ? h->err : "
 int slaq_adamw_step(slaq_adamw_t* h, const int32_t* d_active, void* cuda_stream) {
     if (!h) return SLAQ_E_ARG;
     if (!slaq::on_device(h)) return slaq::fail(h, SLAQ_E_ARG, "the plan's device is not the current one");
+    if (!slaq::aligned(d_active)) return slaq::fail(h, SLAQ_E_ARG, "the list of active groups is not aligned to its type");
     slaq::StepArgs a = {h->tensors, h->grads, h->tensor_of, h->n_units, h->n_groups, h->unit, h->groups, d_active, h->ticket};
     h->step<<<h->grid, slaq::kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(a);
     return cudaGetLastError() == cudaSuccess ? SLAQ_OK : slaq::fail(h, SLAQ_E_CUDA, "the step could not be launched");

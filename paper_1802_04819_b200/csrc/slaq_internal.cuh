@@ -148,6 +148,12 @@ struct Staging {
     double* m_seen;
 };
 
+// Whether the addresses are those of their types' elements; null is.  The GPU faults on others.
+template <class... T>
+bool aligned(const T*... at) {
+    return ((reinterpret_cast<uintptr_t>(at) % sizeof(T) == 0) && ...);
+}
+
 }  // namespace slaq
 
 struct slaq_handle {

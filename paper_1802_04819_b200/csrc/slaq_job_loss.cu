@@ -243,6 +243,7 @@ extern "C" int slaq_job_row_grad(int32_t n_jobs, const int64_t* d_offsets, int64
                                  float* d_out_row_grad, int32_t zero_rest, void* cuda_stream) {
     using namespace slaq;
     if (n_jobs < 0 || rows < 0 || (n_jobs && (!d_offsets || (rows && !d_out_row_grad)))) return SLAQ_E_ARG;
+    if (!aligned(d_offsets, d_targets, d_weights, d_out_row_grad)) return SLAQ_E_ARG;
     if (n_jobs == 0 || rows == 0) return n_jobs == 0 && rows && zero_rest ? SLAQ_E_ARG : SLAQ_OK;
     JobArgs a = {n_jobs, d_offsets, rows, d_targets, nullptr, d_weights, d_out_row_grad, nullptr, zero_rest != 0 && n_jobs <= kFewJobs};
     const bool before = zero_rest && !a.zero_rest;
@@ -263,6 +264,7 @@ extern "C" int slaq_job_losses(int32_t n_jobs, const int64_t* d_offsets, int64_t
                                const float* d_weights, double* d_out_losses, void* cuda_stream) {
     using namespace slaq;
     if (n_jobs < 0 || rows < 0 || (n_jobs && (!d_offsets || (rows && !d_logprob) || !d_out_losses))) return SLAQ_E_ARG;
+    if (!aligned(d_offsets, d_targets, d_logprob, d_weights, d_out_losses)) return SLAQ_E_ARG;
     if (n_jobs == 0) return SLAQ_OK;
     JobArgs a = {n_jobs, d_offsets, rows, d_targets, d_logprob, d_weights, nullptr, d_out_losses, false};
     return launch_jobs<true>(a, static_cast<cudaStream_t>(cuda_stream), false);
@@ -274,6 +276,10 @@ extern "C" int slaq_append_token_losses(slaq_t* h, int32_t n, const int32_t* d_j
     using namespace slaq;
     // the append's own checks come first, so that a refused call has launched nothing
     if (!h) return SLAQ_E_ARG;
+    if (!aligned(d_job_ids, d_offsets, d_targets, d_logprob, d_weights, d_iter_times, d_cores_used, d_out_losses)) {
+        h->err = "an address that its elements' size does not divide";
+        return SLAQ_E_ARG;
+    }
     if (n > 0 && n <= h->max_jobs && d_job_ids && d_out_losses && !(d_cores_used && !d_iter_times)) {
         int device = -1;
         if (cudaGetDevice(&device) == cudaSuccess && device == h->device)

@@ -697,7 +697,9 @@ int check_rows(const RowArgs& a, int type) {
     if (a.vocab > kMaxVocab || a.rows > 0x7FFFFFFF) return SLAQ_E_RANGE;
     if (a.rows && (!a.logits || (a.rows > 1 && a.stride < 0))) return SLAQ_E_ARG;
     if (reinterpret_cast<uintptr_t>(a.logits) % size_of(type)) return SLAQ_E_ARG;
-    return SLAQ_OK;
+    const bool ok = aligned(a.targets, a.logprob, a.entropy, a.top_ids, a.top_logprobs, a.g_logprob, a.g_entropy, a.in_entropy) &&
+                    aligned(reinterpret_cast<const float2*>(a.norm), reinterpret_cast<const float2*>(a.in_norm));
+    return ok ? SLAQ_OK : SLAQ_E_ARG;
 }
 int check_gradient(const RowArgs& a, int type) {
     if (a.rows && (!a.targets || !a.grad || !a.g_logprob || (a.rows > 1 && a.grad_stride < a.vocab))) return SLAQ_E_ARG;
@@ -832,7 +834,6 @@ extern "C" int slaq_token_logprobs(const void* d_logits, int type, int64_t rows,
     a.top = top, a.top_ids = d_out_top_ids, a.top_logprobs = d_out_top_logprobs;
     if (const int rc = check_rows(a, type)) return rc;
     if (top < 0 || (top > 0 && rows && (!d_out_top_ids || !d_out_top_logprobs)) || (d_out_logprob && !d_targets && rows)) return SLAQ_E_ARG;
-    if (reinterpret_cast<uintptr_t>(d_out_norm) % 8) return SLAQ_E_ARG;
     if (top > kMaxTop) return SLAQ_E_RANGE;
     if (rows == 0) return SLAQ_OK;
     return by_type(type, [&](auto e) { return launch_logprobs<decltype(e)>(a, static_cast<cudaStream_t>(cuda_stream)); });
@@ -849,7 +850,6 @@ extern "C" int slaq_token_logprobs_grad(const void* d_logits, int type, int64_t 
     a.grad = d_out_grad, a.grad_stride = grad_stride;
     if (const int rc = check_rows(a, type)) return rc;
     if (rows && (!d_norm || (d_grad_entropy && !d_entropy))) return SLAQ_E_ARG;
-    if (reinterpret_cast<uintptr_t>(d_norm) % 8) return SLAQ_E_ARG;
     if (const int rc = check_gradient(a, type)) return rc;
     if (rows == 0) return SLAQ_OK;
     return by_type(type, [&](auto e) {

@@ -18,7 +18,7 @@ P, Q = 1 << 20, 1 << 30          # addresses that are only looked at
 def fake(tmp_path_factory):
     where = tmp_path_factory.mktemp("fake")
     inc = ["-I", str(ROOT / "include"), "-I", str(CSRC), "-I", str(Path(shutil.which("nvcc")).resolve().parent.parent / "include")]
-    sources = [CSRC / "slaq_adamw.cu", CSRC / "slaq_logprob.cu", CSRC / "slaq_job_loss.cu", ROOT / "tests" / "host_fakes" / "fake_training.cpp"]
+    sources = [CSRC / "slaq_adamw.cu", CSRC / "slaq_logprob.cu", CSRC / "slaq_job_loss.cu", *(ROOT / "tests" / "host_fakes" / name for name in ("fake_training.cpp", "fake_handle.cu"))]
     objects, running = [], []
     for source in sources:
         objects.append(str(where / (source.stem + ".o")))
@@ -36,6 +36,8 @@ def fake(tmp_path_factory):
     lib.slaq_adamw_set_group.argtypes = [vp, c_int32, vp, vp]
     lib.slaq_adamw_destroy.argtypes = [vp]
     lib.fake_limit.argtypes = [vp]
+    lib.fake_handle.restype = vp
+    lib.fake_handle_end.argtypes = [vp]
     return lib
 
 
@@ -97,3 +99,50 @@ def test_a_call_takes_no_shared_memory_from_another_threads(fake):
     assert len({kernel for kernel, _ in calls[:3]}) == 1 and len({size for _, size in calls}) == 4
     for kernel, size in calls:
         assert fake.fake_limit(kernel) >= size
+
+
+ROWS = [("logprobs", dict(x=4, targets=8, logprob=4, entropy=4, norm=8, ids=4, best=4)),
+        ("grad", dict(x=4, targets=8, norm=8, entropy=4, g=4, h=4, out=4)),
+        ("loss", dict(x=4, targets=8, g=4, logprob=4, out=4)),
+        ("row_grad", dict(offsets=8, targets=8, weights=4, out=4)),
+        ("losses", dict(offsets=8, targets=8, logprob=4, weights=4, out=8)),
+        ("append", dict(ids=4, offsets=8, targets=8, logprob=4, weights=4, times=8, cores=4, out=8))]
+
+
+def _call(lib, kind, at, handle=None):
+    """The call with these addresses."""
+    vp = c_void_p
+    a = {k: vp(v) for k, v in at.items()}
+    rows = (a.get("x"), c_int(0), c_int64(4), c_int32(100), c_int64(100), a.get("targets"), c_float(1.0))
+    if kind == "logprobs":
+        return lib.slaq_token_logprobs(*rows, a["logprob"], a["entropy"], a["norm"], c_int32(3), a["ids"], a["best"], None)
+    if kind == "grad":
+        return lib.slaq_token_logprobs_grad(*rows, a["norm"], a["entropy"], a["g"], a["h"], a["out"], c_int64(100), None)
+    if kind == "loss":
+        return lib.slaq_token_loss(*rows, a["g"], a["logprob"], a["out"], c_int64(100), None)
+    if kind == "row_grad":
+        return lib.slaq_job_row_grad(c_int32(2), a["offsets"], c_int64(4), a["targets"], a["weights"], a["out"], c_int32(1), None)
+    if kind == "losses":
+        return lib.slaq_job_losses(c_int32(2), a["offsets"], c_int64(4), a["targets"], a["logprob"], a["weights"], a["out"], None)
+    return lib.slaq_append_token_losses(vp(handle), c_int32(2), a["ids"], a["offsets"], c_int64(4), a["targets"], a["logprob"], a["weights"], a["times"], a["cores"], a["out"])
+
+
+@pytest.mark.parametrize("kind,sizes", ROWS, ids=[k for k, _ in ROWS])
+def test_addresses_that_their_elements_size_does_not_divide_are_refused(fake, kind, sizes):
+    """The GPU would fault.  A refused call launches nothing, an append neither the losses."""
+    handle = fake.fake_handle(c_int32(8)) if kind == "append" else None
+    good = {k: (i + 1) << 32 for i, k in enumerate(sizes)}
+    before = _number(fake, "launches").value
+    assert _call(fake, kind, good, handle) == 0 and _number(fake, "launches").value == before + 1
+    for name, size in sizes.items():
+        for by in (1, size // 2):
+            assert _call(fake, kind, {**good, name: good[name] + by}, handle) == -1, (name, by)
+    assert _number(fake, "launches").value == before + 1
+    if handle:
+        fake.fake_handle_end(handle)
+
+
+def test_a_list_of_groups_at_an_odd_address_is_refused(fake, plan):
+    _, h = plan()
+    assert fake.slaq_adamw_step(h, 1 << 32, None) == 0
+    assert fake.slaq_adamw_step(h, (1 << 32) + 2, None) == -1
