@@ -633,9 +633,22 @@ int fail(slaq_adamw_handle* h, int code, const char* what) {
     h->err = what;
     return code;
 }
+// Whether a call of the runtime did what it should.  An error that it left behind would be taken for that of a later call.
+bool done(cudaError_t e) {
+    if (e != cudaSuccess) (void)cudaGetLastError();
+    return e == cudaSuccess;
+}
+template <class... Params, class... Args>
+bool launch(void (*kernel)(Params...), int blocks, int threads, cudaStream_t st, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.stream = st;
+    return done(cudaLaunchKernelEx(&cfg, kernel, args...));
+}
 bool on_device(const slaq_adamw_handle* h) {
     int d = -1;
-    return cudaGetDevice(&d) == cudaSuccess && d == h->device;
+    return done(cudaGetDevice(&d)) && d == h->device;
 }
 // What the step computes with is finite in 32 bits, so that elements that are 0 stay so: the factor of the gradients, the decay, and the
 // learning rate over 1 - beta1^t, which is largest at the first step.  eps is 0 or a normal number: the step's reciprocal takes what lies
@@ -746,31 +759,27 @@ int create(slaq_adamw_handle* h, void* dev_ws, size_t bytes, int32_t n_tensors, 
     if (param_type == SLAQ_F32) h->step = pick<float, float>(masters, eight);
     else if (param_type == SLAQ_BF16) h->step = grad_type == SLAQ_F32 ? pick<__nv_bfloat16, float>(masters, eight) : pick<__nv_bfloat16, __nv_bfloat16>(masters, eight);
     else h->step = grad_type == SLAQ_F32 ? pick<__half, float>(masters, eight) : pick<__half, __half>(masters, eight);
-    if (cudaGetDevice(&h->device) != cudaSuccess) return SLAQ_E_CUDA;
+    if (!done(cudaGetDevice(&h->device))) return SLAQ_E_CUDA;
     const size_t need = layout(nullptr, nullptr, n_tensors, blocks, n_groups);   // as many units as blocks: the size does not depend on the states
     if (dev_ws) {
         if (((uintptr_t)dev_ws & 255) || bytes < need) return SLAQ_E_NOMEM;
         h->ws = dev_ws;
     } else {
-        if (cudaMalloc(&h->ws, need) != cudaSuccess) {
-            (void)cudaGetLastError();
-            return SLAQ_E_NOMEM;
-        }
+        if (!done(cudaMalloc(&h->ws, need))) return SLAQ_E_NOMEM;
         h->owns_ws = true;
     }
     layout(h, static_cast<char*>(h->ws), n_tensors, blocks, n_groups);
     std::vector<Group> gs((size_t)n_groups);
     for (int32_t k = 0; k < n_groups; ++k) gs[k] = device_group(groups[k]);
-    auto to_device = [&](void* to, const void* from, size_t n) { return n == 0 || cudaMemcpyAsync(to, from, n, cudaMemcpyHostToDevice, st) == cudaSuccess; };
+    auto to_device = [&](void* to, const void* from, size_t n) { return n == 0 || done(cudaMemcpyAsync(to, from, n, cudaMemcpyHostToDevice, st)); };
     int sm = 0, per_sm = 0;
     if (!to_device(h->tensors, refs.data(), sizeof(TensorRef) * refs.size()) || !to_device(h->grads, grads.data(), sizeof(void*) * grads.size()) ||
         !to_device(h->groups, gs.data(), sizeof(Group) * gs.size()) ||
-        cudaMemsetAsync(h->ticket, 0, sizeof(unsigned int), st) != cudaSuccess ||
-        cudaDeviceGetAttribute(&sm, cudaDevAttrMultiProcessorCount, h->device) != cudaSuccess ||
-        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, h->step, kThreads, 0) != cudaSuccess)
+        !done(cudaMemsetAsync(h->ticket, 0, sizeof(unsigned int), st)) || !done(cudaDeviceGetAttribute(&sm, cudaDevAttrMultiProcessorCount, h->device)) ||
+        !done(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, h->step, kThreads, 0)))
         return SLAQ_E_CUDA;
-    if (n_tensors) fill_units_kernel<<<n_tensors, 256, 0, st>>>(h->tensors, h->unit, h->tensor_of);
-    if (cudaGetLastError() != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return SLAQ_E_CUDA;   // the lists above end here
+    if (n_tensors && !launch(fill_units_kernel, n_tensors, 256, st, h->tensors, h->unit, h->tensor_of)) return SLAQ_E_CUDA;
+    if (!done(cudaStreamSynchronize(st))) return SLAQ_E_CUDA;   // the lists above end here
     const int64_t wanted = (units + kThreads / 32 - 1) / (kThreads / 32);
     h->grid = (int)std::max<int64_t>(1, std::min<int64_t>(wanted, (int64_t)sm * std::max(per_sm, 1)));
     return SLAQ_OK;
@@ -819,7 +828,7 @@ int slaq_adamw_create(void* dev_ws, size_t bytes, int32_t n_tensors, const slaq_
 
 int slaq_adamw_destroy(slaq_adamw_t* h) {
     if (!h) return SLAQ_OK;
-    if (h->owns_ws && h->ws) cudaFree(h->ws);   // waits for the steps that still read it
+    if (h->owns_ws && h->ws) slaq::done(cudaFree(h->ws));   // waits for the steps that still read it
     delete h;
     return SLAQ_OK;
 }
@@ -831,8 +840,7 @@ int slaq_adamw_step(slaq_adamw_t* h, const int32_t* d_active, void* cuda_stream)
     if (!slaq::on_device(h)) return slaq::fail(h, SLAQ_E_ARG, "the plan's device is not the current one");
     if (!slaq::aligned(d_active)) return slaq::fail(h, SLAQ_E_ARG, "the list of active groups is not aligned to its type");
     slaq::StepArgs a = {h->tensors, h->grads, h->tensor_of, h->n_units, h->n_groups, h->unit, h->groups, d_active, h->ticket};
-    h->step<<<h->grid, slaq::kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(a);
-    return cudaGetLastError() == cudaSuccess ? SLAQ_OK : slaq::fail(h, SLAQ_E_CUDA, "the step could not be launched");
+    return slaq::launch(h->step, h->grid, slaq::kThreads, static_cast<cudaStream_t>(cuda_stream), a) ? SLAQ_OK : slaq::fail(h, SLAQ_E_CUDA, "the step could not be launched");
 }
 
 int slaq_adamw_set_group(slaq_adamw_t* h, int32_t group, const slaq_adamw_group* g, void* cuda_stream) {
@@ -843,8 +851,8 @@ int slaq_adamw_set_group(slaq_adamw_t* h, int32_t group, const slaq_adamw_group*
     slaq_adamw_group v = *g;
     const bool keep = v.step < 0;
     if (keep) v.step = 0;
-    slaq::set_group_kernel<<<1, 1, 0, static_cast<cudaStream_t>(cuda_stream)>>>(h->groups, group, slaq::device_group(v), keep);
-    return cudaGetLastError() == cudaSuccess ? SLAQ_OK : slaq::fail(h, SLAQ_E_CUDA, "the group could not be set");
+    const bool ok = slaq::launch(slaq::set_group_kernel, 1, 1, static_cast<cudaStream_t>(cuda_stream), h->groups, group, slaq::device_group(v), keep);
+    return ok ? SLAQ_OK : slaq::fail(h, SLAQ_E_CUDA, "the group could not be set");
 }
 
 int slaq_adamw_set_grads(slaq_adamw_t* h, const void* const* grads, void* cuda_stream) {
@@ -854,9 +862,9 @@ int slaq_adamw_set_grads(slaq_adamw_t* h, const void* const* grads, void* cuda_s
     if (!grads) return slaq::fail(h, SLAQ_E_ARG, "grads is null");
     if (const int rc = slaq::check_grads(h, grads)) return rc;
     cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
-    if (cudaStreamIsCapturing(static_cast<cudaStream_t>(cuda_stream), &capturing) != cudaSuccess || capturing != cudaStreamCaptureStatusNone)
+    if (!slaq::done(cudaStreamIsCapturing(static_cast<cudaStream_t>(cuda_stream), &capturing)) || capturing != cudaStreamCaptureStatusNone)
         return slaq::fail(h, SLAQ_E_ARG, "gradients are not changed while the stream is captured");
-    if (cudaMemcpyAsync(h->grads, grads, sizeof(void*) * (size_t)h->n_tensors, cudaMemcpyHostToDevice, static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess)
+    if (!slaq::done(cudaMemcpyAsync(h->grads, grads, sizeof(void*) * (size_t)h->n_tensors, cudaMemcpyHostToDevice, static_cast<cudaStream_t>(cuda_stream))))
         return slaq::fail(h, SLAQ_E_CUDA, "copy of the gradients' addresses");
     return SLAQ_OK;
 }
@@ -866,8 +874,8 @@ int slaq_adamw_get_steps(slaq_adamw_t* h, int64_t* out_steps, void* cuda_stream)
     if (!slaq::on_device(h)) return slaq::fail(h, SLAQ_E_ARG, "the plan's device is not the current one");
     if (!out_steps) return slaq::fail(h, SLAQ_E_ARG, "out_steps is null");
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (cudaMemcpy2DAsync(out_steps, sizeof(int64_t), &h->groups->step, sizeof(slaq::Group), sizeof(int64_t), (size_t)h->n_groups,
-                          cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)
+    if (!slaq::done(cudaMemcpy2DAsync(out_steps, sizeof(int64_t), &h->groups->step, sizeof(slaq::Group), sizeof(int64_t), (size_t)h->n_groups,
+                                      cudaMemcpyDeviceToHost, st)) || !slaq::done(cudaStreamSynchronize(st)))
         return slaq::fail(h, SLAQ_E_CUDA, "copy of the steps");
     return SLAQ_OK;
 }

@@ -146,3 +146,35 @@ def test_a_list_of_groups_at_an_odd_address_is_refused(fake, plan):
     _, h = plan()
     assert fake.slaq_adamw_step(h, 1 << 32, None) == 0
     assert fake.slaq_adamw_step(h, (1 << 32) + 2, None) == -1
+
+
+@pytest.mark.parametrize("failure", ["create", "set_grads", "set_grads copy", "get_steps"])
+def test_an_error_does_not_become_that_of_a_later_step(fake, plan, failure):
+    """The runtime keeps the error of a call that failed until it is asked for; a step that was launched is not to find it."""
+    _, h = plan()
+    grads = (c_void_p * 1)(Q + (9 << 24))
+    if failure == "create":
+        _number(fake, "copies_fail").value = 1
+        assert plan()[0] == -5
+    elif failure == "set_grads":
+        _number(fake, "capture_query_fails").value = 1
+        assert fake.slaq_adamw_set_grads(h, grads, None) == -1
+    elif failure == "set_grads copy":
+        _number(fake, "copies_fail").value = 1
+        assert fake.slaq_adamw_set_grads(h, grads, None) == -5
+    else:
+        _number(fake, "copies_fail").value = 1
+        assert fake.slaq_adamw_get_steps(h, (c_int64 * 1)(), None) == -5
+    before = _number(fake, "launches").value
+    assert fake.slaq_adamw_step(h, None, None) == 0 and _number(fake, "launches").value == before + 1
+    assert fake.cudaGetLastError() == 0
+
+
+def test_a_launch_that_fails_is_an_error_once(fake, plan):
+    from paper_1802_04819_b200.training import _group
+    _, h = plan()
+    for call in (lambda: fake.slaq_adamw_step(h, None, None), lambda: fake.slaq_adamw_set_group(h, 0, byref(_group()), None), lambda: plan()[0]):
+        _number(fake, "launches_fail").value = 1
+        assert call() == -5 and _number(fake, "launches_fail").value == 0
+        assert fake.cudaGetLastError() == 0
+        assert call() == 0
