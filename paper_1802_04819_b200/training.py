@@ -87,7 +87,9 @@ def _matrix(t, name):
 def _torch_stream(stream, device):
     """A torch stream from one or from a raw cudaStream_t.  0 is the device's default stream; torch would make a new one of it."""
     cuda = _load().cuda
-    if not isinstance(stream, int):
+    if hasattr(stream, "cuda_stream"):
+        if stream.device.index != device:
+            _refuse("the stream is another GPU's than the tensors")
         return stream
     return cuda.ExternalStream(stream, device=device) if stream else cuda.default_stream(device)
 
@@ -247,6 +249,8 @@ def append_token_losses(sched, d_job_ids, offsets, targets, logprob, weights, d_
     jobs, off = _job_offsets(offsets, gpu)
     if jobs != n:
         _refuse("offsets has one entry more than there are jobs")
+    if gpu != _current_device():
+        _refuse("the rows are on another GPU than the current one, which is the handle's")
     t, lp = _vector(targets, "targets", torch.int64, rows, gpu), _vector(logprob, "logprob", torch.float32, rows, gpu)
     w = _vector(weights, "weights", torch.float32, rows, gpu)
     if out is None:      # its memory is the handle's stream's: not in use by earlier work of torch's, nor given to later work too early

@@ -115,3 +115,22 @@ def test_a_plans_memory_is_kept_for_every_stream_that_uses_it(world, monkeypatch
         use(0)
     assert all(x.recorded == [9, 0] for x in own)            # once for each
     assert not any(x.recorded for x in weights + grads)      # the caller's
+
+
+def test_a_stream_of_another_gpu_is_refused(world):
+    """Its calls would run on the current stream of the tensors' GPU, which is ordered behind nothing of that stream's."""
+    t = world.torch
+    there = SimpleNamespace(device=SimpleNamespace(index=1), cuda_stream=9)
+    offsets, targets = Tensor(t.int64, 4, 5), Tensor(t.int64, 20, 5)
+    with pytest.raises(world.slaq.SlaqError, match="another GPU"):
+        world.slaq.job_row_grad(offsets, targets, stream=there)
+    assert not world.made
+
+
+def test_rows_on_another_gpu_than_the_schedulers_are_refused(world, monkeypatch):
+    t = world.torch
+    monkeypatch.setattr(Tensor, "get_device", lambda self: 1)
+    sched = SimpleNamespace(_stream=5, _h=None, _check=lambda rc: rc, _lib=SimpleNamespace(slaq_append_token_losses=lambda *a: pytest.fail("called")))
+    args = [Tensor(t.int32, 3, 5), Tensor(t.int64, 4, 5), Tensor(t.int64, 20, 5), Tensor(t.float32, 20, 5)]
+    with pytest.raises(world.slaq.SlaqError, match="another GPU"):
+        world.training.append_token_losses(sched, *args, None, None, None, None)
