@@ -75,7 +75,7 @@ def run(policy="slaq", n_jobs=64, epochs=80, total_cores=64, max_cores_per_job=1
     first = jobs.step(active=nobody).cpu().numpy()
     arrives = np.arange(n_jobs) * (0.75 * epochs) / n_jobs
     credit, mean = np.zeros(n_jobs), []
-    with slaq.Scheduler(n_jobs, max_hist, max_cores_per_job) as sched:
+    with slaq.Scheduler(n_jobs, max_hist, max_cores_per_job, stream=torch.cuda.current_stream()) as sched:   # the losses are made there
         for epoch in range(epochs):
             new = np.nonzero(np.ceil(arrives) == epoch)[0]
             if new.size:

@@ -88,3 +88,15 @@ def test_a_plan_and_its_states_are_dropped_while_another_stream_steps(slaq, bits
     assert all(bool((x == 85).all()) for x in junk)
     # 20 steps of lr, each off by the roundings of a step; 8-bit states: a constant gradient is the largest of its block, and kept exactly
     torch.testing.assert_close(p, torch.full_like(p, 0.8), rtol=0, atol=1e-4)
+
+
+def test_a_cluster_of_training_jobs_on_another_stream(slaq):
+    """The scheduler's handle and the trainers are on one stream, whichever is current."""
+    from paper_1802_04819_b200 import trainers
+    want, jobs = trainers.run("slaq", n_jobs=12, epochs=6)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got, others = trainers.run("slaq", n_jobs=12, epochs=6)
+        torch.cuda.synchronize()
+    assert got == want and torch.equal(jobs.weights, others.weights)
