@@ -28,7 +28,6 @@ struct JobArgs {
     const float *logprob, *weights;
     float* row_grad;
     double* losses;
-    bool zero_rest;
 };
 
 struct Two {
@@ -166,20 +165,20 @@ __global__ void __launch_bounds__(512) zero_kernel(float* to, int64_t n) {
 }
 
 // A block, or a cluster of blocks, for each job.
-template <int T, bool kClustered, bool kLosses>
+template <int T, bool kClustered, bool kLosses, bool kZeroRest>
 __global__ void __launch_bounds__(T) jobs_kernel(JobArgs a) {
     __shared__ Two shared[T / 32], from_blocks[kCluster];
-    if (!kLosses && a.zero_rest) zero_rest(a);
+    if (kZeroRest) zero_rest(a);
     const int64_t j = kClustered ? blockIdx.x / kCluster : blockIdx.x;
     work_on<T, kClustered, kLosses>(a, j, rows_of(a, j), threadIdx.x, kClustered ? (int)cg::this_cluster().block_rank() : 0, shared, from_blocks);
 }
 
 // Short jobs: a warp for each; what is long among them is then done by all warps of its block.
 constexpr int kShort = 2048, kBlockJobs = 16;
-template <bool kLosses>
+template <bool kLosses, bool kZeroRest>
 __global__ void __launch_bounds__(32 * kBlockJobs) short_jobs_kernel(JobArgs a) {
     __shared__ Two shared[kBlockJobs];
-    if (!kLosses && a.zero_rest) zero_rest(a);
+    if (kZeroRest) zero_rest(a);
     const int64_t first = (int64_t)blockIdx.x * kBlockJobs, mine = first + (threadIdx.x >> 5);
     bool is_long = false;
     if (mine < a.n_jobs) {
@@ -200,7 +199,7 @@ __global__ void __launch_bounds__(32 * kBlockJobs) short_jobs_kernel(JobArgs a) 
 // 10); 1,000 jobs: 6.8 us, in a kernel of their own 5.2.  4,000 jobs: 10.8 us, without any zeros 9.8.
 constexpr int kFewJobs = 512;
 
-template <bool kLosses>
+template <bool kLosses, bool kZeroRest>
 int launch_jobs(const JobArgs& a, cudaStream_t st, bool behind_zeros) {
     const int64_t mean = a.rows / a.n_jobs;
     cudaLaunchConfig_t cfg = {};
@@ -217,20 +216,20 @@ int launch_jobs(const JobArgs& a, cudaStream_t st, bool behind_zeros) {
     if (mean <= 256) {
         cfg.gridDim = dim3((unsigned)((a.n_jobs + kBlockJobs - 1) / kBlockJobs));
         cfg.blockDim = dim3(32 * kBlockJobs);
-        e = cudaLaunchKernelEx(&cfg, short_jobs_kernel<kLosses>, a);
+        e = cudaLaunchKernelEx(&cfg, short_jobs_kernel<kLosses, kZeroRest>, a);
     } else if (mean <= 2048) {
         cfg.gridDim = dim3((unsigned)a.n_jobs);
         cfg.blockDim = dim3(128);
-        e = cudaLaunchKernelEx(&cfg, jobs_kernel<128, false, kLosses>, a);
+        e = cudaLaunchKernelEx(&cfg, jobs_kernel<128, false, kLosses, kZeroRest>, a);
     } else if (mean < 16384 || a.n_jobs > 296) {
         cfg.gridDim = dim3((unsigned)a.n_jobs);
         cfg.blockDim = dim3(512);
-        e = cudaLaunchKernelEx(&cfg, jobs_kernel<512, false, kLosses>, a);
+        e = cudaLaunchKernelEx(&cfg, jobs_kernel<512, false, kLosses, kZeroRest>, a);
     } else {
         cfg.gridDim = dim3((unsigned)a.n_jobs * kCluster);
         cfg.blockDim = dim3(1024);
         ++cfg.numAttrs;
-        e = cudaLaunchKernelEx(&cfg, jobs_kernel<1024, true, kLosses>, a);
+        e = cudaLaunchKernelEx(&cfg, jobs_kernel<1024, true, kLosses, kZeroRest>, a);
     }
     if (e != cudaSuccess) (void)cudaGetLastError();
     return e == cudaSuccess ? SLAQ_OK : SLAQ_E_CUDA;
@@ -245,19 +244,19 @@ extern "C" int slaq_job_row_grad(int32_t n_jobs, const int64_t* d_offsets, int64
     if (n_jobs < 0 || rows < 0 || (n_jobs && (!d_offsets || (rows && !d_out_row_grad)))) return SLAQ_E_ARG;
     if (!aligned(d_offsets, d_targets, d_weights, d_out_row_grad)) return SLAQ_E_ARG;
     if (n_jobs == 0 || rows == 0) return n_jobs == 0 && rows && zero_rest ? SLAQ_E_ARG : SLAQ_OK;
-    JobArgs a = {n_jobs, d_offsets, rows, d_targets, nullptr, d_weights, d_out_row_grad, nullptr, zero_rest != 0 && n_jobs <= kFewJobs};
-    const bool before = zero_rest && !a.zero_rest;
-    if (before) {
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)std::min<int64_t>((rows + 4 * 512 - 1) / (4 * 512), 4 * 148));
-        cfg.blockDim = dim3(512);
-        cfg.stream = static_cast<cudaStream_t>(cuda_stream);
-        if (cudaLaunchKernelEx(&cfg, zero_kernel, d_out_row_grad, rows) != cudaSuccess) {
-            (void)cudaGetLastError();
-            return SLAQ_E_CUDA;
-        }
+    JobArgs a = {n_jobs, d_offsets, rows, d_targets, nullptr, d_weights, d_out_row_grad, nullptr};
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (!zero_rest) return launch_jobs<false, false>(a, st, false);
+    if (n_jobs <= kFewJobs) return launch_jobs<false, true>(a, st, false);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)std::min<int64_t>((rows + 4 * 512 - 1) / (4 * 512), 4 * 148));
+    cfg.blockDim = dim3(512);
+    cfg.stream = st;
+    if (cudaLaunchKernelEx(&cfg, zero_kernel, d_out_row_grad, rows) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return SLAQ_E_CUDA;
     }
-    return launch_jobs<false>(a, static_cast<cudaStream_t>(cuda_stream), before);
+    return launch_jobs<false, false>(a, st, true);
 }
 
 extern "C" int slaq_job_losses(int32_t n_jobs, const int64_t* d_offsets, int64_t rows, const int64_t* d_targets, const float* d_logprob,
@@ -266,8 +265,8 @@ extern "C" int slaq_job_losses(int32_t n_jobs, const int64_t* d_offsets, int64_t
     if (n_jobs < 0 || rows < 0 || (n_jobs && (!d_offsets || (rows && !d_logprob) || !d_out_losses))) return SLAQ_E_ARG;
     if (!aligned(d_offsets, d_targets, d_logprob, d_weights, d_out_losses)) return SLAQ_E_ARG;
     if (n_jobs == 0) return SLAQ_OK;
-    JobArgs a = {n_jobs, d_offsets, rows, d_targets, d_logprob, d_weights, nullptr, d_out_losses, false};
-    return launch_jobs<true>(a, static_cast<cudaStream_t>(cuda_stream), false);
+    JobArgs a = {n_jobs, d_offsets, rows, d_targets, d_logprob, d_weights, nullptr, d_out_losses};
+    return launch_jobs<true, false>(a, static_cast<cudaStream_t>(cuda_stream), false);
 }
 
 extern "C" int slaq_append_token_losses(slaq_t* h, int32_t n, const int32_t* d_job_ids, const int64_t* d_offsets, int64_t rows,
