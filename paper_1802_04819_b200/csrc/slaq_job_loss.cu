@@ -4,9 +4,10 @@
 // negative or its weight 0:  loss_j = -sum w_r logprob_r / sum w_r, in 64 bits: the scheduler works on differences of losses
 // that a converged job reports at 1e-4 of their size and less.
 //
-// 12 to 20 bytes are read per row and little else happens, so what counts is that short jobs do not leave threads idle and
-// that a long one is not left to a single SM: a warp, a block or a cluster of eight blocks works on a job, by the mean number of
-// its rows, and every sum is taken in an order that the sizes alone decide.
+// 12 to 20 bytes are read per row and little else happens, so what counts is that the threads have rows and that many are on their way.
+// A warp, a block or a cluster of eight blocks works on a job, by the mean number of the jobs' rows: what is known without
+// reading the offsets.  A job far longer than the others is then one block's, on one SM: 2,000 jobs of 10 rows and one of 2 M take 1.5 ms,
+// 5,000 of 20 and one of 1 M 0.2 ms.  Every sum is taken in an order that the sizes alone decide.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -199,6 +200,16 @@ __global__ void __launch_bounds__(32 * kBlockJobs) short_jobs_kernel(JobArgs a) 
 // 10); 1,000 jobs: 6.8 us, in a kernel of their own 5.2.  4,000 jobs: 10.8 us, without any zeros 9.8.
 constexpr int kFewJobs = 512;
 
+// By the mean length.  Jobs of equal length (row factors, us; losses alike), a warp or 128 threads:
+//       256 rows: 500 jobs 2.9 and 2.9, 2,000 3.0 and 5.4;   512: 500 jobs 3.8 and 2.8, 8,000 8.2 and 16.3;   1,024: 500 jobs 5.3 and 2.8, 2,000 5.5 and 5.0
+// but 4,000 jobs of 1 to 2,000 rows, 490 on average, 25.3 and 22.6 us with both calls: a block of warps ends with its longest job.
+// 128 or 512 threads:
+//     2,048 rows: 160 jobs 3.1 and 4.1, 2,000 7.3 and 17.6;   4,096: 160 jobs 4.3 and 3.5, 2,000 14.7 and 18.5
+// 512 threads, which take 0.23 us for 1,000 rows, or a cluster of eight blocks, of which 14 are 5 us and each further one 0.2 us, whatever they do:
+//     16,384 rows: 4 jobs 5.2 and 6.2, 148 5.6 and 38;   32,768: 4 jobs 9.4 and 6.5, 16 9.4 and 9.6;   65,536: 32 jobs 16.6 and 10.5, 64 16.7 and 18.6;
+//     262,144: 48 jobs 165 and 43
+constexpr int64_t kWarpRows = 256, kSmallBlockRows = 2048, kClusterRows = 32768, kClusterRowsPerJob = 2048;
+
 template <bool kLosses, bool kZeroRest>
 int launch_jobs(const JobArgs& a, cudaStream_t st, bool behind_zeros) {
     const int64_t mean = a.rows / a.n_jobs;
@@ -213,15 +224,15 @@ int launch_jobs(const JobArgs& a, cudaStream_t st, bool behind_zeros) {
     cfg.attrs = attr;
     cfg.numAttrs = behind_zeros;
     cudaError_t e;
-    if (mean <= 256) {
+    if (mean <= kWarpRows) {
         cfg.gridDim = dim3((unsigned)((a.n_jobs + kBlockJobs - 1) / kBlockJobs));
         cfg.blockDim = dim3(32 * kBlockJobs);
         e = cudaLaunchKernelEx(&cfg, short_jobs_kernel<kLosses, kZeroRest>, a);
-    } else if (mean <= 2048) {
+    } else if (mean <= kSmallBlockRows) {
         cfg.gridDim = dim3((unsigned)a.n_jobs);
         cfg.blockDim = dim3(128);
         e = cudaLaunchKernelEx(&cfg, jobs_kernel<128, false, kLosses, kZeroRest>, a);
-    } else if (mean < 16384 || a.n_jobs > 296) {
+    } else if (mean < kClusterRows || mean < kClusterRowsPerJob * a.n_jobs) {
         cfg.gridDim = dim3((unsigned)a.n_jobs);
         cfg.blockDim = dim3(512);
         e = cudaLaunchKernelEx(&cfg, jobs_kernel<512, false, kLosses, kZeroRest>, a);
