@@ -10,7 +10,9 @@ A training step of many jobs whose logits lie in one matrix, job j's rows being 
 
 Every call is asynchronous on ``stream`` (a torch stream or a raw cudaStream_t; default: torch's current stream of the
 tensors' device; ``append_token_losses`` is on the handle's).  Results that are not given as ``out`` are allocated by torch for
-that stream; inputs must be ready on it, and stay alive until it has passed the call.  No call records anything for autograd.  Refusals raise ``SlaqError``.
+that stream; inputs must be ready on it, and stay alive until it has passed the call.  No call records anything for autograd:
+logits that require a gradient are given it by ``logits.backward(grad)``.  A given ``out``, and weights that require a gradient,
+count as changed in place (in a CUDA graph: when it is captured).  Refusals raise ``SlaqError``.
 """
 
 from __future__ import annotations
@@ -28,12 +30,12 @@ F32, BF16, F16 = 0, 1, 2
 MAX_VOCAB, MAX_TOP = 1 << 22, 32
 STATE_BLOCK = 256
 
-_torch = _calls = _address = _current_stream = _current_device = None
+_torch = _calls = _address = _current_stream = _current_device = _changed = None
 _types, _at = {}, {}          # element types; the addresses of the C functions
 
 
 def _load():
-    global _torch, _calls, _address, _current_stream, _current_device
+    global _torch, _calls, _address, _current_stream, _current_device, _changed
     if _torch is None:
         import torch
         lib, _calls = load_library(), _marshal()
@@ -44,6 +46,7 @@ def _load():
         # the address alone: torch.cuda.current_stream() makes an object, 3 of the 8 us of a call
         _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
         _current_device = torch.cuda.current_device
+        _changed = torch.autograd.graph.increment_version     # of a tensor, or of a list
         _torch = torch
     return _torch
 
@@ -168,10 +171,13 @@ def token_logprobs_grad(logits, targets, norm, grad_logprob, entropy=None, grad_
     t = _vector(targets, "targets", torch.int64, rows, gpu)
     n, g = _vector(norm, "norm", f32, 2 * rows, gpu), _vector(grad_logprob, "grad_logprob", f32, rows, gpu)
     e, h = _vector(entropy, "entropy", f32, rows, gpu), _vector(grad_entropy, "grad_entropy", f32, rows, gpu)
+    given = out is not None
     out, to, to_pitch = _gradient(out, logits)
     rc = _calls.token_logprobs_grad(_at["token_logprobs_grad"], x, kind, rows, vocab, pitch, t, scale, n, e, g, h, to, to_pitch, _current_stream(gpu))
     if rc < 0:
         _check(rc, _GRADIENT if rc == -1 else None)
+    if given:
+        _changed(out)
     return out
 
 
@@ -183,11 +189,14 @@ def token_loss(logits, targets, row_grad, scale: float = 1.0, out=None, stream=N
         with _elsewhere(stream, gpu):
             return token_loss(logits, targets, row_grad, scale, out)
     t, g = _vector(targets, "targets", torch.int64, rows, gpu), _vector(row_grad, "row_grad", torch.float32, rows, gpu)
+    given = out is not None
     out, to, to_pitch = _gradient(out, logits)
     logprob = torch.empty(rows, device=out.device, dtype=torch.float32)
     rc = _calls.token_loss(_at["token_loss"], x, kind, rows, vocab, pitch, t, scale, g, logprob.data_ptr(), to, to_pitch, _current_stream(gpu))
     if rc < 0:
         _check(rc, _GRADIENT if rc == -1 else None)
+    if given:
+        _changed(out)
     return logprob, out
 
 
@@ -221,6 +230,8 @@ def job_row_grad(offsets, targets=None, weights=None, out=None, stream=None):
     rc = _calls.job_row_grad(_at["job_row_grad"], n, off, rows, t, w, to, fresh and n > 0, _current_stream(gpu))
     if rc < 0:
         _check(rc)
+    if not fresh:
+        _changed(out)
     return out
 
 
@@ -234,12 +245,15 @@ def job_losses(offsets, targets, logprob, weights=None, out=None, stream=None):
             return job_losses(offsets, targets, logprob, weights, out)
     t, lp = _vector(targets, "targets", torch.int64, rows, gpu), _vector(logprob, "logprob", torch.float32, rows, gpu)
     w = _vector(weights, "weights", torch.float32, rows, gpu)
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty(n, device=logprob.device, dtype=torch.float64)
     to = _vector(out, "out", torch.float64, n, gpu)
     rc = _calls.job_losses(_at["job_losses"], n, off, rows, t, lp, w, to, _current_stream(gpu))
     if rc < 0:
         _check(rc)
+    if given:
+        _changed(out)
     return out
 
 
@@ -350,6 +364,7 @@ class AdamW:
         _check(rc, {-1: "a group or its numbers out of range, a tensor listed twice, or tensors that overlap"}.get(rc))
         self._gpu, self._n_groups = gpu, len(groups)
         self._streams = {raw}                       # those that it is kept for
+        self._watched = [p for p in params if p.requires_grad]
 
     def _ok(self, rc):
         return _check(rc, self._lib.slaq_adamw_last_error(self._h).decode() if rc < 0 else None)
@@ -378,6 +393,8 @@ class AdamW:
         rc = _calls.adamw_step(_at["adamw_step"], self._h.value, a, self._here())
         if rc < 0:
             self._ok(rc)
+        if self._watched:
+            _changed(self._watched)
 
     def set_group(self, group: int, stream=None, **values):
         """New numbers of a group from the next step on; what is not named stays as it is, the count of steps too."""

@@ -10,7 +10,7 @@ class Tensor:
     """What the calls ask of a tensor.  `stream` is the one that was current when it was made."""
 
     def __init__(self, dtype, n, stream):
-        self.dtype, self.n, self.stream, self.recorded, self.is_cuda = dtype, n, stream, [], True
+        self.dtype, self.n, self.stream, self.recorded, self.is_cuda, self.requires_grad = dtype, n, stream, [], True, False
         self.device = SimpleNamespace(index=0)
 
     def to(self, dtype):
