@@ -605,7 +605,7 @@ typedef struct slaq_adamw_handle slaq_adamw_t;
  * slaq_adamw_workspace_bytes() long, that outlives the plan.  Host arrays; the call returns when the plan is on the device and
  * must not be captured.  Any alignment of the tensors that suits their type will do.
  * Errors: SLAQ_E_ARG (null, unknown types, a group or its numbers out of range, a tensor listed twice, tensors that
- * overlap one another or a gradient), SLAQ_E_RANGE (more than 2^38 elements), SLAQ_E_NOMEM, SLAQ_E_CUDA.
+ * overlap one another or a gradient, a stream that is captured), SLAQ_E_RANGE (more than 2^38 elements), SLAQ_E_NOMEM, SLAQ_E_CUDA.
  */
 int slaq_adamw_create(void* dev_ws, size_t bytes, int32_t n_tensors, const slaq_adamw_tensor* tensors, int32_t n_groups,
                       const slaq_adamw_group* groups, int param_type, int grad_type, int state_bits, void* cuda_stream,
@@ -627,7 +627,7 @@ int slaq_adamw_step(slaq_adamw_t* h, const int32_t* d_active, void* cuda_stream)
 int slaq_adamw_set_group(slaq_adamw_t* h, int32_t group, const slaq_adamw_group* g, void* cuda_stream);
 /* Other gradients (host array of n_tensors device addresses) from the next step on, in the stream's order; not while it is captured. */
 int slaq_adamw_set_grads(slaq_adamw_t* h, const void* const* grads, void* cuda_stream);
-/* Steps taken per group (host, n_groups entries); waits for the stream. */
+/* Steps taken per group (host, n_groups entries); waits for the stream, which must not be captured (SLAQ_E_ARG). */
 int slaq_adamw_get_steps(slaq_adamw_t* h, int64_t* out_steps, void* cuda_stream);
 
 #ifdef __cplusplus

@@ -638,6 +638,11 @@ bool done(cudaError_t e) {
     if (e != cudaSuccess) (void)cudaGetLastError();
     return e == cudaSuccess;
 }
+// A stream that is captured, or cannot be asked: to wait for it would end the capture with an error.
+bool captured(cudaStream_t st) {
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    return !done(cudaStreamIsCapturing(st, &status)) || status != cudaStreamCaptureStatusNone;
+}
 template <class... Params, class... Args>
 bool launch(void (*kernel)(Params...), int blocks, int threads, cudaStream_t st, Args... args) {
     cudaLaunchConfig_t cfg = {};
@@ -760,6 +765,7 @@ int create(slaq_adamw_handle* h, void* dev_ws, size_t bytes, int32_t n_tensors, 
     else if (param_type == SLAQ_BF16) h->step = grad_type == SLAQ_F32 ? pick<__nv_bfloat16, float>(masters, eight) : pick<__nv_bfloat16, __nv_bfloat16>(masters, eight);
     else h->step = grad_type == SLAQ_F32 ? pick<__half, float>(masters, eight) : pick<__half, __half>(masters, eight);
     if (!done(cudaGetDevice(&h->device))) return SLAQ_E_CUDA;
+    if (captured(st)) return SLAQ_E_ARG;
     const size_t need = layout(nullptr, nullptr, n_tensors, blocks, n_groups);   // as many units as blocks: the size does not depend on the states
     if (dev_ws) {
         if (((uintptr_t)dev_ws & 255) || bytes < need) return SLAQ_E_NOMEM;
@@ -861,8 +867,7 @@ int slaq_adamw_set_grads(slaq_adamw_t* h, const void* const* grads, void* cuda_s
     if (h->n_tensors == 0) return SLAQ_OK;
     if (!grads) return slaq::fail(h, SLAQ_E_ARG, "grads is null");
     if (const int rc = slaq::check_grads(h, grads)) return rc;
-    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
-    if (!slaq::done(cudaStreamIsCapturing(static_cast<cudaStream_t>(cuda_stream), &capturing)) || capturing != cudaStreamCaptureStatusNone)
+    if (slaq::captured(static_cast<cudaStream_t>(cuda_stream)))
         return slaq::fail(h, SLAQ_E_ARG, "gradients are not changed while the stream is captured");
     if (!slaq::done(cudaMemcpyAsync(h->grads, grads, sizeof(void*) * (size_t)h->n_tensors, cudaMemcpyHostToDevice, static_cast<cudaStream_t>(cuda_stream))))
         return slaq::fail(h, SLAQ_E_CUDA, "copy of the gradients' addresses");
@@ -874,6 +879,7 @@ int slaq_adamw_get_steps(slaq_adamw_t* h, int64_t* out_steps, void* cuda_stream)
     if (!slaq::on_device(h)) return slaq::fail(h, SLAQ_E_ARG, "the plan's device is not the current one");
     if (!out_steps) return slaq::fail(h, SLAQ_E_ARG, "out_steps is null");
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (slaq::captured(st)) return slaq::fail(h, SLAQ_E_ARG, "the stream is being captured");
     if (!slaq::done(cudaMemcpy2DAsync(out_steps, sizeof(int64_t), &h->groups->step, sizeof(slaq::Group), sizeof(int64_t), (size_t)h->n_groups,
                                       cudaMemcpyDeviceToHost, st)) || !slaq::done(cudaStreamSynchronize(st)))
         return slaq::fail(h, SLAQ_E_CUDA, "copy of the steps");

@@ -267,13 +267,16 @@ def append_token_losses(sched, d_job_ids, offsets, targets, logprob, weights, d_
         _refuse("the rows are on another GPU than the current one, which is the handle's")
     t, lp = _vector(targets, "targets", torch.int64, rows, gpu), _vector(logprob, "logprob", torch.float32, rows, gpu)
     w = _vector(weights, "weights", torch.float32, rows, gpu)
-    if out is None:      # its memory is the handle's stream's: not in use by earlier work of torch's, nor given to later work too early
+    given = out is not None
+    if not given:        # its memory is the handle's stream's: not in use by earlier work of torch's, nor given to later work too early
         with contextlib.nullcontext() if sched._stream == _current_stream(gpu) else _elsewhere(sched._stream, gpu):
             out = torch.empty(n, dtype=torch.float64, device=logprob.device)
     sched._check(sched._lib.slaq_append_token_losses(
         sched._h, n, _vector(d_job_ids, "job ids", torch.int32, n, gpu), off, rows, t, lp, w,
         _vector(d_iter_times, "iteration times", torch.float64, n, gpu), _vector(d_cores_used, "cores", torch.int32, n, gpu),
         _vector(out, "out", torch.float64, n, gpu)))
+    if given:
+        _changed(out)
     return out
 
 
@@ -361,7 +364,7 @@ class AdamW:
                                                              (exp_avg_sq_scale, self.exp_avg_sq_scale)) if given is None and made is not None for t in made]
             rc = self._lib.slaq_adamw_create(self._ws.data_ptr(), need, n, table, len(groups), (_Group * len(groups))(*groups),
                                              _types[kind], _types[grad_kind], state_bits, raw, ctypes.byref(self._h))
-        _check(rc, {-1: "a group or its numbers out of range, a tensor listed twice, or tensors that overlap"}.get(rc))
+        _check(rc, {-1: "a group or its numbers out of range, a tensor listed twice, tensors that overlap, or a stream that is being captured"}.get(rc))
         self._gpu, self._n_groups = gpu, len(groups)
         self._streams = {raw}                       # those that it is kept for
         self._watched = [p for p in params if p.requires_grad]

@@ -10,7 +10,8 @@
 struct slaq_handle;
 
 extern "C" {
-int fake_launches = 0, fake_memsets = 0;
+int fake_launches = 0, fake_copies = 0;
+int fake_capturing = 0;
 int fake_capture_query_fails = 0;          // cudaStreamIsCapturing fails that often
 int fake_copies_fail = 0;                  // cudaMemcpyAsync
 int fake_launches_fail = 0;
@@ -51,15 +52,16 @@ cudaError_t cudaFree(void* p) { std::free(p); return cudaSuccess; }
 cudaError_t cudaMemcpyAsync(void* d, const void* s, size_t n, cudaMemcpyKind, cudaStream_t) {
     if (fake_copies_fail > 0) return --fake_copies_fail, is(cudaErrorStreamCaptureUnsupported);
     std::memcpy(d, s, n);
+    ++fake_copies;
     return cudaSuccess;
 }
 cudaError_t cudaMemcpy2DAsync(void*, size_t, const void*, size_t, size_t, size_t, cudaMemcpyKind, cudaStream_t) {
     if (fake_copies_fail > 0) return --fake_copies_fail, is(cudaErrorStreamCaptureUnsupported);
     return cudaSuccess;
 }
-cudaError_t cudaMemsetAsync(void*, int, size_t, cudaStream_t) { ++fake_memsets; return cudaSuccess; }   // the tests' addresses are not always memory
+cudaError_t cudaMemsetAsync(void* d, int v, size_t n, cudaStream_t) { std::memset(d, v, n); return cudaSuccess; }
 cudaError_t cudaStreamIsCapturing(cudaStream_t, cudaStreamCaptureStatus* s) {
-    *s = cudaStreamCaptureStatusNone;
+    *s = fake_capturing ? cudaStreamCaptureStatusActive : cudaStreamCaptureStatusNone;
     if (fake_capture_query_fails > 0) return --fake_capture_query_fails, is(cudaErrorStreamCaptureImplicit);
     return cudaSuccess;
 }

@@ -178,3 +178,19 @@ def test_a_launch_that_fails_is_an_error_once(fake, plan):
         assert call() == -5 and _number(fake, "launches_fail").value == 0
         assert fake.cudaGetLastError() == 0
         assert call() == 0
+
+
+def test_calls_that_wait_are_refused_while_the_stream_is_captured(fake, plan):
+    """Waiting would end the capture with an error of its own."""
+    _, h = plan()
+    launches, copies = _number(fake, "launches").value, _number(fake, "copies").value
+    _number(fake, "capturing").value = 1
+    try:
+        assert plan()[0] == -1
+        assert fake.slaq_adamw_get_steps(h, (c_int64 * 1)(), None) == -1
+        assert fake.slaq_adamw_set_grads(h, (c_void_p * 1)(Q + (9 << 24)), None) == -1
+        assert _number(fake, "launches").value == launches and _number(fake, "copies").value == copies
+        assert fake.slaq_adamw_step(h, None, None) == 0
+    finally:
+        _number(fake, "capturing").value = 0
+    assert plan()[0] == 0

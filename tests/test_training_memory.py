@@ -60,6 +60,7 @@ def world(monkeypatch):
     monkeypatch.setattr(training, "_torch", fake)
     monkeypatch.setattr(training, "_current_stream", lambda gpu: w.stream)
     monkeypatch.setattr(training, "_current_device", lambda: 0)
+    monkeypatch.setattr(training, "_changed", lambda t: None)
     w.torch = fake
     return w
 
