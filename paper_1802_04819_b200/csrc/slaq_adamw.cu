@@ -237,7 +237,10 @@ __device__ __forceinline__ Codes encode(const Eight& m, const Eight& r, int lane
             most_m >= kTiny ? most_m * kPer : 0.0f, most_r >= kTiny ? most_r * kPer : 0.0f};
 }
 
-// sqrt and 1/x to 1 ulp or two, denormal arguments of the root included
+// sqrt and 1/x to 1 ulp or two, denormal arguments of the root included.  A weight's step is then off by a few ulp of
+// the step, which is far smaller than the weight: against 64 bits new weights are as exact as with correctly rounded operations (3.6e-8 and
+// 4.2e-8 of their size).  With 32-bit states a root to the nearest takes 917 us where this one takes 886 (209 M bf16 weights with masters; without masters 772
+// and 674), a division instead of the product with 1/x 1,043 (808).  With 8-bit states the division takes 720 us instead of 601.
 __device__ __forceinline__ float root(float x) {
     float y;
     asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -257,7 +260,9 @@ __device__ __forceinline__ Pair sum_of_products(Pair a, Pair b) {
     return pair_of(__fadd_rn(p, r), __fadd_rn(q, t));
 }
 
-// What a step needs of a group.  1 - beta^t is a difference of 64-bit numbers (1e-3 at the first step for beta2 = 0.999).
+// What a step needs of a group.  1 - beta^t is a difference of 64-bit numbers (1e-3 at the first step for beta2 = 0.999), rounded to 32
+// before the root and the division: up to 1.5 ulp of a step in all.  Both in 64 bits cost a step over 320 small tensors, in which every warp has
+// one tensor, 9.5 us instead of 8.5, and 10 where the step's last block does it for the next.
 struct Numbers {
     float b1, a1, b2, a2, correct, eps, keep, size, grad_scale;
 };
@@ -504,8 +509,9 @@ struct Ahead {
 
 // The same with 8-bit states where weights and gradients are of 16 bits and there is no master copy: a block is then 48 bytes a lane, and one ahead leaves 25 KB
 // on their way to an SM where 40 are wanted.  Three ahead, and 32 blocks in a row, whose scales fill a line of each state:
-// 599 us for 304 M elements (5.1 TB/s); with fused products and a root good to 1 ulp 528, then against 604 with one ahead: instructions
-// bound it.  With more bytes a block it is the other way round (fp32: 1110 us against 790).
+// 599 us for 304 M elements (5.1 TB/s); with fused products and a root good to 1 ulp 528, then against 604 with one ahead.  It has 28 % of the
+// warps resident and uses 69 % of the issue slots, but more warps do not help: registers for six, seven or eight blocks on an SM instead of
+// five (78, 72, 64 instead of 96): 641, 672 and 745 us; two blocks ahead 608.  With more bytes a block three ahead lose (fp32: 1110 us against 790).
 template <class P>
 __global__ void __launch_bounds__(kThreads) deep_step_kernel(StepArgs a) {
     using Blocks = Ahead<P, P>;

@@ -768,8 +768,9 @@ cudaError_t launch_stream(RowArgs a, int cluster, cudaStream_t st) {
 // A warp to a row while there are rows for all warps and a row is not too long for one (2,400 x 5,000 with 5 alternatives: 14.3 us, a
 // block of 128 threads 18.5; 30,000 x 3,000: 39 and 68; but 2,000 x 16,000: 20.5 and 17.3).  With few rows a cluster shares one, as many
 // blocks as make two on every SM (64 x 130,001 fp32: 11.0 us; four on every SM 12.1).  More threads where a block has the SM for
-// itself (there 512 threads 12.0 us, 128 threads 17); with many rows several small blocks hide one another's ends better than one
-// large one (8,192 x 65,536 bf16: 128 threads 166 us, 512 threads 242).
+// itself (there 512 threads 12.0 us, 128 threads 17); with many rows several small blocks hide one another's ends better than
+// large ones, up to a length: 8,192 x 32,768 bf16 98 us with 128 threads, 105 with 256; 8,192 x 65,536, which may touch 8,193 vectors and gets
+// 256, 168 and 174 in a burst, 187 and 195 under load (512 threads: 242); 600 x 65,536 22.6 and 20.5; 2,048 x 65,536 fp32 90 and 84.
 template <class E>
 cudaError_t launch_logprobs(const RowArgs& a, cudaStream_t st) {
     if (a.vocab <= kNarrow) return launch_narrow<E, false>(a, st);
@@ -788,7 +789,7 @@ cudaError_t launch_logprobs(const RowArgs& a, cudaStream_t st) {
 // 4,096 x 128,000 bf16 in clusters of four: 403 us, 79 % of the copy bandwidth (a step read twice from memory: 495 us; parts of 32 KB in
 // clusters of eight 445; blocks of 512 threads 507).  What bounds it is the special function unit, two exponentials an element keep
 // it busy 63 % of the time, and the turns: a block waits for its cluster once a row.  Exponentials by a polynomial in a quarter
-// or half of the places gained nothing: 393 and 408 us.
+// or half of the places were worth 2 % and nothing: 393 and 408 us.
 template <class E>
 cudaError_t launch_loss(RowArgs a, cudaStream_t st) {
     if (a.vocab <= kNarrow) return launch_narrow<E, true>(a, st);

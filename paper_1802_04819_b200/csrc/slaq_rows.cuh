@@ -21,7 +21,10 @@ template <> __device__ __forceinline__ __half from_float<__half>(float x) { retu
 constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kGone = -200.0f;   // 2^kGone is 0 in 32 bits, and 0 x kGone is 0 where 0 x -inf is not
 
-// 2^x to 2 ulp, 0 from -126 down
+// 2^x to 2 ulp, 0 from -126 down.  Of a difference (x - m) scale log2(e) whose constant is rounded once: log probabilities are then within
+// 1.3e-7 of 64 bits, relatively, where elementary operations in 32 bits with expf come to 0.8e-7.  expf in its place would cost more than
+// anything else here does: 8,192 x 65,536 bf16 264 us instead of 168, loss and gradient of 4,096 x 128,000 528 instead of 400, the gradient
+// alone of 4,096 x 128,000 403 instead of 322.
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
