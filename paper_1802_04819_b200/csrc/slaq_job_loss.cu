@@ -199,6 +199,7 @@ __global__ void __launch_bounds__(32 * kBlockJobs) short_jobs_kernel(JobArgs a) 
 // Up to here every block looks at all offsets (512 jobs of 500 rows: 3.9 us, a call from Python 7.6; zeros in a kernel of their own 4.2 and
 // 10); 1,000 jobs: 6.8 us, in a kernel of their own 5.2.  4,000 jobs: 10.8 us, without any zeros 9.8.
 constexpr int kFewJobs = 512;
+constexpr int64_t kFewRows = (int64_t)1 << 26;   // each of which may have to be held against all of these jobs
 
 // By the mean length.  Jobs of equal length (row factors, us; losses alike), a warp or 128 threads:
 //       256 rows: 500 jobs 2.9 and 2.9, 2,000 3.0 and 5.4;   512: 500 jobs 3.8 and 2.8, 8,000 8.2 and 16.3;   1,024: 500 jobs 5.3 and 2.8, 2,000 5.5 and 5.0
@@ -258,7 +259,7 @@ extern "C" int slaq_job_row_grad(int32_t n_jobs, const int64_t* d_offsets, int64
     JobArgs a = {n_jobs, d_offsets, rows, d_targets, nullptr, d_weights, d_out_row_grad, nullptr};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (!zero_rest) return launch_jobs<false, false>(a, st, false);
-    if (n_jobs <= kFewJobs) return launch_jobs<false, true>(a, st, false);
+    if (n_jobs <= kFewJobs && rows <= kFewRows) return launch_jobs<false, true>(a, st, false);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)std::min<int64_t>((rows + 4 * 512 - 1) / (4 * 512), 4 * 148));
     cfg.blockDim = dim3(512);
