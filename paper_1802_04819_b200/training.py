@@ -291,6 +291,8 @@ class _Group(ctypes.Structure):
 
 
 def _group(lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=1.0, step=0):
+    if not -1 <= step <= 1 << 53:      # the field would hold another number
+        _refuse("a count of steps is 0 .. 2^53")
     return _Group(lr, betas[0], betas[1], eps, weight_decay, grad_scale, step)
 
 
@@ -321,6 +323,8 @@ class AdamW:
         self._groups = [dict(g) for g in ([{}] if groups is None else groups)]
         groups = [_group(**g) for g in self._groups]
         grads = list(grads)
+        if not all(0 <= g < len(groups) for g in group_of) or any(g.step < 0 for g in groups):
+            _refuse("a tensor's group is not one of the groups, or a group has a negative count of steps")
         if kind not in _types or not params[0].is_cuda or len(grads) != n or len(group_of) != n or not groups:
             _refuse("parameters are fp32, bf16 or fp16 tensors on a GPU, with a gradient and a group each")
 

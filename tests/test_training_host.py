@@ -81,9 +81,14 @@ def test_an_epsilon_below_the_normal_numbers_is_refused(fake, plan, eps, code):
 def test_numbers_that_a_step_in_32_bits_does_not_hold_are_refused(fake, plan, numbers, code):
     """An infinite factor makes NaN of elements that are 0; a count of 2^63 - 1 overflows with the next step."""
     from paper_1802_04819_b200.training import _group
-    assert plan([_group(**numbers)])[0] == code
+
+    def group(step, numbers):
+        g = _group(**{k: v for k, v in numbers.items() if k != "step"})
+        g.step = numbers.get("step", step)
+        return g
+    assert plan([group(0, numbers)])[0] == code
     _, h = plan()
-    assert fake.slaq_adamw_set_group(h, 0, byref(_group(**{"step": -1, **numbers})), None) == code
+    assert fake.slaq_adamw_set_group(h, 0, byref(group(-1, numbers)), None) == code
 
 
 def test_a_call_takes_no_shared_memory_from_another_threads(fake):

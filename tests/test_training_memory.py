@@ -135,3 +135,20 @@ def test_rows_on_another_gpu_than_the_schedulers_are_refused(world, monkeypatch)
     args = [Tensor(t.int32, 3, 5), Tensor(t.int64, 4, 5), Tensor(t.int64, 20, 5), Tensor(t.float32, 20, 5)]
     with pytest.raises(world.slaq.SlaqError, match="another GPU"):
         world.training.append_token_losses(sched, *args, None, None, None, None)
+
+
+@pytest.mark.parametrize("changes", [dict(group_of=[0, 2 ** 32]), dict(group_of=[-(2 ** 32), 0]), dict(group_of=[0, 1]), dict(groups=[dict(step=2 ** 64)]),
+                                     dict(groups=[dict(step=2 ** 53 + 1)]), dict(groups=[dict(step=-1)])])
+def test_numbers_that_their_fields_do_not_hold_are_refused(world, monkeypatch, changes):
+    """2^32 is 0 in 32 bits: the tensor would have been stepped with group 0."""
+    t = world.torch
+    lib = SimpleNamespace(slaq_adamw_create=lambda *a: 0, slaq_adamw_destroy=lambda *a: 0, slaq_adamw_set_group=lambda *a: 0, slaq_adamw_workspace_bytes=lambda *a: 4096)
+    monkeypatch.setattr(world.training, "load_library", lambda: lib)
+    weights, grads = [Tensor(t.float32, n, 5) for n in (300, 7)], [Tensor(t.float32, n, 5) for n in (300, 7)]
+    with pytest.raises(world.slaq.SlaqError) as e:
+        world.slaq.AdamW(weights, grads, **changes)
+    assert e.value.code == -1
+    plan = world.slaq.AdamW(weights, grads)
+    with pytest.raises(world.slaq.SlaqError):
+        plan.set_group(0, step=2 ** 64)
+    plan.set_group(0, lr=0.1)
