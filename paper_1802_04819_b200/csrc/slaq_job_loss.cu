@@ -196,11 +196,6 @@ __global__ void __launch_bounds__(32 * kBlockJobs) short_jobs_kernel(JobArgs a) 
     }
 }
 
-// Up to here every block looks at all offsets (512 jobs of 500 rows: 3.9 us, a call from Python 7.6; zeros in a kernel of their own 4.2 and
-// 10); 1,000 jobs: 6.8 us, in a kernel of their own 5.2.  4,000 jobs: 10.8 us, without any zeros 9.8.
-constexpr int kFewJobs = 512;
-constexpr int64_t kFewRows = (int64_t)1 << 26;   // each of which may have to be held against all of these jobs
-
 // By the mean length.  Jobs of equal length (row factors, us; losses alike), a warp or 128 threads:
 //       256 rows: 500 jobs 2.9 and 2.9, 2,000 3.0 and 5.4;   512: 500 jobs 3.8 and 2.8, 8,000 8.2 and 16.3;   1,024: 500 jobs 5.3 and 2.8, 2,000 5.5 and 5.0
 // but 4,000 jobs of 1 to 2,000 rows, 490 on average, 25.3 and 22.6 us with both calls: a block of warps ends with its longest job.
@@ -210,6 +205,13 @@ constexpr int64_t kFewRows = (int64_t)1 << 26;   // each of which may have to be
 //     16,384 rows: 4 jobs 5.2 and 6.2, 148 5.6 and 38;   32,768: 4 jobs 9.4 and 6.5, 16 9.4 and 9.6;   65,536: 32 jobs 16.6 and 10.5, 64 16.7 and 18.6;
 //     262,144: 48 jobs 165 and 43
 constexpr int64_t kWarpRows = 256, kSmallBlockRows = 2048, kClusterRows = 32768, kClusterRowsPerJob = 2048;
+
+// Every block looks at all offsets while that is this many loads in all; zeros in a kernel of their own are another launch.  A fresh result, us on
+// the device and in a call from Python, with all offsets looked at and with the other kernel:
+//     700 jobs of 500 rows 4.5 / 6.8 and 3.9 / 9.0;   1,500 of 500 7.9 / 10.2 and 5.8 / 8.9;   2,000 of 200, 16 of them in a block, 5.5 / 6.9 and 4.0 / 9.0;
+//     6,000 of 200 9.0 / 10.3 and 6.4 / 8.9;   4,000 of 500 23.6 / 24.6 and 10.1 / 12.3 (without any zeros 9.6 / 12.3)
+constexpr int64_t kOffsetsLookedAt = (int64_t)1 << 19;
+constexpr int64_t kFewRows = (int64_t)1 << 26;   // each of which may have to be held against all of these jobs
 
 template <bool kLosses, bool kZeroRest>
 int launch_jobs(const JobArgs& a, cudaStream_t st, bool behind_zeros) {
@@ -259,7 +261,8 @@ extern "C" int slaq_job_row_grad(int32_t n_jobs, const int64_t* d_offsets, int64
     JobArgs a = {n_jobs, d_offsets, rows, d_targets, nullptr, d_weights, d_out_row_grad, nullptr};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (!zero_rest) return launch_jobs<false, false>(a, st, false);
-    if (n_jobs <= kFewJobs && rows <= kFewRows) return launch_jobs<false, true>(a, st, false);
+    const int64_t blocks = rows / n_jobs <= kWarpRows ? (n_jobs + kBlockJobs - 1) / kBlockJobs : n_jobs;
+    if (blocks * n_jobs <= kOffsetsLookedAt && rows <= kFewRows) return launch_jobs<false, true>(a, st, false);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)std::min<int64_t>((rows + 4 * 512 - 1) / (4 * 512), 4 * 148));
     cfg.blockDim = dim3(512);

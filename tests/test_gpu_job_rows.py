@@ -32,10 +32,11 @@ def test_rows_of_refused_jobs_are_zeros(slaq, offsets, factors, scale):
         assert bool(((got - want).abs() <= 2.0 ** -24 * want.abs()).all())
 
 
-@pytest.mark.parametrize("jobs", [5, 510, 515, 30_000])
-def test_many_jobs_of_which_some_are_refused(slaq, jobs):
-    """Groups of five jobs with 3, 0, 4, 1 and 2 rows; every seventh group's third offset leaves the array, so that two jobs are refused."""
-    lengths = torch.tensor([3, 0, 4, 1, 2]).repeat(jobs // 5)
+@pytest.mark.parametrize("jobs,scale", [(5, 1), (2890, 1), (2900, 1), (30_000, 1), (5, 500), (720, 500), (730, 500), (3000, 200)])
+def test_many_jobs_of_which_some_are_refused(slaq, jobs, scale):
+    """Groups of five jobs with 3, 0, 4, 1 and 2 times so many rows; every seventh group's third offset leaves the array, so that two jobs
+    are refused.  Zeros are written by the same kernel or, for more jobs, by one of their own."""
+    lengths = torch.tensor([3, 0, 4, 1, 2]).repeat(jobs // 5) * scale
     off = torch.zeros(jobs + 1, dtype=torch.int64)
     off[1:] = lengths.cumsum(0)
     off += 6
@@ -54,7 +55,7 @@ def test_many_jobs_of_which_some_are_refused(slaq, jobs):
     assert bool(((got - want).abs() <= 2.0 ** -24 * want.abs()).all())
 
 
-@pytest.mark.parametrize("jobs", [2, 600])
+@pytest.mark.parametrize("jobs", [2, 600, 3000])
 def test_the_same_in_a_replayed_graph(slaq, jobs):
     off = torch.arange(0, 3 * jobs + 3, 3)
     rows = 3 * jobs + 4
