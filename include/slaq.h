@@ -546,6 +546,28 @@ int slaq_token_loss(const void* d_logits, int type, int64_t rows, int32_t vocab,
                     void* cuda_stream);
 
 /*
+ * Tokens drawn from rows of logits (as above) with given random numbers.  With m the row's largest logit x, T its temperature:
+ * w_i = exp((x_i - m) / T), in 64 bits; the order of a row is that of falling logits, equal ones lowest id first.
+ *   K = the first top_k of the order (0 or less, or more than there are: all that are not -inf), S their sum of w;
+ *   kept = of these the shortest beginning of the order whose sum reaches top_p S, at least one token (1: all of K), and of that the tokens
+ *   with w >= min_p (0: all);
+ *   token = the first one by id at which the running sum of w over the kept ones exceeds u times their sum, u = d_uniform[r] in [0, 1).
+ * Temperature 0: the token of the largest logit, lowest id first, whatever the other numbers.
+ * Each of the four numbers is one for all rows, or, where its array [rows] is not NULL, one per row: temperature 0 or 1e-30 .. 1e30,
+ * top_p and min_p 0 .. 1.
+ * d_out_token [rows];  d_out_logprob [rows]: ln of w / sum of w over the whole row, what slaq_token_logprobs gives with scale 1 / T;
+ * d_out_kept_logprob [rows]: ln of w / sum over what is kept, the probability of the draw;  d_out_kept [rows]: how many are kept.
+ * The last three may be NULL; with temperature 0 the two are 0 and 1 token is kept.
+ * A negative uniform: the row is not asked for and not read; token -1, the others 0.  A row with a NaN or +inf, a uniform of 1 or more or NaN,
+ * or numbers of its own that are out of range: token -1, NaN, NaN, 0.  A row of masked tokens (-inf) only: token -1, -inf, -inf, 0.
+ * Errors: as slaq_token_logprobs, with the numbers for all rows out of range SLAQ_E_ARG.
+ */
+int slaq_sample_tokens(const void* d_logits, int type, int64_t rows, int32_t vocab, int64_t row_stride, const float* d_uniform,
+                       float temperature, const float* d_temperatures, int32_t top_k, const int32_t* d_top_ks, float top_p,
+                       const float* d_top_ps, float min_p, const float* d_min_ps, int64_t* d_out_token, float* d_out_logprob,
+                       float* d_out_kept_logprob, int32_t* d_out_kept, void* cuda_stream);
+
+/*
  * Mean losses of jobs.  Job j owns rows d_offsets[j] .. d_offsets[j+1) of `rows` rows (d_offsets [n_jobs + 1], not falling);
  * a row counts with d_weights[r] (NULL: 1), and not at all if its target is negative (d_targets may be NULL) or its weight 0.
  * slaq_job_losses: d_out_losses[j] = -sum w logprob / sum w, in 64 bits, always summed in the same order.
@@ -623,12 +645,68 @@ const char* slaq_adamw_last_error(const slaq_adamw_t* h);
  * stream, or ordered streams), replayed graphs included.  Errors: SLAQ_E_ARG, SLAQ_E_CUDA.
  */
 int slaq_adamw_step(slaq_adamw_t* h, const int32_t* d_active, void* cuda_stream);
+/*
+ * The same with a factor for the gradients of every group, read on the device: group k's are multiplied by grad_scale x
+ * d_factors[k], or by grad_scale x d_factors[d_factor_of[k]] where several groups share a factor (d_factor_of, n_groups entries; NULL:
+ * n_factors is the number of groups).  A group whose product is not finite, or whose entry of d_factor_of is not below n_factors, is left
+ * as it is, like one that is not active.  d_factors NULL (n_factors 0, d_factor_of NULL): slaq_adamw_step.
+ */
+int slaq_adamw_step_factors(slaq_adamw_t* h, const int32_t* d_active, const float* d_factors, int32_t n_factors,
+                            const int32_t* d_factor_of, void* cuda_stream);
 /* New numbers of a group from the next step on, in the stream's order; step < 0 keeps the count.  Errors: SLAQ_E_ARG, SLAQ_E_RANGE, SLAQ_E_CUDA. */
 int slaq_adamw_set_group(slaq_adamw_t* h, int32_t group, const slaq_adamw_group* g, void* cuda_stream);
 /* Other gradients (host array of n_tensors device addresses) from the next step on, in the stream's order; not while it is captured. */
 int slaq_adamw_set_grads(slaq_adamw_t* h, const void* const* grads, void* cuda_stream);
 /* Steps taken per group (host, n_groups entries); waits for the stream, which must not be captured (SLAQ_E_ARG). */
 int slaq_adamw_get_steps(slaq_adamw_t* h, int64_t* out_steps, void* cuda_stream);
+
+/*
+ * Norms of gradients over many tensors, per group (usually a job), and clipping.  A plan holds the gradients' addresses, types and groups.
+ *   norm = |scale| sqrt(sum x^2) over the group's tensors, in 64 bits from sums of a few squares in 32;
+ *   factor = max_norm / norm where norm > max_norm, otherwise 1; NaN where the norm is not finite.
+ * The factors are what slaq_adamw_step_factors takes, which then writes nothing for the clipping and leaves a group
+ * whose gradients are not finite alone; slaq_grad_norms_apply multiplies the gradients by them, in place or into other tensors.
+ */
+typedef struct slaq_grad_tensor {
+    const void* grad;
+    void* out;               /* where slaq_grad_norms_apply puts the product, of the same type; NULL: in place */
+    int64_t n;               /* elements; 0 is allowed, its pointers are not looked at then */
+    int32_t group;
+    int32_t type;            /* of this tensor: they may differ */
+} slaq_grad_tensor;
+typedef struct slaq_grad_norms_handle slaq_grad_norms_t;
+
+/*
+ * Make a plan.  dev_ws as in slaq_adamw_create, slaq_grad_norms_workspace_bytes() long.  Host array; the call returns when the plan is on
+ * the device and must not be captured.  Any alignment that suits the types will do.
+ * Errors: SLAQ_E_ARG (null, an unknown type, a group out of range, what apply writes overlapping itself or a gradient that is not
+ * written in place, a stream that is captured), SLAQ_E_RANGE (more than 2^38 elements), SLAQ_E_NOMEM, SLAQ_E_CUDA.
+ */
+int slaq_grad_norms_create(void* dev_ws, size_t bytes, int32_t n_tensors, const slaq_grad_tensor* tensors, int32_t n_groups,
+                           void* cuda_stream, slaq_grad_norms_t** out);
+/* Bytes slaq_grad_norms_create needs for tensors of these sizes (0 for sizes outside the limits).  Host arithmetic only. */
+size_t slaq_grad_norms_workspace_bytes(int32_t n_tensors, const int64_t* numels, int32_t n_groups);
+/* Release the plan (NULL is accepted).  With a workspace of the caller, its calls must have ended. */
+int slaq_grad_norms_destroy(slaq_grad_norms_t* h);
+/* Message for the last error of h. */
+const char* slaq_grad_norms_last_error(const slaq_grad_norms_t* h);
+/*
+ * Norms and factors, asynchronous on cuda_stream, one launch.  d_active as in slaq_adamw_step; a group that is not active is not read: norm
+ * 0, factor 1.  scale: the gradients count as scale x what is stored (the grad_scale of the step that follows), finite in 32 bits.
+ * max_norm >= 0, infinity for none; d_max_norms [n_groups] in its place where it is not NULL (NaN gives the factor NaN).
+ * d_out_norm [n_groups], d_out_factor [n_groups] or NULL.  A norm beyond 32 bits is infinity there, its factor is not.
+ * Calls of one plan must run one after the other (one stream, or ordered streams), replayed graphs included.  The sums are always
+ * added in the same order.  Errors: SLAQ_E_ARG, SLAQ_E_CUDA.
+ */
+int slaq_grad_norms_measure(slaq_grad_norms_t* h, const int32_t* d_active, double scale, double max_norm, const float* d_max_norms,
+                            float* d_out_norm, float* d_out_factor, void* cuda_stream);
+/*
+ * out = grad x d_factor[group], rounded once to the type.  Groups that are not active, or whose factor is NaN, stay as they are, and so do
+ * gradients in place whose factor is 1.  Errors: SLAQ_E_ARG, SLAQ_E_CUDA.
+ */
+int slaq_grad_norms_apply(slaq_grad_norms_t* h, const int32_t* d_active, const float* d_factor, void* cuda_stream);
+/* Other gradients (host array of n_tensors device addresses) from the next call on, in the stream's order; not while it is captured. */
+int slaq_grad_norms_set_grads(slaq_grad_norms_t* h, const void* const* grads, void* cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -34,6 +34,8 @@ EXPORTED_SYMBOLS = [
     "slaq_token_logprobs", "slaq_token_logprobs_grad", "slaq_token_loss", "slaq_job_row_grad", "slaq_job_losses",
     "slaq_append_token_losses", "slaq_adamw_create", "slaq_adamw_workspace_bytes", "slaq_adamw_destroy",
     "slaq_adamw_last_error", "slaq_adamw_step", "slaq_adamw_set_group", "slaq_adamw_set_grads", "slaq_adamw_get_steps",
+    "slaq_sample_tokens", "slaq_adamw_step_factors", "slaq_grad_norms_create", "slaq_grad_norms_workspace_bytes", "slaq_grad_norms_destroy",
+    "slaq_grad_norms_last_error", "slaq_grad_norms_measure", "slaq_grad_norms_apply", "slaq_grad_norms_set_grads",
 ]
 
 
@@ -126,6 +128,7 @@ def load_library(variant: str | None = None):
         "slaq_token_logprobs": (c_int, [vp, c_int, c_int64, c_int32, c_int64, vp, c_float, vp, vp, vp, c_int32, vp, vp, vp]),
         "slaq_token_logprobs_grad": (c_int, [vp, c_int, c_int64, c_int32, c_int64, vp, c_float, vp, vp, vp, vp, vp, c_int64, vp]),
         "slaq_token_loss": (c_int, [vp, c_int, c_int64, c_int32, c_int64, vp, c_float, vp, vp, vp, c_int64, vp]),
+        "slaq_sample_tokens": (c_int, [vp, c_int, c_int64, c_int32, c_int64, vp, c_float, vp, c_int32, vp, c_float, vp, c_float, vp, vp, vp, vp, vp, vp]),
         "slaq_job_row_grad": (c_int, [c_int32, vp, c_int64, vp, vp, vp, c_int32, vp]),
         "slaq_job_losses": (c_int, [c_int32, vp, c_int64, vp, vp, vp, vp, vp]),
         "slaq_append_token_losses": (c_int, [vp, c_int32, vp, vp, c_int64, vp, vp, vp, vp, vp, vp]),
@@ -137,6 +140,14 @@ def load_library(variant: str | None = None):
         "slaq_adamw_set_group": (c_int, [vp, c_int32, vp, vp]),
         "slaq_adamw_set_grads": (c_int, [vp, vp, vp]),
         "slaq_adamw_get_steps": (c_int, [vp, vp, vp]),
+        "slaq_adamw_step_factors": (c_int, [vp, vp, vp, c_int32, vp, vp]),
+        "slaq_grad_norms_create": (c_int, [vp, c_size_t, c_int32, vp, c_int32, vp, POINTER(vp)]),
+        "slaq_grad_norms_workspace_bytes": (c_size_t, [c_int32, vp, c_int32]),
+        "slaq_grad_norms_destroy": (c_int, [vp]),
+        "slaq_grad_norms_last_error": (c_char_p, [vp]),
+        "slaq_grad_norms_measure": (c_int, [vp, vp, c_double, c_double, vp, vp, vp, vp]),
+        "slaq_grad_norms_apply": (c_int, [vp, vp, vp, vp]),
+        "slaq_grad_norms_set_grads": (c_int, [vp, vp, vp]),
     }
     sig["slaq_result_take"] = (vp, [c_size_t])      # page-locked memory for results, internal to the binding
     sig["slaq_result_give"] = (None, [vp])

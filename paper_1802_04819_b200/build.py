@@ -13,7 +13,7 @@ CSRC = PKG / "csrc"
 LIB = PKG / "libslaq.so"
 MARSHAL = PKG / "_marshal.so"      # Python extension: argument marshalling of the loop's two calls
 SOURCES = ["slaq_api.cu", "slaq_fit.cu", "slaq_gain.cu", "slaq_alloc.cu", "slaq_select.cu", "slaq_pipe.cu",
-           "slaq_logprob.cu", "slaq_job_loss.cu", "slaq_adamw.cu"]
+           "slaq_logprob.cu", "slaq_job_loss.cu", "slaq_adamw.cu", "slaq_grad_norm.cu", "slaq_sample.cu"]
 
 
 # Instrumented builds of the same sources, each a library of its own beside libslaq.so.

@@ -138,9 +138,14 @@ typedef int (*logprobs_fn)(const void*, int, int64_t, int32_t, int64_t, const in
 typedef int (*grad_fn)(const void*, int, int64_t, int32_t, int64_t, const int64_t*, float, const float*, const float*, const float*, const float*, void*,
                        int64_t, void*);
 typedef int (*loss_fn)(const void*, int, int64_t, int32_t, int64_t, const int64_t*, float, const float*, float*, void*, int64_t, void*);
+typedef int (*sample_fn)(const void*, int, int64_t, int32_t, int64_t, const float*, float, const float*, int32_t, const int32_t*, float, const float*, float,
+                         const float*, int64_t*, float*, float*, int32_t*, void*);
 typedef int (*row_grad_fn)(int32_t, const int64_t*, int64_t, const int64_t*, const float*, float*, int32_t, void*);
 typedef int (*losses_fn)(int32_t, const int64_t*, int64_t, const int64_t*, const float*, const float*, double*, void*);
 typedef int (*step_fn)(void*, const int32_t*, void*);
+typedef int (*step_factors_fn)(void*, const int32_t*, const float*, int32_t, const int32_t*, void*);
+typedef int (*measure_fn)(void*, const int32_t*, double, double, const float*, float*, float*, void*);
+typedef int (*apply_fn)(void*, const int32_t*, const float*, void*);
 
 /* The first argument of each is the C function's address, the others are its own. */
 #define CALL(name, count, type, ...)                                                     \
@@ -209,6 +214,28 @@ CALL(token_loss, 13, loss_fn, {
     void* const stream = pointer_of(a[12]);
     RUN(fn(l.x, l.type, l.rows, l.vocab, l.pitch, l.targets, l.scale, g, logprob, out, pitch, stream))
 })
+CALL(sample_tokens, 20, sample_fn, {
+    const void* const x = pointer_of(a[1]);
+    const int type = (int)number_of(a[2]);
+    const int64_t rows = number_of(a[3]);
+    const long long vocab = number_of(a[4]);
+    const int64_t pitch = number_of(a[5]);
+    const float* const uniform = pointer_of(a[6]);
+    const float temperature = (float)PyFloat_AsDouble(a[7]);
+    const float* const temperatures = pointer_of(a[8]);
+    const long long k = number_of(a[9]);
+    const int32_t* const ks = pointer_of(a[10]);
+    const float p = (float)PyFloat_AsDouble(a[11]);
+    const float* const ps = pointer_of(a[12]);
+    const float q = (float)PyFloat_AsDouble(a[13]);
+    const float* const qs = pointer_of(a[14]);
+    int64_t* const token = pointer_of(a[15]);
+    float *const logprob = pointer_of(a[16]), *const kept_logprob = pointer_of(a[17]);
+    int32_t* const kept = pointer_of(a[18]);
+    void* const stream = pointer_of(a[19]);
+    RUN(fn(x, type, rows, vocab > INT32_MAX ? INT32_MAX : (int32_t)vocab, pitch, uniform, temperature, temperatures,
+           k > INT32_MAX ? INT32_MAX : k < 0 ? 0 : (int32_t)k, ks, p, ps, q, qs, token, logprob, kept_logprob, kept, stream))
+})
 CALL(job_row_grad, 9, row_grad_fn, {
     const long long jobs = number_of(a[1]);
     const int64_t *const offsets = pointer_of(a[2]), rows = number_of(a[3]), *const targets = pointer_of(a[4]);
@@ -232,6 +259,31 @@ CALL(adamw_step, 4, step_fn, {
     void* const stream = pointer_of(a[3]);
     RUN(fn(plan, active, stream))
 })
+CALL(adamw_step_factors, 7, step_factors_fn, {
+    void* const plan = pointer_of(a[1]);
+    const int32_t* const active = pointer_of(a[2]);
+    const float* const factors = pointer_of(a[3]);
+    const long long n_factors = number_of(a[4]);
+    const int32_t* const factor_of = pointer_of(a[5]);
+    void* const stream = pointer_of(a[6]);
+    RUN(n_factors > INT32_MAX ? -2 : fn(plan, active, factors, (int32_t)n_factors, factor_of, stream))
+})
+CALL(grad_norms_measure, 9, measure_fn, {
+    void* const plan = pointer_of(a[1]);
+    const int32_t* const active = pointer_of(a[2]);
+    const double scale = PyFloat_AsDouble(a[3]), most = PyFloat_AsDouble(a[4]);
+    const float* const mosts = pointer_of(a[5]);
+    float *const norm = pointer_of(a[6]), *const factor = pointer_of(a[7]);
+    void* const stream = pointer_of(a[8]);
+    RUN(fn(plan, active, scale, most, mosts, norm, factor, stream))
+})
+CALL(grad_norms_apply, 5, apply_fn, {
+    void* const plan = pointer_of(a[1]);
+    const int32_t* const active = pointer_of(a[2]);
+    const float* const factor = pointer_of(a[3]);
+    void* const stream = pointer_of(a[4]);
+    RUN(fn(plan, active, factor, stream))
+})
 
 #define METHOD(name, text) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, text}
 static PyMethodDef methods[] = {
@@ -241,9 +293,13 @@ static PyMethodDef methods[] = {
     METHOD(token_logprobs, "one slaq_token_logprobs call"),
     METHOD(token_logprobs_grad, "one slaq_token_logprobs_grad call"),
     METHOD(token_loss, "one slaq_token_loss call"),
+    METHOD(sample_tokens, "one slaq_sample_tokens call"),
     METHOD(job_row_grad, "one slaq_job_row_grad call"),
     METHOD(job_losses, "one slaq_job_losses call"),
     METHOD(adamw_step, "one slaq_adamw_step call"),
+    METHOD(adamw_step_factors, "one slaq_adamw_step_factors call"),
+    METHOD(grad_norms_measure, "one slaq_grad_norms_measure call"),
+    METHOD(grad_norms_apply, "one slaq_grad_norms_apply call"),
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};

@@ -6,7 +6,8 @@ A training step of many jobs whose logits lie in one matrix, job j's rows being 
     logprob, grad = slaq.token_loss(logits, targets, row_grad)        # log probabilities, gradient by the logits
     sched.append_token_losses(job_ids, offsets, targets, logprob)     # the jobs' losses, into their histories
     ...                                                               # the model's own backward pass
-    adamw.step(active=alloc)                                          # only the jobs that were given cores
+    norm, factor = norms.measure(max_norm, active=alloc)              # GradNorms: the jobs' gradient norms, and what clips them
+    adamw.step(active=alloc, factors=factor)                          # only the jobs that were given cores
 
 Every call is asynchronous on ``stream`` (a torch stream or a raw cudaStream_t; default: torch's current stream of the
 tensors' device; ``append_token_losses`` is on the handle's).  Results that are not given as ``out`` are allocated by torch for
@@ -19,6 +20,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import math
 from ctypes import c_double, c_int32, c_int64, c_void_p
 from typing import NamedTuple
 
@@ -39,7 +41,8 @@ def _load():
     if _torch is None:
         import torch
         lib, _calls = load_library(), _marshal()
-        for name in ("token_logprobs", "token_logprobs_grad", "token_loss", "job_row_grad", "job_losses", "adamw_step"):
+        for name in ("token_logprobs", "token_logprobs_grad", "token_loss", "sample_tokens", "job_row_grad", "job_losses", "adamw_step", "adamw_step_factors", "grad_norms_measure",
+                     "grad_norms_apply"):
             _at[name] = ctypes.cast(getattr(lib, "slaq_" + name), c_void_p).value
         _address = _calls.address
         _types.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
@@ -199,6 +202,47 @@ def token_loss(logits, targets, row_grad, scale: float = 1.0, out=None, stream=N
     if given:
         _changed((out,))
     return logprob, out
+
+
+class TokenSamples(NamedTuple):
+    token: object            # [rows] int64, -1 where there is none
+    logprob: object          # [rows] float32: of the token among all tokens, at the row's temperature
+    kept_logprob: object     # [rows] float32: .. among those that were kept, the probability of the draw
+    kept: object             # [rows] int32: how many were kept; None without top_k, top_p and min_p
+
+
+def _number(value, none, name, dtype, rows, gpu):
+    """(a number for all rows, None), or (0, the address of the rows' numbers)"""
+    if value is None:
+        return none, None
+    return (0, _vector(value, name, dtype, rows, gpu)) if _torch.is_tensor(value) else (value, None)
+
+
+def sample_tokens(logits, uniform, temperature=1.0, top_k=None, top_p=None, min_p=None, stream=None) -> TokenSamples:
+    """slaq_sample_tokens: a token of every row of ``logits`` [rows, vocab], drawn with the random number ``uniform`` float32 [rows] of
+    [0, 1) (negative: the row is not asked for).  ``temperature``, ``top_k``, ``top_p``, ``min_p``: a number, or a tensor [rows]
+    (float32; ``top_k`` int32).  Temperature 0 takes the largest logit; None, top_k 0, top_p 1 and min_p 0 keep every token."""
+    torch = _load()
+    x, kind, rows, vocab, pitch, gpu = _matrix(logits, "logits")
+    if not _is_here(stream, gpu):
+        with _elsewhere(stream, gpu):
+            return sample_tokens(logits, uniform, temperature, top_k, top_p, min_p)
+    f32 = torch.float32
+    if uniform is None or temperature is None:
+        _refuse("a random number per row and a temperature are wanted")
+    u, (t, ts) = _vector(uniform, "uniform", f32, rows, gpu), _number(temperature, 1.0, "temperature", f32, rows, gpu)
+    k, ks = _number(top_k, 0, "top_k", torch.int32, rows, gpu)
+    p, ps = _number(top_p, 1.0, "top_p", f32, rows, gpu)
+    q, qs = _number(min_p, 0.0, "min_p", f32, rows, gpu)
+    empty, device = torch.empty, logits.device
+    token = empty(rows, device=device, dtype=torch.int64)
+    logprob, kept_logprob = empty(rows, device=device, dtype=f32), empty(rows, device=device, dtype=f32)
+    kept = None if top_k is None and top_p is None and min_p is None else empty(rows, device=device, dtype=torch.int32)
+    rc = _calls.sample_tokens(_at["sample_tokens"], x, kind, rows, vocab, pitch, u, t, ts, k, ks, p, ps, q, qs, token.data_ptr(), logprob.data_ptr(),
+                              kept_logprob.data_ptr(), None if kept is None else kept.data_ptr(), _current_stream(gpu))
+    if rc < 0:
+        _check(rc, "bad argument: a temperature, top_p or min_p out of range" if rc == -1 else None)
+    return TokenSamples(token, logprob, kept_logprob, kept)
 
 
 def _job_offsets(offsets, gpu):
@@ -391,14 +435,23 @@ class AdamW:
         with contextlib.nullcontext() if _is_here(stream, self._gpu) else _elsewhere(stream, self._gpu):
             self._ok(call(self._here()))
 
-    def step(self, active=None, stream=None):
+    def step(self, active=None, stream=None, factors=None, factor_of=None):
         """One step of the groups whose entry of ``active`` (int32 CUDA tensor [groups], for instance the allocation of
-        ``schedule_device``) is above 0; None: of all."""
+        ``schedule_device``) is above 0; None: of all.  ``factors`` (float32 [groups], for instance those of ``GradNorms.measure``)
+        multiply the groups' gradients; a group whose factor is not finite is left as it is.  Where groups share factors,
+        ``factor_of`` (int32 [groups]) says which of them is each group's."""
         if not _is_here(stream, self._gpu):
             with _elsewhere(stream, self._gpu):
-                return self.step(active)
+                return self.step(active, None, factors, factor_of)
         a = _vector(active, "active", _torch.int32, self._n_groups, self._gpu)
-        rc = _calls.adamw_step(_at["adamw_step"], self._h.value, a, self._here())
+        if factors is None:
+            if factor_of is not None:
+                _refuse("factor_of without factors")
+            rc = _calls.adamw_step(_at["adamw_step"], self._h.value, a, self._here())
+        else:
+            n = self._n_groups if factor_of is None else factors.numel()
+            rc = _calls.adamw_step_factors(_at["adamw_step_factors"], self._h.value, a, _vector(factors, "factors", _torch.float32, n, self._gpu), n,
+                                           _vector(factor_of, "factor_of", _torch.int32, self._n_groups, self._gpu), self._here())
         if rc < 0:
             self._ok(rc)
         if self._watched:
@@ -440,4 +493,124 @@ class AdamW:
             pass
 
 
-__all__ = ["AdamW", "TokenLogprobs", "token_logprobs", "token_logprobs_grad", "token_loss", "job_row_grad", "job_losses"]
+class _GradTensor(ctypes.Structure):
+    _fields_ = [("grad", c_void_p), ("out", c_void_p), ("n", c_int64), ("group", c_int32), ("type", c_int32)]
+
+
+class GradNorm(NamedTuple):
+    norm: object             # [groups] float32
+    factor: object           # [groups] float32: what clips the group's gradients; NaN where their norm is not finite
+
+
+class GradNorms:
+    """A plan of slaq_grad_norms_*: the norms of groups of gradients over many tensors, and clipping.
+
+    ``grads``: a list of contiguous CUDA tensors (fp32, bf16 or fp16, which may be mixed); ``group_of``: the group of each tensor
+    (default: all 0), ``n_groups`` groups (default: as many as ``group_of`` names).  ``out``: tensors like the gradients that
+    ``apply`` writes to (default: the gradients themselves)."""
+
+    def __init__(self, grads, group_of=None, n_groups=None, out=None, stream=None):
+        torch = _load()
+        self._h = c_void_p()
+        self._lib = load_library()
+        grads = list(grads)
+        n = len(grads)
+        if not grads:
+            _refuse("a plan without tensors")
+        group_of = [0] * n if group_of is None else [int(g) for g in group_of]
+        if len(group_of) != n or (out is not None and len(out := list(out)) != n):
+            _refuse("group_of or out has another length than grads")
+        n_groups = max(group_of) + 1 if n_groups is None else n_groups
+        if not all(0 <= g < n_groups for g in group_of) or n_groups >= 1 << 31:
+            _refuse("a tensor's group is not one of the groups")
+        if not grads[0].is_cuda or any(g.dtype not in _types for g in grads):
+            _refuse("gradients are fp32, bf16 or fp16 tensors on a GPU")
+        gpu = grads[0].get_device()
+        table, sizes = (_GradTensor * n)(), [g.numel() for g in grads]
+        for row, g, size, k in zip(table, grads, sizes, group_of):
+            row.grad, row.n, row.group, row.type = _vector(g, "grads", g.dtype, size, gpu), size, k, _types[g.dtype]
+        for row, g, size, o in zip(table, grads, sizes, out or ()):
+            row.out = _vector(o, "out", g.dtype, size, gpu)
+        with contextlib.nullcontext() if _is_here(stream, gpu) else _elsewhere(stream, gpu):
+            raw = _current_stream(gpu)
+            numels = np.array(sizes, np.int64)
+            need = self._lib.slaq_grad_norms_workspace_bytes(n, numels.ctypes.data, n_groups)
+            self._ws = torch.empty(max(need, 1), dtype=torch.uint8, device=grads[0].device)
+            rc = self._lib.slaq_grad_norms_create(self._ws.data_ptr(), need, n, table, n_groups, raw, ctypes.byref(self._h))
+        _check(rc, {-1: "tensors that overlap, or a stream that is being captured"}.get(rc))
+        self.grads, self.out, self._gpu, self._n_groups = grads, out, gpu, n_groups
+        self._streams = {raw}                       # those that the workspace is kept for
+
+    def _ok(self, rc):
+        return _check(rc, self._lib.slaq_grad_norms_last_error(self._h).decode() if rc < 0 else None)
+
+    def _here(self):
+        raw = _current_stream(self._gpu)
+        if raw not in self._streams:
+            self._ws.record_stream(_torch_stream(raw, self._gpu))
+            self._streams.add(raw)
+        return raw
+
+    def _result(self, given, name):
+        if given is None:
+            given = _torch.empty(self._n_groups, dtype=_torch.float32, device=self._ws.device)
+            return given, given.data_ptr()
+        return given, _vector(given, name, _torch.float32, self._n_groups, self._gpu)
+
+    def measure(self, max_norm=math.inf, active=None, scale: float = 1.0, norm=None, factor=None, stream=None) -> GradNorm:
+        """Norms of the groups whose entry of ``active`` (int32 [groups]) is above 0, None: of all, and the factors that bring
+        them down to ``max_norm``: a number, or float32 [groups] on the GPU.  The gradients count as ``scale`` times what is stored.
+        A group that is not active has norm 0 and factor 1.  ``norm`` and ``factor`` may be given (float32 [groups])."""
+        if not _is_here(stream, self._gpu):
+            with _elsewhere(stream, self._gpu):
+                return self.measure(max_norm, active, scale, norm, factor)
+        a = _vector(active, "active", _torch.int32, self._n_groups, self._gpu)
+        mosts = None
+        if _torch.is_tensor(max_norm):
+            max_norm, mosts = 0.0, _vector(max_norm, "max_norm", _torch.float32, self._n_groups, self._gpu)
+        given = [t for t in (norm, factor) if t is not None]
+        norm, to_norm = self._result(norm, "norm")
+        factor, to_factor = self._result(factor, "factor")
+        rc = _calls.grad_norms_measure(_at["grad_norms_measure"], self._h.value, a, scale, max_norm, mosts, to_norm, to_factor, self._here())
+        if rc < 0:
+            self._ok(rc)
+        if given:
+            _changed(given)
+        return GradNorm(norm, factor)
+
+    def apply(self, factor, active=None, stream=None):
+        """Gradients times their group's ``factor`` (float32 [groups]), in place or into ``out``.  Groups that are not active or whose
+        factor is NaN stay as they are."""
+        if not _is_here(stream, self._gpu):
+            with _elsewhere(stream, self._gpu):
+                return self.apply(factor, active)
+        a = _vector(active, "active", _torch.int32, self._n_groups, self._gpu)
+        f = _vector(factor, "factor", _torch.float32, self._n_groups, self._gpu)
+        rc = _calls.grad_norms_apply(_at["grad_norms_apply"], self._h.value, a, f, self._here())
+        if rc < 0:
+            self._ok(rc)
+        _changed(self.grads if self.out is None else self.out)
+
+    def set_grads(self, grads, stream=None):
+        """Other gradient tensors of the same types and sizes from the next call on."""
+        grads = list(grads)
+        if len(grads) != len(self.grads):
+            _refuse("grads has another length than before")
+        rows = (c_void_p * len(grads))(*[_vector(g, "grads", old.dtype, old.numel(), self._gpu) for g, old in zip(grads, self.grads)])
+        with contextlib.nullcontext() if _is_here(stream, self._gpu) else _elsewhere(stream, self._gpu):
+            self._ok(self._lib.slaq_grad_norms_set_grads(self._h, rows, self._here()))
+        self.grads = grads
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._lib.slaq_grad_norms_destroy(self._h)
+            self._h = c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+__all__ = ["AdamW", "GradNorm", "GradNorms", "TokenLogprobs", "TokenSamples", "sample_tokens", "token_logprobs", "token_logprobs_grad", "token_loss", "job_row_grad", "job_losses"]
