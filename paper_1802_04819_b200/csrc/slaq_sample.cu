@@ -6,8 +6,12 @@
 //
 // The result is an integer, and in a large vocabulary the sums of 32-bit weights are off by more than many a token's weight.  So sums come with a
 // bound of their error; where a decision lies within it, the row is summed up again in 64 bits.
+#include <cooperative_groups.h>
+
 #include "slaq_internal.cuh"
 #include "slaq_rows.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace slaq {
 namespace {
@@ -63,49 +67,76 @@ __device__ __forceinline__ void write_none(const SampleArgs& a, int64_t row, int
 }
 __device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < CUDART_INF_F; }
 
-// Weights in 32 bits: 2^(x c - M), M a whole number above m c, so that sums of other M are brought to this one exactly.  c comes in two
-// parts, which leaves two roundings of the exponent t: an error of at most 2^-23 |t| ln 2 of a weight, beside the exponential's own 2^-22.
-// Of the sum S of V weights 2^t the mean of |t| is at most log2(V / S) - the entropy of the shares is at most that of equal ones.  Beyond
-// kMostExponent the parts of c are not enough.
-constexpr float kMostExponent = 65536.0f;
+// Weights in 32 bits: 2^t, t = x c - M with c = log2(e) / T rounded to 32 bits, M a whole number above m c, so that sums with another M are brought to
+// this one exactly.  A weight is off by the exponential's 2^-22 and by |t| ln 2 (2^-24 + 2^-25), t's rounding and c's (what c's puts on all weights
+// alike cancels).  Of the sum S of V weights the mean of |t| is at most log2(V / S): the entropy of the shares is at most that of equal ones.
+// Five additions in 32 bits lead to what is added up in 64.
+constexpr float kMostExponent = 4194304.0f;                    // 2^22: beyond, M is not above m c by a little
 struct Scale {
-    float hi, lo;
-    double c;                      // log2(e) / T
-    __device__ __forceinline__ explicit Scale(float T) {
-        c = 1.4426950408889634 / (double)T;
-        hi = __double2float_rz(c);
-        lo = fmaxf((float)(c - (double)hi), 1e-38f);        // above 0: a masked token is -inf, whichever way
-    }
-    __device__ __forceinline__ float base(float m) const { return m == -CUDART_INF_F ? 0.0f : ceilf(m * hi) + 1.0f; }
-    __device__ __forceinline__ float exponent(float x, float M) const { return fmaf(x, lo, fmaf(x, hi, -M)); }
+    double exact;                  // c before it is rounded
+    float c;
+    __device__ __forceinline__ explicit Scale(float T) : exact(1.4426950408889634 / (double)T), c((float)exact) {}
+    __device__ __forceinline__ float base(float m) const { return m == -CUDART_INF_F ? 0.0f : ceilf(m * c) + 1.0f; }
+    __device__ __forceinline__ float exponent(float x, float M) const { return fmaf(x, c, -M); }
     __device__ __forceinline__ float weight(float x, float M) const { return exp2_fast(exponent(x, M)); }
-    __device__ __forceinline__ bool holds(float m) const { return fabsf(m * hi) <= kMostExponent; }
-    // of a sum of V weights, relative to it: 5 additions in 32 bits, the exponential, the exponents
-    __device__ __forceinline__ double error(int V, double S) const { return 5.0 * 5.97e-8 + 2.4e-7 + 8.3e-8 * fmax(log2((double)V / S), 0.0); }
+    __device__ __forceinline__ bool holds(float m) const { return fabsf(m * c) <= kMostExponent; }
+    // log2 of the largest element's weight with base M
+    __device__ __forceinline__ double of_largest(float m, float M) const { return (double)m * c - M; }
 };
-// .. and in 64 bits
+// Bounds of a sum's error: of its weights alike, and through their exponents.
+struct Error {
+    double alike, exponents;
+    __device__ __forceinline__ Error(int V, double S)
+        : alike(5.0 * 5.97e-8 + 2.4e-7), exponents(6.3e-8 * fmax(log2((double)V / S), 0.0)) {}
+    __device__ __forceinline__ double both() const { return alike + exponents; }
+    // .. of the difference between the sum up to a token and u times the sum, near 0: (1 - u) of the errors before it and u of those behind
+    __device__ __forceinline__ double at(double u) const { return alike * 2.0 * u * (1.0 - u) + exponents * fmax(u, 1.0 - u) + 1e-15; }
+};
+
+// Weights in 64 bits, of the largest 1: exp((x - m) / T) as 2^t, t = (x - m) c = k / 16 + f: a table of 2^(j / 16) and the series of 2^f
+// to its seventh term, |f ln 2| <= 0.0217 (the next is 4e-16).  What is less than 2^-1000 counts as 0.  exp() takes three times as long for a row: its
+// branches leave one weight at a time in work.
+constexpr int kSteps = 16;
 struct Exact {
-    double m, by;
-    __device__ __forceinline__ Exact(float most, float T) : m(most), by(1.0 / (double)T) {}
-    __device__ __forceinline__ double weight(float x) const { return exp(((double)x - m) * by); }
+    double c, m;
+    float least;                   // 0 below
+    const double* table;
+    __device__ __forceinline__ Exact(float m, const Scale& s, const double* t)
+        : c(s.exact), m(m), least((float)((double)m - 1000.0 / s.exact)), table(t) {}
+    __device__ __forceinline__ double weight(float x) const {
+        constexpr double kLn2 = 0.6931471805599453, kMagic = 422212465065984.0;   // 1.5 x 2^48: a 16th is its last place
+        const double d = (double)x - m, r = fma(d, c, kMagic), f = fma(d, c, kMagic - r);
+        const int k = __double2loint(r);
+        double p = kLn2 * kLn2 * kLn2 * kLn2 * kLn2 * kLn2 / 720.0;
+        p = fma(p, f, kLn2 * kLn2 * kLn2 * kLn2 * kLn2 / 120.0);
+        p = fma(p, f, kLn2 * kLn2 * kLn2 * kLn2 / 24.0);
+        p = fma(p, f, kLn2 * kLn2 * kLn2 / 6.0);
+        p = fma(p, f, kLn2 * kLn2 / 2.0);
+        p = fma(p, f, kLn2);
+        p = fma(p, f, 1.0) * table[k & (kSteps - 1)];
+        return x >= least ? __hiloint2double(__double2hiint(p) + ((k >> 4) << 20), __double2loint(p)) : 0.0;
+    }
 };
 // 2^d for a whole number d <= 0, exactly; 0 far below
 __device__ __forceinline__ double power(float d) { return d > -1000.0f ? __hiloint2double((1023 + (int)d) << 20, 0) : 0.0; }
 
-// Kept are the elements above `value`, and those equal to it up to id `last`.
+// Kept are the elements above `value`, and those equal to it up to id `last`; nothing that is masked.
 struct Cut {
     float value;
     uint32_t last;
     __device__ __forceinline__ bool keeps(float x, int i) const { return x > value || (x == value && (uint32_t)i <= last && x > -CUDART_INF_F); }
 };
+__device__ __forceinline__ Cut unmasked() { return {-CUDART_INF_F, 0}; }
+__device__ __forceinline__ Cut tighter(const Cut& a, const Cut& b) { return a.value > b.value || (a.value == b.value && a.last < b.last) ? a : b; }
 
-__device__ __forceinline__ double warp_sum(double x) {
+template <class T>
+__device__ __forceinline__ T warp_sum(T x) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
     return x;
 }
 template <class T>
-__device__ __forceinline__ T warp_before(T x) {      // inclusive prefix
+__device__ __forceinline__ T warp_before(T x) {      // with its own
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -115,12 +146,132 @@ __device__ __forceinline__ T warp_before(T x) {      // inclusive prefix
     return x;
 }
 
-// f(vectors, number of the first) for the row's vectors [begin, end), a warp's lanes side by side; what is not in the row is -inf.
+// .. and, from that, without it: not by subtraction, which would lose what is small beside its own
+template <class T>
+__device__ __forceinline__ T without_own(T in) {
+    const T y = __shfl_up_sync(~0u, in, 1);
+    return (threadIdx.x & 31) ? y : T(0);
+}
+
+// ---- T threads that work on a row: a block, or one of a block's warps ----
+template <int T>
+struct Team {
+    static constexpr int kPerBlock = T == 32 ? 4 : 1;
+    static __device__ __forceinline__ int thread() { return T == 32 ? threadIdx.x & 31 : threadIdx.x; }
+    static __device__ __forceinline__ int warp() { return T == 32 ? 0 : threadIdx.x >> 5; }
+    static __device__ __forceinline__ int index() { return T == 32 ? threadIdx.x >> 5 : 0; }
+    static __device__ __forceinline__ void sync() {
+        if constexpr (T == 32) __syncwarp();
+        else __syncthreads();
+    }
+};
+constexpr int kMaxCluster = 8;     // of blocks of 512
+// Elements that are listed and sorted at most, intervals of a row's values, and groups of elements whose largest one is kept
+template <int T>
+struct Sizes {
+    static constexpr int kListed = T >= 256 ? 2048 : T == 128 ? 1024 : 256;
+    static constexpr int kBins = T == 32 ? 512 : 2048;
+    static constexpr int kGroups = T == 32 ? 256 : 4096;
+};
+template <int T>
+struct Shared {
+    static constexpr int W = T / 32, kRuns = T == 512 ? W * kMaxCluster : W;
+    float most[kRuns];             // per run of the row, in a cluster in its first block
+    double sum[kRuns];
+    double table[kSteps];
+    double more[W];
+    int count[W];
+    float bound[kMaxCluster], block_most[kMaxCluster];
+    double before, after;
+    int found, listed, lowest, highest, before_it;
+    uint32_t key_low, key_high;
+};
+template <int T>
+struct Lists {                     // of the kernel with filters
+    using S = Sizes<T>;
+    union {
+        struct {
+            uint32_t hist[S::kBins], parts[S::kBins];
+        };
+        double weight[S::kListed];
+    };
+    union {
+        unsigned long long key[S::kListed];
+        float group[S::kGroups];   // until the list is made: see below
+    };
+    uint32_t id[S::kListed];
+};
+
+template <int T>
+__device__ __forceinline__ double team_sum(double x, Shared<T>& sh) {
+    x = warp_sum(x);
+    if constexpr (T == 32) return x;
+    Team<T>::sync();
+    if ((threadIdx.x & 31) == 0) sh.more[Team<T>::warp()] = x;
+    Team<T>::sync();
+    x = 0.0;
+#pragma unroll
+    for (int w = 0; w < T / 32; ++w) x += sh.more[w];
+    return x;
+}
+template <int T>
+__device__ __forceinline__ int team_sum(int x, Shared<T>& sh) {
+    x = __reduce_add_sync(~0u, x);
+    if constexpr (T == 32) return x;
+    Team<T>::sync();
+    if ((threadIdx.x & 31) == 0) sh.count[Team<T>::warp()] = x;
+    Team<T>::sync();
+    x = 0;
+#pragma unroll
+    for (int w = 0; w < T / 32; ++w) x += sh.count[w];
+    return x;
+}
+// what the threads before this one have
+template <int T>
+__device__ __forceinline__ double team_before(double x, Shared<T>& sh) {
+    const double in = warp_before(x), out = without_own(in);
+    if constexpr (T == 32) return out;
+    Team<T>::sync();
+    if ((threadIdx.x & 31) == 31) sh.more[Team<T>::warp()] = in;
+    Team<T>::sync();
+    double before = 0.0;
+    for (int w = 0; w < Team<T>::warp(); ++w) before += sh.more[w];
+    return before + out;
+}
+template <int T>
+__device__ __forceinline__ int team_before(int x, Shared<T>& sh) {
+    const int in = warp_before(x);
+    if constexpr (T == 32) return in - x;
+    Team<T>::sync();
+    if ((threadIdx.x & 31) == 31) sh.count[Team<T>::warp()] = in;
+    Team<T>::sync();
+    int before = in - x;
+    for (int w = 0; w < Team<T>::warp(); ++w) before += sh.count[w];
+    return before;
+}
+// `place` set to `value` for all, with a barrier on both sides
+template <int T, class V>
+__device__ __forceinline__ void set_all(V& place, V value) {
+    Team<T>::sync();
+    if (Team<T>::thread() == 0) place = value;
+    Team<T>::sync();
+}
+template <int T>
+__device__ __forceinline__ void fill_table(Shared<T>& sh) {
+    Team<T>::sync();
+    if (Team<T>::thread() < kSteps) sh.table[Team<T>::thread()] = exp2(Team<T>::thread() / (double)kSteps);
+    Team<T>::sync();
+}
+
+// ---- a row's vectors ----
+template <class E>
+using Batch = Vector<E>[kUnroll];
+// f(batch, number of its first vector) for the vectors [begin, end), a warp's lanes side by side; what is not in the row is -inf.
 template <class E, class F>
 __device__ __forceinline__ void over_vectors(const Row<E>& x, int begin, int end, F&& f) {
     const int lane = threadIdx.x & 31;
     for (int v = begin; v < end; v += 32 * kUnroll) {
-        Vector<E> in[kUnroll];
+        Batch<E> in;
         if (v >= x.lo && v + 32 * kUnroll <= min(end, x.hi)) {
             const E* const from = x.x + x.first(v + lane);
 #pragma unroll
@@ -132,239 +283,246 @@ __device__ __forceinline__ void over_vectors(const Row<E>& x, int begin, int end
         f(in, v + lane);
     }
 }
+// .. a vector at a time, the next one on its way: f(vector, its number)
+template <class E, class F>
+__device__ __forceinline__ void over_single(const Row<E>& x, int begin, int end, F&& f) {
+    const int lane = threadIdx.x & 31;
+    auto load = [&](int v) { return v < end ? x.load(v) : Row<E>::nothing(); };
+    Vector<E> next = load(begin + lane);
+    for (int v = begin; v < end; v += 32) {
+        const Vector<E> in = next;
+        next = load(v + 32 + lane);
+        f(in, v + lane);
+    }
+}
 // .. element by element: f(element, id)
 template <class E, class F>
 __device__ __forceinline__ void over_elements(const Row<E>& x, int begin, int end, F&& f) {
-    over_vectors(x, begin, end, [&](const Vector<E>(&in)[kUnroll], int v) {
+    over_vectors(x, begin, end, [&](const Batch<E>& in, int v) {
 #pragma unroll
         for (int k = 0; k < kUnroll; ++k)
 #pragma unroll
             for (int e = 0; e < Vector<E>::N; ++e) f(in[k].one(e), x.first(v + k * 32) + e);
     });
 }
-
-// The part of a row's vectors that a warp of T / 32 takes: neighbours, so that the warps' sums are those of runs of ids.
-template <int T>
-struct Runs {
-    int per;
-    __device__ __forceinline__ explicit Runs(int vectors) : per(((vectors + T / 32 - 1) / (T / 32) + 31) / 32 * 32) {}
-    __device__ __forceinline__ int begin(int w) const { return w * per; }
-    __device__ __forceinline__ int end(int w, int vectors) const { return min((w + 1) * per, vectors); }
-};
-
-constexpr int kBins = 4096;        // of a histogram
-constexpr int kListed = 2048;      // elements that are sorted at most
-
-template <int T>
-struct Block {
-    float most[T / 32];
-    double sum[T / 32], more[T / 32];
-    int count[T / 32];
-    int found, listed, lowest, highest, before_it;
-    double before, after;
-    uint32_t key_low, key_high;
-};
-struct Lists {                     // of the kernel with filters, behind its Block
-    union {
-        uint32_t hist[kBins];
-        double weight[kListed];
-    };
-    unsigned long long key[kListed];
-};
-
-template <int T>
-__device__ __forceinline__ double block_sum(double x, Block<T>& sh) {
-    x = warp_sum(x);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) sh.more[threadIdx.x >> 5] = x;
-    __syncthreads();
-    x = 0.0;
-    for (int w = 0; w < T / 32; ++w) x += sh.more[w];
-    return x;
+template <class E>
+__device__ __forceinline__ float largest(const Batch<E>& in) {
+    float most = in[0].max();
+#pragma unroll
+    for (int k = 1; k < kUnroll; ++k) most = max_nan(most, in[k].max());
+    return most;
 }
-// what the threads before this one have, and in `all` what all have
-template <int T>
-__device__ __forceinline__ double block_before(double x, Block<T>& sh, double& all) {
-    const double in = warp_before(x);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 31) sh.more[threadIdx.x >> 5] = in;
-    __syncthreads();
-    double before = 0.0;
-    all = 0.0;
-    for (int w = 0; w < T / 32; ++w) {
-        if (w < (int)(threadIdx.x >> 5)) before += sh.more[w];
-        all += sh.more[w];
+template <class E>
+__device__ __forceinline__ float weights_of(const Batch<E>& in, const Scale& c, float M) {
+    const Pair off = pair_of(-M, -M), by = pair_of(c.c, c.c);
+    Pair sum[kUnroll];
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+        constexpr int P = Vector<E>::N / 2;
+        Pair e[P];
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            float a, b;
+            split(fma2(in[k].at(i), by, off), a, b);
+            e[i] = pair_of(exp2_fast(a), exp2_fast(b));
+        }
+        sum[k] = e[0] + e[1];
+        if constexpr (P == 4) sum[k] = sum[k] + (e[2] + e[3]);
     }
-    return before + (in - x);
+    float a, b;
+    split((sum[0] + sum[1]) + (sum[2] + sum[3]), a, b);
+    return a + b;
 }
-template <int T>
-__device__ __forceinline__ int block_before(int x, Block<T>& sh) {
-    const int in = warp_before(x);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 31) sh.count[threadIdx.x >> 5] = in;
-    __syncthreads();
-    int before = in - x;
-    for (int w = 0; w < (int)(threadIdx.x >> 5); ++w) before += sh.count[w];
-    return before;
-}
-// sh.<place> set to `value` for all; a barrier on both sides
-template <class S, class V>
-__device__ __forceinline__ void set_all(S& place, V value) {
-    __syncthreads();
-    if (threadIdx.x == 0) place = value;
-    __syncthreads();
+// .. with -inf in the place of what is not wanted
+template <class E, class F>
+__device__ __forceinline__ void mask(Batch<E>& in, const Row<E>& x, int v, F&& wanted) {
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k)
+#pragma unroll
+        for (int i = 0; i < Vector<E>::N / 2; ++i) {
+            float a, b;
+            split(in[k].at(i), a, b);
+            const int id = x.first(v + k * 32) + 2 * i;
+            in[k].put(i, pair_of(wanted(a, id) ? a : -CUDART_INF_F, wanted(b, id + 1) ? b : -CUDART_INF_F));
+        }
 }
 
-// The row's largest element m, its base M, the sum S, and in sh.sum those of the warps' runs, all in 32-bit weights.
+// The vectors that a warp of `warps` takes: neighbours, so that the warps' sums are those of runs of ids.
+struct Runs {
+    int vectors, per;
+    __device__ __forceinline__ Runs(int vectors, int warps) : vectors(vectors), per(((vectors + warps - 1) / warps + 31) / 32 * 32) {}
+    __device__ __forceinline__ int begin(int w) const { return min(w * per, vectors); }
+    __device__ __forceinline__ int end(int w) const { return min((w + 1) * per, vectors); }
+};
+
+// Sums of runs with base M, each in sh.sum; all of them together.  Every warp adds them in the same order.
+template <int T>
+__device__ __forceinline__ double sum_of_runs(const Shared<T>& sh, int runs) {
+    double s = 0.0;
+    for (int r = threadIdx.x & 31; r < runs; r += 32) s += sh.sum[r];
+    return warp_sum(s);
+}
 struct Total {
     float m, M;
     double S;
 };
-template <class E, int T>
-__device__ __forceinline__ Total sums_of_row(const Row<E>& x, const Scale& c, Block<T>& sh) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Runs<T> runs(x.vectors);
+// A warp's run: its largest element and the sum of its weights with that one's base.  each(largest of a lane's batch)
+template <class E, class F>
+__device__ __forceinline__ void sum_run(const Row<E>& x, int begin, int end, const Scale& c, float& most, double& sum, F&& each) {
     float m = -CUDART_INF_F, M = 0.0f;
     double s = 0.0;
-    over_vectors(x, runs.begin(warp), runs.end(warp, x.vectors), [&](const Vector<E>(&in)[kUnroll], int) {
-        float most = in[0].max();
-#pragma unroll
-        for (int k = 1; k < kUnroll; ++k) most = max_nan(most, in[k].max());
-        if (!(most <= m)) {
-            const float higher = c.base(most);
+    over_vectors(x, begin, end, [&](const Batch<E>& in, int) {
+        const float l = largest(in);
+        each(l);
+        if (!(l <= m)) {
+            const float higher = c.base(l);
             s = m == -CUDART_INF_F ? 0.0 : s * power(M - higher);
-            m = max_nan(m, most);
+            m = max_nan(m, l);
             M = higher;
         }
-        const Pair off = pair_of(-M, -M), hi = pair_of(c.hi, c.hi), lo = pair_of(c.lo, c.lo);
-        Pair sum[kUnroll];
-#pragma unroll
-        for (int k = 0; k < kUnroll; ++k) {
-            constexpr int P = Vector<E>::N / 2;
-            Pair e[P];
-#pragma unroll
-            for (int i = 0; i < P; ++i) {
-                float a, b;
-                split(fma2(in[k].at(i), lo, fma2(in[k].at(i), hi, off)), a, b);
-                e[i] = pair_of(exp2_fast(a), exp2_fast(b));
-            }
-            sum[k] = e[0] + e[1];
-            if constexpr (P == 4) sum[k] = sum[k] + (e[2] + e[3]);
-        }
-        float a, b;
-        split((sum[0] + sum[1]) + (sum[2] + sum[3]), a, b);
-        s += (double)(a + b);
+        s += (double)weights_of(in, c, M);
     });
-    const float most = warp_max_nan(m);
-    if (lane == 0) sh.most[warp] = most;
-    __syncthreads();
-    Total t = {sh.most[0], 0.0f, 0.0};
-#pragma unroll
-    for (int w = 1; w < T / 32; ++w) t.m = max_nan(t.m, sh.most[w]);
+    most = warp_max_nan(m);
+    sum = warp_sum(m == -CUDART_INF_F ? 0.0 : s * power(M - c.base(most)));
+}
+// What the warps left in sh.most and sh.sum, brought to one base.
+template <int T>
+__device__ __forceinline__ Total join_runs(Shared<T>& sh, int runs, const Scale& c) {
+    float m = -CUDART_INF_F;
+    for (int r = threadIdx.x & 31; r < runs; r += 32) m = max_nan(m, sh.most[r]);
+    Total t = {warp_max_nan(m), 0.0f, 0.0};
     t.M = c.base(t.m);
-    s = warp_sum(m == -CUDART_INF_F ? 0.0 : s * power(M - t.M));
-    if (lane == 0) sh.sum[warp] = s;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < T / 32; ++w) t.S += sh.sum[w];
+    for (int r = Team<T>::thread(); r < runs; r += T) sh.sum[r] *= power((sh.most[r] == -CUDART_INF_F ? -CUDART_INF_F : c.base(sh.most[r])) - t.M);
+    Team<T>::sync();
+    t.S = sum_of_runs(sh, runs);
     return t;
 }
-// .. in 64-bit weights, of what is kept; the number of those
+// The sums of the runs over what is kept, in 32-bit weights with base M; how many are kept.
 template <class E, int T>
-__device__ __noinline__ double exact_sums(const Row<E>& x, const Exact& w, const Cut& cut, Block<T>& sh, int& kept) {
-    const int warp = threadIdx.x >> 5;
-    const Runs<T> runs(x.vectors);
+__device__ __noinline__ double fast_sums(const Row<E>& x, const Scale& c, float M, const Cut cut, Shared<T>& sh, int& kept) {
+    const Runs runs(x.vectors, T / 32);
+    const int warp = Team<T>::warp();
     double s = 0.0;
     int n = 0;
-    over_elements(x, runs.begin(warp), runs.end(warp, x.vectors), [&](float y, int i) {
-        if (cut.keeps(y, i)) {
-            s += w.weight(y);
-            ++n;
+    over_vectors(x, runs.begin(warp), runs.end(warp), [&](const Batch<E>& given, int v) {
+        if (!(largest(given) >= cut.value)) return;
+        Batch<E> in;
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) in[k] = given[k];
+        mask(in, x, v, [&](float y, int i) {
+            const bool keep = cut.keeps(y, i);
+            n += keep;
+            return keep;
+        });
+        s += (double)weights_of(in, c, M);
+    });
+    s = warp_sum(s);
+    kept = team_sum<T>(n, sh);
+    if ((threadIdx.x & 31) == 0) sh.sum[warp] = s;
+    Team<T>::sync();
+    return sum_of_runs(sh, T / 32);
+}
+// .. in 64-bit weights
+template <class E, int T>
+__device__ __noinline__ double exact_sums(const Row<E>& x, const Exact& w, const Cut cut, Shared<T>& sh, int& kept) {
+    const Runs runs(x.vectors, T / 32);
+    const int warp = Team<T>::warp();
+    double s = 0.0;
+    int n = 0;
+    over_single(x, runs.begin(warp), runs.end(warp), [&](const Vector<E>& in, int v) {
+#pragma unroll 1                       // two weights at a time: more of them do not fit the registers
+        for (int i = 0; i < Vector<E>::N / 2; ++i) {
+            float y, z;
+            split(in.at(i), y, z);
+            const bool keep_y = cut.keeps(y, x.first(v) + 2 * i), keep_z = cut.keeps(z, x.first(v) + 2 * i + 1);
+            const double a = w.weight(y), b = w.weight(z);
+            s += (keep_y ? a : 0.0) + (keep_z ? b : 0.0);
+            n += keep_y + keep_z;
         }
     });
     s = warp_sum(s);
-    n = __reduce_add_sync(~0u, n);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) sh.sum[warp] = s, sh.count[warp] = n;
-    __syncthreads();
-    s = 0.0;
-    kept = 0;
-    for (int k = 0; k < T / 32; ++k) s += sh.sum[k], kept += sh.count[k];
-    return s;
+    kept = team_sum<T>(n, sh);
+    if ((threadIdx.x & 31) == 0) sh.sum[warp] = s;
+    Team<T>::sync();
+    return sum_of_runs(sh, T / 32);
 }
 
-// The first element at which the running sum exceeds `target`: the run by sh.sum, then the threads' parts of that run.  sh.found is the
-// element, or -1, and sh.before and sh.after are the sums on its two sides.
+// The first element at which the running sum exceeds `target`: the run by sh.sum, the thread's part of that run, the element.  sh.found is the
+// element, or -1, and sh.before and sh.after are the sums on its two sides.  weight(element, id); sums(vectors v .. v + 3 of one lane)
 template <class E, int T, class Weight>
-__device__ __forceinline__ void find(const Row<E>& x, double target, Block<T>& sh, Weight&& weight) {
-    const Runs<T> runs(x.vectors);
+__device__ __forceinline__ void find(const Row<E>& x, const Runs& runs, int n_runs, double target, Shared<T>& sh, Weight&& weight) {
+    const int lane = threadIdx.x & 31, tid = Team<T>::thread();
+    // the last run before which the sum does not exceed it, among those that weigh
+    double before = 0.0, from_run = 0.0;
     int run = 0;
-    double before = 0.0;
-    for (; run < T / 32 - 1 && before + sh.sum[run] <= target; ++run) before += sh.sum[run];
-    set_all(sh.found, -1);
-    const int begin = runs.begin(run), end = runs.end(run, x.vectors), per = (end - begin + T - 1) / T;
-    const int mine = begin + (int)threadIdx.x * per, stop = min(mine + per, end);
-    double s = 0.0;
-    int last = -1;
-    auto walk = [&](auto&& f) {
-        for (int v = mine; v < stop; ++v) {
-            const Vector<E> in = x.load(v);
-#pragma unroll
-            for (int e = 0; e < Vector<E>::N; ++e) f(in.one(e), x.first(v) + e);
+    for (int r0 = 0; r0 < n_runs; r0 += 32) {
+        const double s = r0 + lane < n_runs ? sh.sum[r0 + lane] : 0.0, in = warp_before(s), out = without_own(in);
+        const unsigned int here = __ballot_sync(~0u, s > 0.0 && before + out <= target);
+        if (here) {
+            const int l = 31 - __clz(here);
+            run = r0 + l;
+            from_run = before + __shfl_sync(~0u, out, l);
         }
-    };
-    walk([&](float y, int i) {
-        const double w = weight(y, i);
-        s += w;
-        if (w > 0.0) last = i;
-    });
-    double all;
-    const double from = before + block_before<T>(s, sh, all);
-    if (from <= target && target < from + s) {
-        double sum = from;
-        int at = -1;
-        walk([&](float y, int i) {
-            const double w = weight(y, i);
-            if (at < 0 || sum <= target) {               // the last of them, where roundings leave no other
-                if (w > 0.0) at = i, sh.before = sum, sh.after = sum + w;
-                sum += w;
+        before += __shfl_sync(~0u, in, 31);
+    }
+    const int begin = runs.begin(run), end = runs.end(run), per = (end - begin + T - 1) / T;
+    const int mine = begin + tid * per, stop = min(mine + per, end);
+    double s = 0.0;
+    for (int v = mine; v < stop; ++v) {
+        const Vector<E> in = x.load(v);
+        const int i = x.first(v);
+        double part = 0.0;
+#pragma unroll
+        for (int e = 0; e < Vector<E>::N; ++e) part += weight(in.one(e), i + e);
+        s += part;
+    }
+    const double from = from_run + team_before<T>(s, sh);
+    if (tid == 0) sh.found = -1, sh.lowest = -1;
+    Team<T>::sync();
+    if (s > 0.0 && from <= target) atomicMax(&sh.lowest, tid);
+    Team<T>::sync();
+    // that thread's elements, its warp's lanes side by side
+    const int owner = sh.lowest;
+    if (owner >= 0 && tid >> 5 == owner >> 5) {
+        double sum = __shfl_sync(~0u, from, owner & 31);
+        const int v0 = begin + owner * per, v1 = min(v0 + per, end);
+        int last = -1;
+        double last_before = 0.0, last_after = 0.0;
+        for (int i0 = max(x.first(v0), 0); i0 < min(x.first(v1), x.V); i0 += 32) {
+            const int i = i0 + lane;
+            const bool in_row = i < min(x.first(v1), x.V);
+            const double w = in_row ? weight(as_float(x.x[i]), i) : 0.0;
+            const double in = warp_before(w), out = without_own(in);
+            const unsigned int here = __ballot_sync(~0u, w > 0.0 && sum + out <= target);
+            if (here) {
+                const int l = 31 - __clz(here);
+                last = i0 + l;
+                last_before = sum + __shfl_sync(~0u, out, l), last_after = sum + __shfl_sync(~0u, in, l);
             }
-        });
-        sh.found = at;
+            sum += __shfl_sync(~0u, in, 31);
+        }
+        if (lane == 0) sh.found = last, sh.before = last_before, sh.after = last_after;
     }
-    __syncthreads();
-    if (sh.found < 0) {                                  // between two threads' sums, by rounding: the last that weighs
-        __syncthreads();
-        if (last >= 0 && from <= target) atomicMax(&sh.found, last);
-        if (threadIdx.x == 0) sh.before = sh.after = target;
-        __syncthreads();
-    }
+    Team<T>::sync();
 }
 
-// Drawn from what is kept, the row's own order, in 64 bits.  S: the sum over the whole row.
-struct Drawn {
-    int token;
-    double logprob, kept_logprob;
-};
+// Drawn from what is kept in 64 bits, sh.sum and C being its sums.  log2_S: of the whole row's sum.
 template <class E, int T>
-__device__ __noinline__ Drawn draw_exactly(const Row<E>& x, float m, float Temp, float u, Cut cut, double S, Block<T>& sh, int& kept) {
-    const Exact w(m, Temp);
-    const double C = exact_sums<E, T>(x, w, cut, sh, kept);
-    if (S <= 0.0) S = C;
-    find<E, T>(x, u * C, sh, [&](float y, int i) { return cut.keeps(y, i) ? w.weight(y) : 0.0; });
-    Drawn d = {sh.found, 0.0, 0.0};
-    const double z = d.token < 0 ? 0.0 : ((double)as_float(x.x[d.token]) - w.m) * w.by;
-    d.logprob = z - log(S), d.kept_logprob = z - log(C);
-    return d;
+__device__ __noinline__ void draw_exactly(const SampleArgs& a, int64_t row, const Row<E>& x, const Scale& c, const Exact& w, float u, const Cut cut, double log2_S, double C,
+                                          int kept, Shared<T>& sh) {
+    find<E, T>(x, Runs(x.vectors, T / 32), T / 32, u * C, sh, [&](float y, int i) { return cut.keeps(y, i) ? w.weight(y) : 0.0; });
+    if (Team<T>::thread() == 0) {
+        const int token = sh.found;
+        const double z = token < 0 ? 0.0 : ((double)as_float(x.x[token]) - w.m) * c.exact, log2_C = log2(C);
+        write(a, row, token, (float)((z - (log2_S == log2_S ? log2_S : log2_C)) * 0.6931471805599453), (float)((z - log2_C) * 0.6931471805599453), kept);
+    }
 }
-
 template <class E, int T>
-__device__ __forceinline__ void write_greedy(const SampleArgs& a, int64_t row, const Row<E>& x, float m, Block<T>& sh) {
-    set_all(sh.found, 0x7FFFFFFF);
-    const Runs<T> runs(x.vectors);
-    const int warp = threadIdx.x >> 5;
+__device__ __forceinline__ void write_greedy(const SampleArgs& a, int64_t row, const Row<E>& x, float m, Shared<T>& sh) {
+    set_all<T>(sh.found, 0x7FFFFFFF);
+    const Runs runs(x.vectors, T / 32);
     int first = 0x7FFFFFFF;
-    over_vectors(x, runs.begin(warp), runs.end(warp, x.vectors), [&](const Vector<E>(&in)[kUnroll], int v) {
+    over_vectors(x, runs.begin(Team<T>::warp()), runs.end(Team<T>::warp()), [&](const Batch<E>& in, int v) {
 #pragma unroll
         for (int k = 0; k < kUnroll; ++k)
             if (in[k].max() == m)
@@ -373,25 +531,62 @@ __device__ __forceinline__ void write_greedy(const SampleArgs& a, int64_t row, c
                     if (in[k].one(e) == m) first = min(first, x.first(v + k * 32) + e);
     });
     if (first != 0x7FFFFFFF) atomicMin(&sh.found, first);
-    __syncthreads();
-    if (threadIdx.x == 0) write(a, row, sh.found, 0.0f, 0.0f, 1);
+    Team<T>::sync();
+    if (Team<T>::thread() == 0) write(a, row, sh.found, 0.0f, 0.0f, 1);
 }
+
+// The team's row, and in a cluster the part of it that the block takes.
+template <int T>
+struct Place {
+    int rank = 0, blocks = 1;
+    int64_t row;
+    __device__ __forceinline__ Place() : row((int64_t)blockIdx.x * Team<T>::kPerBlock + Team<T>::index()) {
+        if constexpr (T == 512) {
+            rank = (int)cg::this_cluster().block_rank(), blocks = (int)cg::this_cluster().num_blocks();
+            row = blockIdx.x / blocks;
+        }
+    }
+    __device__ __forceinline__ int run() const { return rank * (T / 32) + Team<T>::warp(); }
+    __device__ __forceinline__ int runs() const { return blocks * (T / 32); }
+    // a barrier of all that work on the row
+    __device__ __forceinline__ void sync() const {
+        if (T == 512 && blocks > 1) cg::this_cluster().sync();
+        else Team<T>::sync();
+    }
+    template <class P>
+    __device__ __forceinline__ P* of_block(P* p, int r) const {
+        if constexpr (T == 512)
+            if (blocks > 1) return cg::this_cluster().map_shared_rank(p, r);
+        return p;
+    }
+};
 
 // ---- the whole distribution ----
 template <class E, int T>
-__global__ void __launch_bounds__(T) draw_kernel(SampleArgs a) {
-    __shared__ Block<T> sh;
-    const int64_t row = blockIdx.x;
+__global__ void __launch_bounds__(T == 32 ? 128 : T) draw_kernel(SampleArgs a) {
+    __shared__ Shared<T> shared[Team<T>::kPerBlock];
+    Shared<T>& sh = shared[Team<T>::index()];
+    const Place<T> at;
+    const int64_t row = at.row;
+    if (row >= a.rows) return;
     const Asked r = asked_of<false>(a, row);
     if (r.kind) {
-        if (threadIdx.x == 0) write_none(a, row, r.kind, 0.0f);
+        if (at.rank == 0 && Team<T>::thread() == 0) write_none(a, row, r.kind, 0.0f);
         return;
     }
     const Row<E> x(static_cast<const E*>(a.logits) + row * a.stride, a.vocab);
     const Scale c(r.T == 0.0f ? 1.0f : r.T);
-    const Total t = sums_of_row<E, T>(x, c, sh);
+    const Runs runs(x.vectors, at.runs());
+    float most;
+    double sum;
+    sum_run(x, runs.begin(at.run()), runs.end(at.run()), c, most, sum, [](float) {});
+    if (T == 512 && at.blocks > 1) at.sync();                  // every block has begun
+    if ((threadIdx.x & 31) == 0) at.of_block(sh.most, 0)[at.run()] = most, at.of_block(sh.sum, 0)[at.run()] = sum;
+    at.sync();
+    if (at.rank) return;
+    const Total t = join_runs(sh, at.runs(), c);
     if (!is_finite(t.m)) {
-        if (threadIdx.x == 0) write_none(a, row, 0, t.m);
+        if (Team<T>::thread() == 0) write_none(a, row, 0, t.m);
         return;
     }
     if (r.T == 0.0f) {
@@ -399,169 +594,193 @@ __global__ void __launch_bounds__(T) draw_kernel(SampleArgs a) {
         return;
     }
     if (c.holds(t.m)) {
-        const double target = r.u * t.S, margin = c.error(a.vocab, t.S) * t.S;
-        find<E, T>(x, target, sh, [&](float y, int) { return (double)c.weight(y, t.M); });
+        const double target = r.u * t.S, margin = Error(a.vocab, t.S).at(r.u) * t.S;
+        find<E, T>(x, runs, at.runs(), target, sh, [&](float y, int) { return (double)c.weight(y, t.M); });
         const int token = sh.found;
         if (token >= 0 && target - sh.before >= margin && sh.after - target >= margin) {
-            if (threadIdx.x == 0) {
-                const float logprob = (float)(((double)as_float(x.x[token]) * c.c - t.M - log2(t.S)) * 0.6931471805599453);
+            if (Team<T>::thread() == 0) {
+                const double log2_S = log2(t.S) - c.of_largest(t.m, t.M);
+                const float logprob = (float)((((double)as_float(x.x[token]) - t.m) * c.exact - log2_S) * 0.6931471805599453);
                 write(a, row, token, logprob, logprob, 0);
             }
             return;
         }
-        __syncthreads();
+        Team<T>::sync();
     }
-    int kept;
-    const Drawn d = draw_exactly<E, T>(x, t.m, r.T, r.u, Cut{-CUDART_INF_F, 0}, 0.0, sh, kept);
-    if (threadIdx.x == 0) write(a, row, d.token, (float)d.logprob, (float)d.logprob, 0);
+    fill_table(sh);
+    const Exact w(t.m, c, sh.table);
+    int everything;
+    const double S = exact_sums<E, T>(x, w, unmasked(), sh, everything);
+    draw_exactly<E, T>(a, row, x, c, w, r.u, unmasked(), CUDART_NAN, S, 0, sh);
 }
 
 // ---- what is kept ----
 
-// Keys fall from list[0] to list[n - 1]; n <= kListed.
+// The list by rank, which is how many other keys are above: ids and weights.  No two keys are equal.
 template <int T>
-__device__ __forceinline__ void sort_list(unsigned long long* list, int n) {
+__device__ __forceinline__ void rank_list(Lists<T>& lists, int n, const Exact& w) {
+    for (int i = Team<T>::thread(); i < n; i += T) {
+        const unsigned long long mine = lists.key[i];
+        int rank = 0;
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) rank += lists.key[j] > mine;
+        lists.id[rank] = position_of(mine);
+        lists.weight[rank] = w.weight(value_of((uint32_t)(mine >> 32)));
+    }
+    Team<T>::sync();
+}
+// Keys fall from key[0] to key[n - 1].
+template <int T>
+__device__ __forceinline__ void sort_list(unsigned long long* key, int n) {
     int size = 32;
     while (size < n) size *= 2;
-    for (int i = n + threadIdx.x; i < size; i += T) list[i] = 0;
+    for (int i = n + Team<T>::thread(); i < size; i += T) key[i] = 0;
     for (int k = 2; k <= size; k *= 2)
         for (int j = k / 2; j; j /= 2) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < size / 2; i += T) {
+            Team<T>::sync();
+            for (int i = Team<T>::thread(); i < size / 2; i += T) {
                 const int p = 2 * i - (i & (j - 1)), q = p + j;
-                const unsigned long long x = list[p], y = list[q];
-                if ((x < y) == !(p & k)) list[p] = y, list[q] = x;
+                const unsigned long long x = key[p], y = key[q];
+                if ((x < y) == !(p & k)) key[p] = y, key[q] = x;
             }
         }
-    __syncthreads();
+    Team<T>::sync();
 }
 
-// Looks for the border of what is kept.
-//
-// The row's elements are counted in intervals of 1/64 of an octave of their weight, from the largest down.  The counts bound the running sum
-// over the order from both sides, within 1.1 % of what lies above or below; so the border lies in few intervals.  The elements that
-// may be kept, or, where those are too many, the ones of the intervals in question, are listed and sorted.  What is still too many for
-// that is halved at the middle of their values, as often as it takes; if all are equal, the border is a matter of their ids.
+// Intervals of the exponents t <= 0 of weights 2^t, from 0 down, kBins in 64 octaves.  With an interval's count goes the sum of what its exponents are
+// beyond its beginning, in 256ths of it.  The sum of its weights then lies between the count times the weight at the mean exponent and what the chord
+// over the interval gives: 6e-5 more at 32 an octave.
+template <int kBins>
+struct Intervals {
+    static constexpr int kPerOctave = kBins / 64, kParts = 256;
+    // to the nearest 256th: falls with the exponent, -inf last
+    static __device__ __forceinline__ int depth(float t) {
+        const float d = fminf(t * -(float)(kPerOctave * kParts), kBins * kParts - 1.0f);
+        return __float_as_int(d + 12582912.0f) - 0x4B400000;      // 1.5 x 2^23
+    }
+    struct Bounds {
+        double least, most;
+    };
+    static __device__ __forceinline__ Bounds sum_of(int b, uint32_t count, uint32_t parts) {
+        if (count == 0) return {0.0, 0.0};
+        constexpr float per = 1.0f / kPerOctave;
+        // the roundings to 256ths, of exponents of up to 64 in 32 bits, and of this
+        constexpr double slack = 0.36 / (kParts * kPerOctave) + 1.6e-5;
+        const double n = count;
+        const float mean = __fdividef((float)parts, (float)count) * (1.0f / kParts), first = exp2_fast(b * -per), next = exp2_fast((b + 1) * -per);
+        // the last interval goes on to 0
+        return {b == kBins - 1 ? 0.0 : n * exp2_fast((b + mean) * -per) * (1.0 - slack), n * (first + (next - first) * mean) * (1.0 + slack)};
+    }
+};
+
+// Looks for the border of what is kept: the intervals, an interval or two, in which it lies; the elements of those, listed and sorted.  What is
+// too many for that is halved at the middle of its values, as often as it takes; if all are equal, the border is a matter of their ids.
 template <class E, int T>
 struct Search {
+    static constexpr int kBins = Sizes<T>::kBins, kListed = Sizes<T>::kListed;
+    using In = Intervals<kBins>;
     const Row<E>& x;
     const Scale& c;
     const Exact w;
-    const float M;
-    const bool holds;
-    const double shift;            // log2 of the 64-bit weight of what weighs 1 with base M
-    Block<T>& sh;
-    Lists& lists;
-    int begin, end;                // the warp's run
+    const float m;
+    Shared<T>& sh;
+    Lists<T>& lists;
+    const Runs runs;
 
-    __device__ __forceinline__ Search(const Row<E>& x, const Scale& c, float Temp, const Total& t, Block<T>& sh, Lists& lists)
-        : x(x), c(c), w(t.m, Temp), M(t.M), holds(c.holds(t.m)), shift(holds ? t.M - (double)t.m * c.c : 0.0), sh(sh), lists(lists) {
-        const Runs<T> runs(x.vectors);
-        begin = runs.begin(threadIdx.x >> 5), end = runs.end(threadIdx.x >> 5, x.vectors);
-    }
-    // Falls with the value, masked ones last.
-    __device__ __forceinline__ int bin(float y) const {
-        const float t = holds ? c.exponent(y, M) : (float)(((double)y - w.m) * c.c);
-        return (int)fminf(t * -64.0f, kBins - 1.0f);
-    }
-    // bounds of the weight in interval b, with base M; the exponents' roundings, 2^-17 at 64, and the exponential's included
-    static __device__ __forceinline__ float most(int b) { return exp2_fast(b * -0.015625f) * 1.00004f; }
-    static __device__ __forceinline__ float least(int b) { return b == kBins - 1 ? 0.0f : exp2_fast((b + 1) * -0.015625f) * 0.99996f; }
+    __device__ __forceinline__ Search(const Row<E>& x, const Scale& c, const Total& t, Shared<T>& sh, Lists<T>& lists)
+        : x(x), c(c), w(t.m, c, sh.table), m(t.m), sh(sh), lists(lists), runs(x.vectors, T / 32) {}
+    __device__ __forceinline__ int begin() const { return runs.begin(Team<T>::warp()); }
+    __device__ __forceinline__ int end() const { return runs.end(Team<T>::warp()); }
+    // Of the exponent below the largest element's, for which 32 bits do.
+    __device__ __forceinline__ int depth(float y) const { return In::depth((y - m) * c.c); }
+    __device__ __forceinline__ int bin(float y) const { return depth(y) / In::kParts; }
 
-    __device__ __forceinline__ void count(const Cut& in) {
-        __syncthreads();
-        for (int b = threadIdx.x; b < kBins; b += T) lists.hist[b] = 0;
-        __syncthreads();
-        over_elements(x, begin, end, [&](float y, int i) {
-            if (in.keeps(y, i)) atomicAdd(&lists.hist[bin(y)], 1u);
+    __device__ __forceinline__ void count(const Cut in, bool parts) {
+        Team<T>::sync();
+        for (int b = Team<T>::thread(); b < kBins; b += T) lists.hist[b] = lists.parts[b] = 0;
+        Team<T>::sync();
+        over_elements(x, begin(), end(), [&](float y, int i) {
+            if (!in.keeps(y, i)) return;
+            const int d = depth(y);
+            atomicAdd(&lists.hist[d / In::kParts], 1u);
+            if (parts) atomicAdd(&lists.parts[d / In::kParts], (uint32_t)(d % In::kParts));
         });
-        __syncthreads();
+        Team<T>::sync();
     }
     // The first interval up to which there are n elements (sh.highest), how many there are before it (sh.before_it) and in it (sh.listed);
     // without so many, the last one.
     __device__ __forceinline__ void reach(int n) {
         constexpr int per = kBins / T;
-        const int b0 = threadIdx.x * per;
+        const int b0 = Team<T>::thread() * per;
         int mine = 0;
         for (int b = b0; b < b0 + per; ++b) mine += lists.hist[b];
-        int sum = block_before<T>(mine, sh);
-        if (sum < n && (sum + mine >= n || threadIdx.x == T - 1)) {
+        int sum = team_before<T>(mine, sh);
+        if (sum < n && (sum + mine >= n || Team<T>::thread() == T - 1)) {
             int b = b0;
             for (; b < b0 + per - 1 && sum + (int)lists.hist[b] < n; ++b) sum += lists.hist[b];
             sh.lowest = sh.highest = b, sh.before_it = sum, sh.listed = lists.hist[b];
         }
-        __syncthreads();
+        Team<T>::sync();
     }
-    // The intervals sh.lowest to sh.highest in which the running sum reaches B; the elements before and in them.  B and S, the sum of all, with
-    // base M, S to `slack` of itself.
-    __device__ __forceinline__ void bracket(double B, double S, double slack) {
+    // The intervals sh.lowest to sh.highest in which the running sum reaches B, which is known to `margin`; the elements before and in them.
+    __device__ __forceinline__ void bracket(double B, double margin) {
         constexpr int per = kBins / T;
-        const int b0 = threadIdx.x * per;
-        double hi = 0.0, lo = 0.0, all_hi, all_lo;
-        for (int b = b0; b < b0 + per; ++b) hi += (double)lists.hist[b] * most(b), lo += (double)lists.hist[b] * least(b);
-        double sum_hi = block_before<T>(hi, sh, all_hi), sum_lo = block_before<T>(lo, sh, all_lo);
-        if (threadIdx.x == 0) sh.lowest = sh.highest = kBins - 1;
-        __syncthreads();
-        const double least_B = B - S * slack, most_B = B + S * slack;
+        const int b0 = Team<T>::thread() * per;
+        auto sum_of = [&](int b) { return In::sum_of(b, lists.hist[b], lists.parts[b]); };
+        double hi = 0.0, lo = 0.0;
         for (int b = b0; b < b0 + per; ++b) {
-            const double h = lists.hist[b];
-            sum_hi += h * most(b), sum_lo += h * least(b);
-            if (sum_hi >= least_B) atomicMin(&sh.lowest, b);
-            if (fmax(sum_lo, S * (1.0 - slack) - fmax(all_hi - sum_hi, 0.0) * (1.0 + 1e-12) - all_hi * 1e-14) >= most_B) atomicMin(&sh.highest, b);
+            const auto s = sum_of(b);
+            hi += s.most, lo += s.least;
         }
-        __syncthreads();
+        double sum_hi = team_before<T>(hi, sh), sum_lo = team_before<T>(lo, sh);
+        if (Team<T>::thread() == 0) sh.lowest = sh.highest = kBins - 1;
+        Team<T>::sync();
+        if (sum_hi + hi >= B - margin || sum_lo + lo >= B + margin)
+            for (int b = b0; b < b0 + per; ++b) {
+                const auto s = sum_of(b);
+                sum_hi += s.most, sum_lo += s.least;
+                if (sum_hi >= B - margin) atomicMin(&sh.lowest, b);
+                if (sum_lo >= B + margin) atomicMin(&sh.highest, b);
+                if (sum_lo >= B + margin) break;
+            }
+        Team<T>::sync();
         int before = 0, inside = 0;
         const int first = min(sh.lowest, sh.highest), last = sh.highest;
         for (int b = b0; b < b0 + per; ++b) (b < first ? before : inside) += b <= last ? lists.hist[b] : 0;
-        const double all_before = block_sum<T>((double)before, sh), all_inside = block_sum<T>((double)inside, sh);
-        if (threadIdx.x == 0) sh.lowest = first, sh.before_it = (int)all_before, sh.listed = (int)all_inside;
-        __syncthreads();
+        before = team_sum<T>(before, sh), inside = team_sum<T>(inside, sh);
+        Team<T>::sync();
+        if (Team<T>::thread() == 0) sh.lowest = first, sh.before_it = before, sh.listed = inside;
+        Team<T>::sync();
     }
 
-    // f(element, id) for the elements of `in` from interval lo to hi
-    template <class F>
-    __device__ __forceinline__ void over_bins(const Cut& in, int lo, int hi, F&& f) {
-        over_vectors(x, begin, end, [&](const Vector<E>(&v)[kUnroll], int at) {
-#pragma unroll
-            for (int k = 0; k < kUnroll; ++k) {
-                if (bin(v[k].max()) > hi) continue;
-#pragma unroll
-                for (int e = 0; e < Vector<E>::N; ++e) {
-                    const float y = v[k].one(e);
-                    const int i = x.first(at + k * 32) + e, b = bin(y);
-                    if (in.keeps(y, i) && b >= lo && b <= hi) f(y, i);
-                }
-            }
-        });
-    }
     __device__ __forceinline__ void append(float y, int i) {
         const int n = atomicAdd(&sh.listed, 1);
         if (n < kListed) lists.key[n] = key_of(y, i);
     }
-    // .. listed and sorted: how many there are, at most kListed
-    __device__ __forceinline__ int list(const Cut& in, int lo, int hi) {
-        set_all(sh.listed, 0);
-        over_bins(in, lo, hi, [&](float y, int i) { append(y, i); });
-        __syncthreads();
-        const int n = min(sh.listed, kListed);
-        sort_list<T>(lists.key, n);
-        return n;
+    // Everything down to interval `hi`, which is as much as a list holds.
+    __device__ __noinline__ void list(int hi) {
+        set_all<T>(sh.listed, 0);
+        over_vectors(x, begin(), end(), [&](const Batch<E>& in, int v) {
+            if (bin(largest(in)) > hi) return;
+#pragma unroll
+            for (int k = 0; k < kUnroll; ++k)
+#pragma unroll
+                for (int e = 0; e < Vector<E>::N; ++e)
+                    if (in[k].one(e) > -CUDART_INF_F && bin(in[k].one(e)) <= hi) append(in[k].one(e), x.first(v + k * 32) + e);
+        });
+        Team<T>::sync();
     }
     __device__ __forceinline__ float value(int i) const { return value_of((uint32_t)(lists.key[i] >> 32)); }
     __device__ __forceinline__ Cut cut_at(int i) const { return {value(i), position_of(lists.key[i])}; }
-    __device__ __forceinline__ void weigh(int n) {
-        for (int i = threadIdx.x; i < n; i += T) lists.weight[i] = w.weight(value(i));
-        __syncthreads();
-    }
     // The first of n places at which above + the running sum of lists.weight reaches B, or exceeds it; the last if none does.  sh.before and
     // sh.after: the sums on its two sides.
     template <bool kExceeds>
     __device__ __forceinline__ int reach_in_list(int n, double above, double B) {
-        const int per = (n + T - 1) / T, i0 = min((int)threadIdx.x * per, n), i1 = min(i0 + per, n);
-        double mine = 0.0, all;
+        const int per = (n + T - 1) / T, i0 = min(Team<T>::thread() * per, n), i1 = min(i0 + per, n);
+        double mine = 0.0;
         for (int i = i0; i < i1; ++i) mine += lists.weight[i];
-        const double from = above + block_before<T>(mine, sh, all);
-        set_all(sh.found, n - 1);
+        const double from = above + team_before<T>(mine, sh);
+        set_all<T>(sh.found, n - 1);
         double sum = from;
         for (int i = i0; i < i1; ++i) {
             sum += lists.weight[i];
@@ -570,42 +789,69 @@ struct Search {
                 break;
             }
         }
-        __syncthreads();
+        Team<T>::sync();
         const int at = sh.found;
         if (at >= i0 && at < i1) {
             sum = from;
             for (int i = i0; i < at; ++i) sum += lists.weight[i];
             sh.before = sum, sh.after = sum + lists.weight[at];
         }
-        __syncthreads();
+        Team<T>::sync();
         return at;
     }
 
-    // The border in intervals sh.lowest to sh.highest: of the first k elements (k > 0), or of those whose sum reaches B in 64-bit weights.
-    __device__ __noinline__ Cut border(const Cut& in, int k, double B) {
+    // The border in intervals sh.lowest to sh.highest: of the first k elements of `in`, or (k = 0) of those whose sum reaches p times that of `in`,
+    // in 64-bit weights.  With k = 0, `of` is that sum, and C and `kept` are the sum and the number of what is kept, sh.sum the runs' sums of it, unless
+    // C is NaN.
+    __device__ __noinline__ Cut border(const Cut in, int k, double p, double& of, double& C, int& kept) {
         const int lo = sh.lowest, hi = sh.highest;
         int above = sh.before_it, n = sh.listed;
-        __syncthreads();
-        // what lies above, and the range of what is in question
-        double A = 0.0;
+        Team<T>::sync();
+        if (Team<T>::thread() == 0) sh.key_low = 0xFFFFFFFFu, sh.key_high = 0, sh.listed = 0;
+        Team<T>::sync();
+        const bool fits = n <= kListed;
+        double S = 0.0, A = 0.0, B = 0.0;
+        uint32_t low = 0xFFFFFFFFu, high = 0;
+        C = CUDART_NAN;
+        over_single(x, begin(), end(), [&](const Vector<E>& v, int at) {
+            if (k && bin(v.max()) > hi) return;
+#pragma unroll 1
+            for (int q = 0; q < Vector<E>::N / 2; ++q) {
+                float y, z;
+                split(v.at(q), y, z);
+                const int id = x.first(at) + 2 * q;
+                const int b_y = in.keeps(y, id) ? bin(y) : kBins, b_z = in.keeps(z, id + 1) ? bin(z) : kBins;
+                if (k == 0) {
+                    const double one = w.weight(y), two = w.weight(z);
+                    S += (b_y < kBins ? one : 0.0) + (b_z < kBins ? two : 0.0);
+                    A += (b_y < lo ? one : 0.0) + (b_z < lo ? two : 0.0);
+                }
+                auto take = [&](float value, int i, int b) {
+                    if (b < lo || b > hi) return;
+                    if (fits) append(value, i);
+                    else low = min(low, order_of(value)), high = max(high, order_of(value));
+                };
+                take(y, id, b_y), take(z, id + 1, b_z);
+            }
+        });
         if (k == 0) {
-            if (lo > 0) over_bins(in, 0, lo - 1, [&](float y, int) { A += w.weight(y); });
-            A = block_sum<T>(A, sh);
+            of = team_sum<T>(S, sh);
+            B = p * of;
+            A = warp_sum(A);
+            if ((threadIdx.x & 31) == 0) sh.sum[Team<T>::warp()] = A;
+            Team<T>::sync();
+            A = sum_of_runs(sh, T / 32);
         }
-        if (n > kListed) {
-            if (threadIdx.x == 0) sh.key_low = 0xFFFFFFFFu, sh.key_high = 0;
-            __syncthreads();
-            uint32_t low = 0xFFFFFFFFu, high = 0;
-            over_bins(in, lo, hi, [&](float y, int) { low = min(low, order_of(y)), high = max(high, order_of(y)); });
+        if (!fits) {
             atomicMin(&sh.key_low, low), atomicMax(&sh.key_high, high);
-            __syncthreads();
+            Team<T>::sync();
             uint32_t bottom = sh.key_low, top = sh.key_high;
             while (n > kListed && bottom < top) {
                 const uint32_t middle = bottom + (top - bottom) / 2;       // the upper half: above it
                 double s = 0.0;
                 int upper = 0;
                 low = 0xFFFFFFFFu, high = 0;
-                over_elements(x, begin, end, [&](float y, int i) {
+                over_elements(x, begin(), end(), [&](float y, int i) {
                     const uint32_t o = order_of(y);
                     if (o < bottom || o > top || !in.keeps(y, i)) return;
                     if (o > middle) {
@@ -616,32 +862,32 @@ struct Search {
                         high = max(high, o);
                     }
                 });
-                const int uppers = (int)block_sum<T>((double)upper, sh);
-                s = block_sum<T>(s, sh);
-                if (threadIdx.x == 0) sh.key_low = 0xFFFFFFFFu, sh.key_high = 0;
-                __syncthreads();
+                upper = team_sum<T>(upper, sh);
+                s = team_sum<T>(s, sh);
+                Team<T>::sync();
+                if (Team<T>::thread() == 0) sh.key_low = 0xFFFFFFFFu, sh.key_high = 0;
+                Team<T>::sync();
                 atomicMin(&sh.key_low, low), atomicMax(&sh.key_high, high);
-                __syncthreads();
-                if (k ? above + uppers >= k : A + s >= B) bottom = sh.key_low, n = uppers;
-                else top = sh.key_high, above += uppers, n -= uppers, A += s;
+                Team<T>::sync();
+                if (k ? above + upper >= k : A + s >= B) bottom = sh.key_low, n = upper;
+                else top = sh.key_high, above += upper, n -= upper, A += s;
             }
             if (bottom == top) {
                 // all equal: the border is the id of the last one that is kept
                 const float v = value_of(top);
-                const double each = w.weight(v);
-                const int wanted = k ? k - above : (int)fmin(fmax(ceil((B - A) / each), 1.0), (double)n);
+                const int wanted = k ? k - above : (int)fmin(fmax(ceil((B - A) / w.weight(v)), 1.0), (double)n);
                 int mine = 0;
-                over_elements(x, begin, end, [&](float y, int i) { mine += y == v && in.keeps(y, i); });
+                over_elements(x, begin(), end(), [&](float y, int i) { mine += y == v && in.keeps(y, i); });
                 mine = __reduce_add_sync(~0u, mine);
-                __syncthreads();
-                if ((threadIdx.x & 31) == 0) sh.count[threadIdx.x >> 5] = mine;
-                set_all(sh.found, 0);
+                Team<T>::sync();
+                if ((threadIdx.x & 31) == 0) sh.count[Team<T>::warp()] = mine;
+                set_all<T>(sh.found, 0);
                 int before = 0;
-                for (int r = 0; r < (int)(threadIdx.x >> 5); ++r) before += sh.count[r];
+                for (int r = 0; r < Team<T>::warp(); ++r) before += sh.count[r];
                 if (before < wanted && before + mine >= wanted)            // in this warp's run
-                    for (int v0 = begin; v0 < end && before < wanted; v0 += 32) {
+                    for (int v0 = begin(); v0 < end() && before < wanted; v0 += 32) {
                         const int at = v0 + (threadIdx.x & 31);
-                        const Vector<E> in_v = at < end ? x.load(at) : Row<E>::nothing();
+                        const Vector<E> in_v = at < end() ? x.load(at) : Row<E>::nothing();
                         auto is = [&](int e) { return in_v.one(e) == v && in.keeps(v, x.first(at) + e); };
                         int equal = 0;
 #pragma unroll
@@ -654,173 +900,435 @@ struct Search {
                                 if (is(e) && ++rank == wanted) sh.found = x.first(at) + e;
                         before += __shfl_sync(~0u, up_to, 31);
                     }
-                __syncthreads();
+                Team<T>::sync();
                 return {v, (uint32_t)sh.found};
             }
-            set_all(sh.listed, 0);
-            over_elements(x, begin, end, [&](float y, int i) {
+            set_all<T>(sh.listed, 0);
+            over_elements(x, begin(), end(), [&](float y, int i) {
                 const uint32_t o = order_of(y);
                 if (o >= bottom && o <= top && in.keeps(y, i)) append(y, i);
             });
-            __syncthreads();
-            n = min(sh.listed, kListed);
-            sort_list<T>(lists.key, n);
-        } else {
-            n = list(in, lo, hi);
         }
+        Team<T>::sync();
+        n = min(sh.listed, kListed);
+        sort_list<T>(lists.key, n);
         if (k) return cut_at(min(k - above, n) - 1);
-        weigh(n);
-        return cut_at(reach_in_list<false>(n, A, B));
+        for (int i = Team<T>::thread(); i < n; i += T) lists.weight[i] = w.weight(value(i));
+        Team<T>::sync();
+        const int at = reach_in_list<false>(n, A, B);
+        if (fits) {
+            // those of the list that are kept, to their runs
+            double s = 0.0;
+            for (int i = threadIdx.x & 31; i <= at; i += 32)
+                if (((int)position_of(lists.key[i]) + x.skip) / Vector<E>::N / runs.per == Team<T>::warp()) s += lists.weight[i];
+            s = warp_sum(s);
+            if ((threadIdx.x & 31) == 0) sh.sum[Team<T>::warp()] += s;
+            Team<T>::sync();
+            C = sum_of_runs(sh, T / 32);
+            kept = above + at + 1;
+        }
+        return cut_at(at);
     }
 };
 
-__device__ __forceinline__ Cut tighter(const Cut& a, const Cut& b) {
-    return a.value > b.value || (a.value == b.value && a.last < b.last) ? a : b;
+// Rows of which more is kept than a list holds.  `counted`: by_count's, or of everything, are the counts that the search has.
+template <class E, int T>
+__device__ __noinline__ void draw_from_many(const SampleArgs& a, int64_t row, const Row<E>& x, const Scale& c, const Asked& r, const Total& t, bool by_count, bool counted,
+                                            Shared<T>& sh, Lists<T>& lists) {
+    const bool by_sum = r.p < 1.0f, by_size = r.q > 0.0f;
+    fill_table(sh);
+    Search<E, T> search(x, c, t, sh, lists);
+    const Exact& w = search.w;
+    const bool holds = c.holds(t.m);
+    const double one = c.of_largest(t.m, t.M), to_largest = exp2(-one);      // where they hold
+    Cut cut = unmasked();
+    double log2_S = holds ? log2(t.S) - one : CUDART_NAN, of, C = CUDART_NAN;
+    int n = 0;
+    if (!holds && (by_count || by_size)) log2_S = log2(exact_sums<E, T>(x, w, unmasked(), sh, n));
+    if (by_count) {
+        if (!counted) search.count(unmasked(), false);
+        search.reach(r.k);
+        cut = search.border(unmasked(), r.k, 0.0, of, C, n);
+    }
+    if (by_sum) {
+        const Cut in = cut;
+        double about = t.S, error = 1e-13;
+        if (!holds) {
+            about = exact_sums<E, T>(x, w, in, sh, n);
+        } else {
+            if (by_count) about = fast_sums<E, T>(x, c, t.M, in, sh, n);
+            error = Error(a.vocab, about).both();
+            about *= to_largest;
+        }
+        if (by_count || !counted) search.count(in, true);
+        search.bracket(r.p * about, 2.0 * error * about);
+        cut = tighter(in, search.border(in, 0, r.p, of, C, n));
+        if (!by_count) log2_S = log2(of);
+    }
+    if (by_size) {
+        float f = __double2float_ru((double)t.m + (double)r.T * log((double)r.q));
+        if (w.weight(f) < r.q) f = nextafterf(f, CUDART_INF_F);
+        else if (w.weight(nextafterf(f, -CUDART_INF_F)) >= r.q) f = nextafterf(f, -CUDART_INF_F);
+        const Cut least = {fminf(f, t.m), 0xFFFFFFFFu}, both = tighter(cut, least);
+        if (both.value != cut.value || both.last != cut.last) C = CUDART_NAN;
+        cut = both;
+    }
+    if (holds && C != C) {
+        C = fast_sums<E, T>(x, c, t.M, cut, sh, n);
+        const double target = r.u * C, margin = Error(a.vocab, C).at(r.u) * C;
+        find<E, T>(x, search.runs, T / 32, target, sh, [&](float y, int i) { return cut.keeps(y, i) ? (double)c.weight(y, t.M) : 0.0; });
+        const int token = sh.found;
+        if (token >= 0 && target - sh.before >= margin && sh.after - target >= margin) {
+            if (Team<T>::thread() == 0) {
+                const double z = ((double)as_float(x.x[token]) - t.m) * c.exact, log2_C = log2(C) - one;
+                write(a, row, token, (float)((z - log2_S) * 0.6931471805599453), (float)((z - log2_C) * 0.6931471805599453), n);
+            }
+            return;
+        }
+        Team<T>::sync();
+        C = CUDART_NAN;
+    }
+    if (C != C) C = exact_sums<E, T>(x, w, cut, sh, n);
+    draw_exactly<E, T>(a, row, x, c, w, r.u, cut, log2_S, C, n, sh);
 }
 
-// ---- with filters ----
+// Draws from a list of n elements that holds all that may be kept.  Of a share top_p alone it may fall short (unless `all_sizes`: min_p
+// keeps nothing below it): false then.
 template <class E, int T>
-__global__ void __launch_bounds__(T) filter_kernel(SampleArgs a) {
-    __shared__ Block<T> sh;
+__device__ __noinline__ bool draw_from_list(const SampleArgs& a, int64_t row, const Row<E>& x, const Scale& c, const Asked& r, const Total& t, int n, bool by_count, bool all_sizes,
+                                            Shared<T>& sh, Lists<T>& lists) {
+    constexpr int kListed = Sizes<T>::kListed, kRanked = T == 32 ? 64 : 256;
+    const bool by_sum = r.p < 1.0f, by_size = r.q > 0.0f;
+    const int tid = Team<T>::thread();
+    if (n == 0) return false;
+    fill_table(sh);
+    Search<E, T> search(x, c, t, sh, lists);
+    const Exact& w = search.w;
+    // by rank: ids and weights
+    if (n <= kRanked) {
+        rank_list<T>(lists, n, w);
+    } else {
+        sort_list<T>(lists.key, n);
+        for (int i = tid; i < n; i += T) {
+            lists.id[i] = position_of(lists.key[i]);
+            lists.weight[i] = w.weight(search.value(i));
+        }
+        Team<T>::sync();
+    }
+    double S = t.S * exp2(-c.of_largest(t.m, t.M));                // in 64-bit weights, to the error of its 32-bit ones
+    int L = by_count ? min(r.k, n) : n;
+    if (by_sum) {
+        double of = S;
+        if (by_count) {
+            double mine = 0.0;
+            for (int i = tid; i < L; i += T) mine += lists.weight[i];
+            of = team_sum<T>(mine, sh);
+        }
+        int last = search.template reach_in_list<false>(L, 0.0, r.p * of);
+        if (!by_count) {
+            const double margin = Error(a.vocab, t.S).both() * S;
+            if (!all_sizes && sh.after < r.p * of - margin) return false;
+            if (r.p * of - sh.before < margin || fabs(sh.after - r.p * of) < margin) {
+                int everything;
+                S = exact_sums<E, T>(x, w, unmasked(), sh, everything);
+                last = search.template reach_in_list<false>(L, 0.0, r.p * S);
+                if (!all_sizes && sh.after < r.p * S) return false;
+            }
+        }
+        L = last + 1;
+    }
+    if (by_size) {
+        set_all<T>(sh.found, L);
+        for (int i = tid; i < L; i += T)
+            if (lists.weight[i] < r.q) {
+                atomicMin(&sh.found, i);
+                break;
+            }
+        Team<T>::sync();
+        L = max(sh.found, 1);
+    }
+    double mine = 0.0;
+    for (int i = tid; i < L; i += T) mine += lists.weight[i];
+    const double C = team_sum<T>(mine, sh), target = r.u * C;
+    // by id: of the tokens before which the sum does not exceed the target the last
+    set_all<T>(sh.found, -1);
+    if (L <= kRanked) {
+        for (int i = tid; i < L; i += T) {
+            const uint32_t id = lists.id[i];
+            double before = 0.0;
+#pragma unroll 4
+            for (int j = 0; j < L; ++j) before += lists.id[j] < id ? lists.weight[j] : 0.0;
+            if (lists.weight[i] > 0.0 && before <= target) atomicMax(&sh.found, (int)id);
+        }
+    } else {
+        for (int i = tid; i < L; i += T) lists.key[i] = (unsigned long long)(0xFFFFFFFFu - lists.id[i]) << 32 | (uint32_t)i;
+        sort_list<T>(lists.key, L);
+        double by_id[kListed / T];
+#pragma unroll
+        for (int j = 0; j < kListed / T; ++j) by_id[j] = j * T + tid < L ? lists.weight[(uint32_t)lists.key[j * T + tid]] : 0.0;
+        Team<T>::sync();
+#pragma unroll
+        for (int j = 0; j < kListed / T; ++j)
+            if (j * T + tid < L) lists.weight[j * T + tid] = by_id[j];
+        Team<T>::sync();
+        const int first = search.template reach_in_list<true>(L, 0.0, target);
+        if (tid == 0) {
+            int i = first;
+            while (i > 0 && lists.weight[i] == 0.0) --i;
+            sh.found = (int)(0xFFFFFFFFu - (uint32_t)(lists.key[i] >> 32));
+        }
+    }
+    Team<T>::sync();
+    if (tid == 0) {
+        const int token = sh.found;
+        const double z = ((double)as_float(x.x[token]) - w.m) * c.exact * 0.6931471805599453;
+        write(a, row, token, (float)(z - log(S)), (float)(z - log(C)), L);
+    }
+    return true;
+}
+
+// A lane's elements come in groups, of each of which the largest is kept while the row is summed up.  The k-th largest of these is at most the k-th
+// largest element; and where the largest of the groups from some value on weigh as much as top_p of the sum, so do the elements from there on.  What
+// reaches such a bound is in the few groups whose largest does: those are read once more, and what reaches it is listed.  Where
+// that fails, the row's elements are counted, and listed if the counts allow it.
+template <class E, int T>
+__global__ void __launch_bounds__(T == 32 ? 128 : T, T == 512 ? 2 : T == 256 ? 4 : 1) filter_kernel(SampleArgs a) {
+    using Size = Sizes<T>;
+    constexpr int kListed = Size::kListed, kGroupBins = Size::kBins < 1024 ? Size::kBins : 1024;
+    using In = Intervals<kGroupBins>;
     extern __shared__ uint4 dynamic[];
-    Lists& lists = *reinterpret_cast<Lists*>(dynamic);
-    const int64_t row = blockIdx.x;
+    struct Both {
+        Shared<T> sh;
+        Lists<T> lists;
+    };
+    Both& both = reinterpret_cast<Both*>(dynamic)[Team<T>::index()];
+    Shared<T>& sh = both.sh;
+    Lists<T>& lists = both.lists;
+    const int tid = Team<T>::thread(), lane = threadIdx.x & 31;
+    const Place<T> at;
+    const int64_t row = at.row;
+    if (row >= a.rows) return;
     const Asked r = asked_of<true>(a, row);
     if (r.kind) {
-        if (threadIdx.x == 0) write_none(a, row, r.kind, 0.0f);
+        if (at.rank == 0 && tid == 0) write_none(a, row, r.kind, 0.0f);
         return;
     }
     const Row<E> x(static_cast<const E*>(a.logits) + row * a.stride, a.vocab);
     const Scale c(r.T == 0.0f ? 1.0f : r.T);
-    const Total t = sums_of_row<E, T>(x, c, sh);
+    const bool by_sum = r.p < 1.0f, by_size = r.q > 0.0f;
+    bool by_count = r.k > 0 && r.k < a.vocab;
+    const Runs runs(x.vectors, at.runs());
+    const int begin = runs.begin(at.run()), end = runs.end(at.run());
+    // batches of a lane to a group, and groups of a lane
+    const int batches = (runs.per + 32 * kUnroll - 1) / (32 * kUnroll), span = (batches * T + Size::kGroups - 1) / Size::kGroups, groups = (batches + span - 1) / span;
+    float most;
+    double sum;
+    {
+        int n = 0;
+        float group = -CUDART_INF_F;
+        sum_run(x, begin, end, c, most, sum, [&](float l) {
+            group = max_nan(group, l);
+            if (++n % span == 0) {
+                lists.group[(n / span - 1) * T + tid] = group;
+                group = -CUDART_INF_F;
+            }
+        });
+        for (int g = n / span; g < groups; ++g) {
+            lists.group[g * T + tid] = group;
+            group = -CUDART_INF_F;
+        }
+    }
+    for (int b = tid; b < kGroupBins; b += T) lists.hist[b] = lists.parts[b] = 0;
+    if (tid == 0) sh.listed = 0;
+    if (T == 512 && at.blocks > 1) at.sync();                  // every block has begun
+    if (lane == 0) at.of_block(sh.most, 0)[at.run()] = most, at.of_block(sh.sum, 0)[at.run()] = sum;
+    // the block's bound
+    float bound = -CUDART_INF_F, block_most = most;
+    if (T != 32) {
+        Team<T>::sync();
+        if (lane == 0) sh.more[Team<T>::warp()] = most;
+        Team<T>::sync();
+        block_most = (float)sh.more[0];
+#pragma unroll
+        for (int w = 1; w < T / 32; ++w) block_most = max_nan(block_most, (float)sh.more[w]);
+    }
+    if (r.T != 0.0f && is_finite(block_most) && c.holds(block_most) && (by_count ? r.k < groups * T : by_sum)) {
+        const float M = c.base(block_most);
+        const double S = team_sum<T>(lane == 0 && most > -CUDART_INF_F ? sum * power(c.base(most) - M) : 0.0, sh);
+        Team<T>::sync();
+        for (int g = 0; g < groups; ++g) {
+            const int d = In::depth(c.exponent(lists.group[g * T + tid], M));
+            atomicAdd(&lists.hist[d / In::kParts], 1u);
+            if (!by_count) atomicAdd(&lists.parts[d / In::kParts], (uint32_t)(d % In::kParts));
+        }
+        Team<T>::sync();
+        constexpr int per = kGroupBins / T;
+        const double wanted = by_count ? (double)r.k : r.p * S * (1.0 + 1e-5);
+        auto part_of = [&](int b) { return by_count ? (double)lists.hist[b] : In::sum_of(b, lists.hist[b], lists.parts[b]).least; };
+        double mine = 0.0;
+        for (int b = tid * per; b < (tid + 1) * per; ++b) mine += part_of(b);
+        double before = team_before<T>(mine, sh);
+        set_all<T>(sh.lowest, kGroupBins - 1);
+        if (before + mine >= wanted)
+            for (int b = tid * per; b < (tid + 1) * per; ++b) {
+                before += part_of(b);
+                if (before < wanted || before == 0.0) continue;   // one at least, if none is wanted
+                atomicMin(&sh.lowest, b);
+                break;
+            }
+        Team<T>::sync();
+        // below every element of the interval
+        const int b = sh.lowest;
+        if (b < kGroupBins - 1) bound = fminf(__double2float_rd(((double)M - (b + 1.01) / In::kPerOctave) / c.c), block_most);
+    }
+    if (tid < at.blocks) {
+        at.of_block(sh.bound, tid)[at.rank] = bound;
+        at.of_block(sh.block_most, tid)[at.rank] = block_most;
+    }
+    at.sync();
+    // Of the blocks' bounds any does for a count, for a share the least.
+    float m = sh.block_most[0];
+    bound = sh.bound[0];
+    for (int b = 1; b < at.blocks; ++b) {
+        m = max_nan(m, sh.block_most[b]);
+        bound = by_count ? fmaxf(bound, sh.bound[b]) : fminf(bound, sh.bound[b]);
+    }
+    bool all_sizes = false;
+    if (by_size && !(by_count && by_sum) && is_finite(m)) {
+        const float q = __double2float_rd((double)m + (double)r.T * log((double)r.q) * 1.0000001);
+        if (q >= bound) bound = fminf(q, m), all_sizes = true;
+    }
+    const bool listing = r.T != 0.0f && is_finite(m) && c.holds(m) && (bound > -CUDART_INF_F || a.vocab <= kListed);
+    if (listing) {
+        int* const listed = at.of_block(&sh.listed, 0);
+        uint16_t* const hit = reinterpret_cast<uint16_t*>(lists.id);
+        set_all<T>(sh.found, 0);
+        for (int g = 0; g < groups; ++g) {
+            const float l = lists.group[g * T + tid];
+            if (!(l >= bound) || l == -CUDART_INF_F) continue;
+            const int n = atomicAdd(&sh.found, 1);
+            if (n < 2 * kListed) hit[n] = (uint16_t)(g * T + tid);
+        }
+        at.sync();                                             // the list takes the groups' place
+        unsigned long long* const key = at.of_block(lists.key, 0);
+        const int hits = sh.found, each = span * kUnroll;
+        if (hits > kListed) {
+            if (tid == 0) atomicAdd(listed, hits);             // there are no fewer elements than groups
+        } else {
+            for (int n = tid; n < hits * each; n += T) {
+                const int h = hit[n / each], g = h / T, of = h % T, k = n % each;
+                const int v = runs.begin(at.rank * (T / 32) + of / 32) + (g * each + k) * 32 + of % 32;
+                if (v >= runs.end(at.rank * (T / 32) + of / 32)) continue;
+                const Vector<E> in = x.load(v);
+                if (!(in.max() >= bound)) continue;
+#pragma unroll
+                for (int e = 0; e < Vector<E>::N; ++e) {
+                    const float y = in.one(e);
+                    if (y >= bound && y > -CUDART_INF_F) {
+                        const int i = atomicAdd(listed, 1);
+                        if (i < kListed) key[i] = key_of(y, x.first(v) + e);
+                    }
+                }
+            }
+        }
+        at.sync();
+    }
+    if (at.rank) return;
+    const Total t = join_runs(sh, at.runs(), c);
     if (!is_finite(t.m)) {
-        if (threadIdx.x == 0) write_none(a, row, 0, t.m);
+        if (tid == 0) write_none(a, row, 0, t.m);
         return;
     }
     if (r.T == 0.0f) {
         write_greedy<E, T>(a, row, x, t.m, sh);
         return;
     }
-    Search<E, T> search(x, c, r.T, t, sh, lists);
-    const Exact& w = search.w;
-    const Cut all = {-CUDART_INF_F, 0};
-    const bool by_sum = r.p < 1.0f, by_size = r.q > 0.0f;
-    bool by_count = r.k > 0 && r.k < a.vocab;
-    // the sum over the whole row in 64-bit weights, to `slack` of itself
-    double S = search.holds ? t.S * exp2(search.shift) : 0.0, slack = search.holds ? c.error(a.vocab, t.S) : 0.0;
-    int everything;
-    if (!search.holds) S = exact_sums<E, T>(x, w, all, sh, everything);
-    int n = 0;                         // what is listed, if that is all that may be kept
-    if (a.vocab <= kListed) {
-        n = search.list(all, 0, kBins - 1);
-    } else {
-        search.count(all);
-        int hi = -1;
+    int n = sh.listed;
+    if (listing && n <= kListed && draw_from_list<E, T>(a, row, x, c, r, t, n, by_count, all_sizes, sh, lists)) return;
+    bool counted = false;
+    if (by_count || by_sum) {
+        Search<E, T> search(x, c, t, sh, lists);
+        search.count(unmasked(), by_sum);
+        counted = true;
         if (by_count) {
             search.reach(r.k);
-            if (sh.before_it + sh.listed < r.k) by_count = false;         // fewer are not masked
-            else hi = sh.highest;
+            by_count = sh.before_it + sh.listed >= r.k;        // otherwise fewer are not masked
         }
-        if (!by_count) {
-            if (by_sum) {
-                search.bracket(r.p * S * exp2(-search.shift), S * exp2(-search.shift), slack + 1e-12);
-                hi = sh.highest;
-            }
-            if (by_size) {
-                const int b = search.bin(__double2float_rd((double)t.m + (double)r.T * log((double)r.q))) + 1;
-                if (hi < 0 || b < hi) hi = min(b, kBins - 1);
-            }
+        const bool holds = c.holds(t.m);
+        if (holds && !by_count && by_sum) {
+            const double S = t.S * exp2(-c.of_largest(t.m, t.M));
+            search.bracket(r.p * S, 2.0 * Error(a.vocab, t.S).both() * S);
         }
-        if (hi >= 0) {
-            int mine = 0;
-            for (int b = threadIdx.x; b <= hi; b += T) mine += lists.hist[b];
-            const int up_to = (int)block_sum<T>((double)mine, sh);
-            if (up_to <= kListed) n = search.list(all, 0, hi);
+        n = sh.before_it + sh.listed;
+        if (holds && (by_count || by_sum) && n <= kListed) {
+            const int hi = sh.highest;
+            Team<T>::sync();
+            search.list(hi);
+            if (draw_from_list<E, T>(a, row, x, c, r, t, n, by_count, false, sh, lists)) return;
+            counted = false;
         }
+        Team<T>::sync();
     }
-    if (n > 0) {
-        // the list holds all that may be kept
-        search.weigh(n);
-        const int K = by_count ? min(r.k, n) : n;
-        int L = K;
-        if (by_sum) {
-            double of = S;
-            if (by_count || a.vocab <= kListed) {
-                double mine = 0.0;
-                for (int i = threadIdx.x; i < K; i += T) mine += lists.weight[i];
-                of = block_sum<T>(mine, sh);
-            }
-            L = search.template reach_in_list<false>(K, 0.0, r.p * of) + 1;
-            const double near = of * slack;
-            if (!by_count && a.vocab > kListed && slack > 0.0 && (r.p * of - sh.before < near || sh.after - r.p * of < near)) {
-                S = exact_sums<E, T>(x, w, all, sh, everything);
-                slack = 0.0;
-                L = search.template reach_in_list<false>(K, 0.0, r.p * S) + 1;
-            }
-        }
-        if (by_size) {
-            set_all(sh.found, L);
-            for (int i = threadIdx.x; i < L; i += T)
-                if (lists.weight[i] < r.q) {
-                    atomicMin(&sh.found, i);
-                    break;
-                }
-            __syncthreads();
-            L = max(sh.found, 1);
-        }
-        double mine = 0.0;
-        for (int i = threadIdx.x; i < L; i += T) mine += lists.weight[i];
-        const double C = block_sum<T>(mine, sh);
-        if (a.vocab <= kListed) {
-            double rest = 0.0;
-            for (int i = L + threadIdx.x; i < n; i += T) rest += lists.weight[i];
-            S = C + block_sum<T>(rest, sh);
-        }
-        // by id: the weights go with them
-        __syncthreads();
-        for (int i = threadIdx.x; i < L; i += T) lists.key[i] = (unsigned long long)(0xFFFFFFFFu - position_of(lists.key[i])) << 32 | (uint32_t)i;
-        sort_list<T>(lists.key, L);
-        double by_id[kListed / T];
+    draw_from_many<E, T>(a, row, x, c, r, t, by_count, counted, sh, lists);
+}
+
+// ---- few tokens: L lanes have one each, and everything in 64 bits ----
+template <class E, int L, bool kFilter>
+__global__ void __launch_bounds__(256) narrow_kernel(SampleArgs a) {
+    const int lane = threadIdx.x & 31, sub = lane % L;
+    const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
+    const bool real = row < a.rows;
+    const Asked r = asked_of<kFilter>(a, real ? row : 0);
+    const bool mine = real && sub < a.vocab && r.kind == 0;
+    const float x = mine ? as_float(static_cast<const E*>(a.logits)[row * a.stride + sub]) : -CUDART_INF_F;
+    float m = x;
 #pragma unroll
-        for (int j = 0; j < kListed / T; ++j) by_id[j] = j * T + threadIdx.x < L ? lists.weight[(uint32_t)lists.key[j * T + threadIdx.x]] : 0.0;
-        __syncthreads();
+    for (int o = L / 2; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(~0u, m, o));
+    const bool greedy = r.T == 0.0f, ok = is_finite(m);
+    const double z = ok && mine && x > -CUDART_INF_F ? ((double)x - (double)m) / (greedy ? 1.0 : (double)r.T) : -CUDART_INF;
+    double w = exp(z), S = w;
 #pragma unroll
-        for (int j = 0; j < kListed / T; ++j)
-            if (j * T + threadIdx.x < L) lists.weight[j * T + threadIdx.x] = by_id[j];
-        __syncthreads();
-        int at = search.template reach_in_list<true>(L, 0.0, r.u * C);
-        if (threadIdx.x == 0) {
-            while (at > 0 && lists.weight[at] == 0.0) --at;
-            const int token = (int)(0xFFFFFFFFu - (uint32_t)(lists.key[at] >> 32));
-            const double z = ((double)as_float(x.x[token]) - w.m) * w.by;
-            write(a, row, token, (float)(z - log(S)), (float)(z - log(C)), L);
+    for (int o = L / 2; o; o >>= 1) S += __shfl_xor_sync(~0u, S, o);
+    bool keep = x > -CUDART_INF_F;
+    if (kFilter || greedy) {
+        // how many are before this one in the row's order, and their sum
+        int rank = 0;
+        double before = 0.0;
+#pragma unroll
+        for (int j = 0; j < L; ++j) {
+            const float y = __shfl_sync(~0u, x, j, L);
+            const double v = __shfl_sync(~0u, w, j, L);
+            const bool earlier = y > x || (y == x && j < sub);
+            rank += earlier;
+            if (earlier) before += v;
         }
-        return;
+        if (kFilter && !greedy) {
+            keep = keep && (r.k <= 0 || rank < r.k);
+            double of = keep ? w : 0.0;
+#pragma unroll
+            for (int o = L / 2; o; o >>= 1) of += __shfl_xor_sync(~0u, of, o);
+            keep = keep && (rank == 0 || ((r.p >= 1.0f || before < r.p * of) && w >= r.q));
+        }
+        if (greedy) keep = keep && rank == 0;
     }
-    // too many for a list
-    Cut cut = all;
-    if (by_count) {
-        search.reach(r.k);
-        cut = search.border(all, r.k, 0.0);
+    // the running sum by id; the last token before which it does not exceed the target
+    double upto = keep ? w : 0.0;
+#pragma unroll
+    for (int o = 1; o < L; o <<= 1) {
+        const double y = __shfl_up_sync(~0u, upto, o, L);
+        if (sub >= o) upto += y;
     }
-    if (by_sum) {
-        int kept;
-        const double of = exact_sums<E, T>(x, w, cut, sh, kept);
-        if (!by_count) S = of;
-        search.count(cut);
-        const double unit = exp2(-search.shift);
-        search.bracket(r.p * of * unit, of * unit, 1e-12);
-        cut = tighter(cut, search.border(cut, 0, r.p * of));
+    const double C = __shfl_sync(~0u, upto, L - 1, L), previous = __shfl_up_sync(~0u, upto, 1, L), out = sub ? previous : 0.0;
+    const unsigned int all = L == 32 ? ~0u : ((1u << (L & 31)) - 1) << (lane & ~(L - 1));
+    const unsigned int here = __ballot_sync(~0u, keep && w > 0.0 && out <= r.u * C) & all;
+    const unsigned int kept = __ballot_sync(~0u, keep) & all;
+    if (!real) return;
+    if (r.kind || !ok) {
+        if (sub == 0) write_none(a, row, r.kind, m);
+    } else if (here ? lane == 31 - __clz(here) : sub == 0) {
+        if (greedy) write(a, row, sub, 0.0f, 0.0f, 1);
+        else write(a, row, here ? sub : -1, (float)(z - log(S)), (float)(z - log(C)), __popc(kept));
     }
-    if (by_size) {
-        float f = __double2float_ru((double)t.m + (double)r.T * log((double)r.q));
-        if (w.weight(f) < r.q) f = nextafterf(f, CUDART_INF_F);
-        else if (w.weight(nextafterf(f, -CUDART_INF_F)) >= r.q) f = nextafterf(f, -CUDART_INF_F);
-        cut = tighter(cut, Cut{fminf(f, t.m), 0xFFFFFFFFu});
-    }
-    int kept;
-    const Drawn d = draw_exactly<E, T>(x, t.m, r.T, r.u, cut, S, sh, kept);
-    if (threadIdx.x == 0) write(a, row, d.token, (float)d.logprob, (float)d.kept_logprob, kept);
 }
 
 // ---- launches ----
@@ -834,25 +1342,51 @@ int by_type(int type, F&& f) {
     if (e != cudaSuccess) (void)cudaGetLastError();
     return e == cudaSuccess ? SLAQ_OK : SLAQ_E_CUDA;
 }
+constexpr size_t kMostShared = 100 * 1024;
 template <class... Params, class... Args>
-cudaError_t launch(void (*kernel)(Params...), int64_t blocks, int threads, size_t smem, cudaStream_t st, Args... args) {
+cudaError_t launch(void (*kernel)(Params...), int64_t blocks, int threads, size_t smem, int cluster, cudaStream_t st, Args... args) {
+    if (smem > 40 * 1024) {   // what a kernel may use is state that all host threads share: never what this call needs, always the most
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostShared);
+        if (e != cudaSuccess) return e;
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
+    cudaLaunchAttribute attr[1] = {};
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
-static_assert(sizeof(Lists) + sizeof(Block<512>) <= 48 * 1024, "more shared memory than a kernel may use unasked");
+constexpr int kSms = 148;
 
+template <class E, int T>
+cudaError_t launch_team(const SampleArgs& a, bool filter, int cluster, cudaStream_t st) {
+    constexpr int teams = Team<T>::kPerBlock, threads = T * teams;
+    const int64_t blocks = (a.rows + teams - 1) / teams * cluster;
+    constexpr size_t smem = sizeof(Shared<T>) + sizeof(Lists<T>);
+    static_assert(teams * smem <= kMostShared);
+    return filter ? launch(filter_kernel<E, T>, blocks, threads, teams * smem, cluster, st, a) : launch(draw_kernel<E, T>, blocks, threads, 0, cluster, st, a);
+}
+template <class E, bool kFilter>
+cudaError_t launch_narrow(const SampleArgs& a, cudaStream_t st) {
+    if (a.vocab <= 16) return launch(narrow_kernel<E, 16, kFilter>, (a.rows + 15) / 16, 256, 0, 1, st, a);
+    return launch(narrow_kernel<E, 32, kFilter>, (a.rows + 7) / 8, 256, 0, 1, st, a);
+}
 template <class E>
 cudaError_t launch_sample(const SampleArgs& a, bool filter, cudaStream_t st) {
-    if (!filter) {
-        if (a.vocab <= 4096) return launch(draw_kernel<E, 64>, a.rows, 64, 0, st, a);
-        return launch(draw_kernel<E, 256>, a.rows, 256, 0, st, a);
-    }
-    if (a.vocab <= kListed) return launch(filter_kernel<E, 128>, a.rows, 128, sizeof(Lists), st, a);
-    return launch(filter_kernel<E, 512>, a.rows, 512, sizeof(Lists), st, a);
+    if (a.vocab <= 32) return filter ? launch_narrow<E, true>(a, st) : launch_narrow<E, false>(a, st);
+    const int vectors = (a.vocab + 2 * (Vector<E>::N - 1)) / Vector<E>::N;
+    if (vectors <= 256) return launch_team<E, 32>(a, filter, 1, st);
+    if (vectors <= 2048 && a.rows > 2 * kSms) return launch_team<E, 128>(a, filter, 1, st);
+    if (a.rows > kSms) return launch_team<E, 256>(a, filter, 1, st);
+    int cluster = 1;
+    while (cluster < kMaxCluster && a.rows * cluster * 2 <= kSms && vectors / (2 * cluster) >= 512) cluster *= 2;
+    return launch_team<E, 512>(a, filter, cluster, st);
 }
 
 }  // namespace
