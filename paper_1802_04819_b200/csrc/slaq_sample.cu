@@ -153,25 +153,14 @@ __device__ __forceinline__ T without_own(T in) {
     return (threadIdx.x & 31) ? y : T(0);
 }
 
-// ---- T threads that work on a row: a block, or one of a block's warps ----
-template <int T>
-struct Team {
-    static constexpr int kPerBlock = T == 32 ? 4 : 1;
-    static __device__ __forceinline__ int thread() { return T == 32 ? threadIdx.x & 31 : threadIdx.x; }
-    static __device__ __forceinline__ int warp() { return T == 32 ? 0 : threadIdx.x >> 5; }
-    static __device__ __forceinline__ int index() { return T == 32 ? threadIdx.x >> 5 : 0; }
-    static __device__ __forceinline__ void sync() {
-        if constexpr (T == 32) __syncwarp();
-        else __syncthreads();
-    }
-};
+// ---- T threads that work on a row: a block, or the blocks of a cluster ----
+__device__ __forceinline__ int thread_index() { return (int)threadIdx.x; }
+__device__ __forceinline__ int warp_index() { return (int)threadIdx.x >> 5; }
 constexpr int kMaxCluster = 8;     // of blocks of 512
 // Elements that are listed and sorted at most, intervals of a row's values, and groups of elements whose largest one is kept
 template <int T>
 struct Sizes {
-    static constexpr int kListed = T >= 256 ? 2048 : T == 128 ? 1024 : 256;
-    static constexpr int kBins = T == 32 ? 512 : 2048;
-    static constexpr int kGroups = T == 32 ? 256 : 4096;
+    static constexpr int kListed = T == 128 ? 1024 : 2048, kBins = 2048, kGroups = 2048;
 };
 template <int T>
 struct Shared {
@@ -181,7 +170,8 @@ struct Shared {
     double table[kSteps];
     double more[W];
     int count[W];
-    float bound[kMaxCluster], block_most[kMaxCluster];
+    float block_most[kMaxCluster];
+    double block_sum[kMaxCluster];
     double before, after;
     int found, listed, lowest, highest, before_it;
     uint32_t key_low, key_high;
@@ -197,7 +187,7 @@ struct Lists {                     // of the kernel with filters
     };
     union {
         unsigned long long key[S::kListed];
-        float group[S::kGroups];   // until the list is made: see below
+        float group[S::kGroups];   // until the list is made
     };
     uint32_t id[S::kListed];
 };
@@ -205,10 +195,9 @@ struct Lists {                     // of the kernel with filters
 template <int T>
 __device__ __forceinline__ double team_sum(double x, Shared<T>& sh) {
     x = warp_sum(x);
-    if constexpr (T == 32) return x;
-    Team<T>::sync();
-    if ((threadIdx.x & 31) == 0) sh.more[Team<T>::warp()] = x;
-    Team<T>::sync();
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) sh.more[warp_index()] = x;
+    __syncthreads();
     x = 0.0;
 #pragma unroll
     for (int w = 0; w < T / 32; ++w) x += sh.more[w];
@@ -217,10 +206,9 @@ __device__ __forceinline__ double team_sum(double x, Shared<T>& sh) {
 template <int T>
 __device__ __forceinline__ int team_sum(int x, Shared<T>& sh) {
     x = __reduce_add_sync(~0u, x);
-    if constexpr (T == 32) return x;
-    Team<T>::sync();
-    if ((threadIdx.x & 31) == 0) sh.count[Team<T>::warp()] = x;
-    Team<T>::sync();
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) sh.count[warp_index()] = x;
+    __syncthreads();
     x = 0;
 #pragma unroll
     for (int w = 0; w < T / 32; ++w) x += sh.count[w];
@@ -230,37 +218,35 @@ __device__ __forceinline__ int team_sum(int x, Shared<T>& sh) {
 template <int T>
 __device__ __forceinline__ double team_before(double x, Shared<T>& sh) {
     const double in = warp_before(x), out = without_own(in);
-    if constexpr (T == 32) return out;
-    Team<T>::sync();
-    if ((threadIdx.x & 31) == 31) sh.more[Team<T>::warp()] = in;
-    Team<T>::sync();
+    __syncthreads();
+    if ((threadIdx.x & 31) == 31) sh.more[warp_index()] = in;
+    __syncthreads();
     double before = 0.0;
-    for (int w = 0; w < Team<T>::warp(); ++w) before += sh.more[w];
+    for (int w = 0; w < warp_index(); ++w) before += sh.more[w];
     return before + out;
 }
 template <int T>
 __device__ __forceinline__ int team_before(int x, Shared<T>& sh) {
     const int in = warp_before(x);
-    if constexpr (T == 32) return in - x;
-    Team<T>::sync();
-    if ((threadIdx.x & 31) == 31) sh.count[Team<T>::warp()] = in;
-    Team<T>::sync();
+    __syncthreads();
+    if ((threadIdx.x & 31) == 31) sh.count[warp_index()] = in;
+    __syncthreads();
     int before = in - x;
-    for (int w = 0; w < Team<T>::warp(); ++w) before += sh.count[w];
+    for (int w = 0; w < warp_index(); ++w) before += sh.count[w];
     return before;
 }
 // `place` set to `value` for all, with a barrier on both sides
 template <int T, class V>
 __device__ __forceinline__ void set_all(V& place, V value) {
-    Team<T>::sync();
-    if (Team<T>::thread() == 0) place = value;
-    Team<T>::sync();
+    __syncthreads();
+    if (thread_index() == 0) place = value;
+    __syncthreads();
 }
 template <int T>
 __device__ __forceinline__ void fill_table(Shared<T>& sh) {
-    Team<T>::sync();
-    if (Team<T>::thread() < kSteps) sh.table[Team<T>::thread()] = exp2(Team<T>::thread() / (double)kSteps);
-    Team<T>::sync();
+    __syncthreads();
+    if (thread_index() < kSteps) sh.table[thread_index()] = exp2(thread_index() / (double)kSteps);
+    __syncthreads();
 }
 
 // ---- a row's vectors ----
@@ -283,7 +269,7 @@ __device__ __forceinline__ void over_vectors(const Row<E>& x, int begin, int end
         f(in, v + lane);
     }
 }
-// .. a vector at a time, the next one on its way: f(vector, its number)
+// .. a vector at a time, the next one on its way: f(vector, its number).  For what is too much code to stand there eight times.
 template <class E, class F>
 __device__ __forceinline__ void over_single(const Row<E>& x, int begin, int end, F&& f) {
     const int lane = threadIdx.x & 31;
@@ -295,14 +281,16 @@ __device__ __forceinline__ void over_single(const Row<E>& x, int begin, int end,
         f(in, v + lane);
     }
 }
-// .. element by element: f(element, id)
+// .. element by element, two at a time: f(element, id)
 template <class E, class F>
 __device__ __forceinline__ void over_elements(const Row<E>& x, int begin, int end, F&& f) {
-    over_vectors(x, begin, end, [&](const Batch<E>& in, int v) {
-#pragma unroll
-        for (int k = 0; k < kUnroll; ++k)
-#pragma unroll
-            for (int e = 0; e < Vector<E>::N; ++e) f(in[k].one(e), x.first(v + k * 32) + e);
+    over_single(x, begin, end, [&](const Vector<E>& in, int v) {
+#pragma unroll 1
+        for (int i = 0; i < Vector<E>::N / 2; ++i) {
+            float y, z;
+            split(in.at(i), y, z);
+            f(y, x.first(v) + 2 * i), f(z, x.first(v) + 2 * i + 1);
+        }
     });
 }
 template <class E>
@@ -313,24 +301,33 @@ __device__ __forceinline__ float largest(const Batch<E>& in) {
     return most;
 }
 template <class E>
+__device__ __forceinline__ Pair weights_of(const Vector<E>& in, Pair by, Pair off) {
+    constexpr int P = Vector<E>::N / 2;
+    Pair e[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        float a, b;
+        split(fma2(in.at(i), by, off), a, b);
+        e[i] = pair_of(exp2_fast(a), exp2_fast(b));
+    }
+    Pair sum = e[0] + e[1];
+    if constexpr (P == 4) sum = sum + (e[2] + e[3]);
+    return sum;
+}
+template <class E>
 __device__ __forceinline__ float weights_of(const Batch<E>& in, const Scale& c, float M) {
     const Pair off = pair_of(-M, -M), by = pair_of(c.c, c.c);
     Pair sum[kUnroll];
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-        constexpr int P = Vector<E>::N / 2;
-        Pair e[P];
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            float a, b;
-            split(fma2(in[k].at(i), by, off), a, b);
-            e[i] = pair_of(exp2_fast(a), exp2_fast(b));
-        }
-        sum[k] = e[0] + e[1];
-        if constexpr (P == 4) sum[k] = sum[k] + (e[2] + e[3]);
-    }
+    for (int k = 0; k < kUnroll; ++k) sum[k] = weights_of(in[k], by, off);
     float a, b;
     split((sum[0] + sum[1]) + (sum[2] + sum[3]), a, b);
+    return a + b;
+}
+template <class E>
+__device__ __forceinline__ float weights_of_one(const Vector<E>& in, const Scale& c, float M) {
+    float a, b;
+    split(weights_of(in, pair_of(c.c, c.c), pair_of(-M, -M)), a, b);
     return a + b;
 }
 // .. with -inf in the place of what is not wanted
@@ -392,8 +389,8 @@ __device__ __forceinline__ Total join_runs(Shared<T>& sh, int runs, const Scale&
     for (int r = threadIdx.x & 31; r < runs; r += 32) m = max_nan(m, sh.most[r]);
     Total t = {warp_max_nan(m), 0.0f, 0.0};
     t.M = c.base(t.m);
-    for (int r = Team<T>::thread(); r < runs; r += T) sh.sum[r] *= power((sh.most[r] == -CUDART_INF_F ? -CUDART_INF_F : c.base(sh.most[r])) - t.M);
-    Team<T>::sync();
+    for (int r = thread_index(); r < runs; r += T) sh.sum[r] *= power((sh.most[r] == -CUDART_INF_F ? -CUDART_INF_F : c.base(sh.most[r])) - t.M);
+    __syncthreads();
     t.S = sum_of_runs(sh, runs);
     return t;
 }
@@ -401,7 +398,7 @@ __device__ __forceinline__ Total join_runs(Shared<T>& sh, int runs, const Scale&
 template <class E, int T>
 __device__ __noinline__ double fast_sums(const Row<E>& x, const Scale& c, float M, const Cut cut, Shared<T>& sh, int& kept) {
     const Runs runs(x.vectors, T / 32);
-    const int warp = Team<T>::warp();
+    const int warp = warp_index();
     double s = 0.0;
     int n = 0;
     over_vectors(x, runs.begin(warp), runs.end(warp), [&](const Batch<E>& given, int v) {
@@ -419,18 +416,18 @@ __device__ __noinline__ double fast_sums(const Row<E>& x, const Scale& c, float 
     s = warp_sum(s);
     kept = team_sum<T>(n, sh);
     if ((threadIdx.x & 31) == 0) sh.sum[warp] = s;
-    Team<T>::sync();
+    __syncthreads();
     return sum_of_runs(sh, T / 32);
 }
 // .. in 64-bit weights
 template <class E, int T>
 __device__ __noinline__ double exact_sums(const Row<E>& x, const Exact& w, const Cut cut, Shared<T>& sh, int& kept) {
     const Runs runs(x.vectors, T / 32);
-    const int warp = Team<T>::warp();
+    const int warp = warp_index();
     double s = 0.0;
     int n = 0;
     over_single(x, runs.begin(warp), runs.end(warp), [&](const Vector<E>& in, int v) {
-#pragma unroll 1                       // two weights at a time: more of them do not fit the registers
+#pragma unroll 2                       // four weights at a time
         for (int i = 0; i < Vector<E>::N / 2; ++i) {
             float y, z;
             split(in.at(i), y, z);
@@ -443,15 +440,15 @@ __device__ __noinline__ double exact_sums(const Row<E>& x, const Exact& w, const
     s = warp_sum(s);
     kept = team_sum<T>(n, sh);
     if ((threadIdx.x & 31) == 0) sh.sum[warp] = s;
-    Team<T>::sync();
+    __syncthreads();
     return sum_of_runs(sh, T / 32);
 }
 
 // The first element at which the running sum exceeds `target`: the run by sh.sum, the thread's part of that run, the element.  sh.found is the
-// element, or -1, and sh.before and sh.after are the sums on its two sides.  weight(element, id); sums(vectors v .. v + 3 of one lane)
-template <class E, int T, class Weight>
-__device__ __forceinline__ void find(const Row<E>& x, const Runs& runs, int n_runs, double target, Shared<T>& sh, Weight&& weight) {
-    const int lane = threadIdx.x & 31, tid = Team<T>::thread();
+// element, or -1, and sh.before and sh.after are the sums on its two sides.  weight(element, id); of_vector(vector, its number)
+template <class E, int T, class Weight, class Sum>
+__device__ __forceinline__ void find(const Row<E>& x, const Runs& runs, int n_runs, double target, Shared<T>& sh, Weight&& weight, Sum&& of_vector) {
+    const int lane = threadIdx.x & 31, tid = thread_index();
     // the last run before which the sum does not exceed it, among those that weigh
     double before = 0.0, from_run = 0.0;
     int run = 0;
@@ -468,19 +465,13 @@ __device__ __forceinline__ void find(const Row<E>& x, const Runs& runs, int n_ru
     const int begin = runs.begin(run), end = runs.end(run), per = (end - begin + T - 1) / T;
     const int mine = begin + tid * per, stop = min(mine + per, end);
     double s = 0.0;
-    for (int v = mine; v < stop; ++v) {
-        const Vector<E> in = x.load(v);
-        const int i = x.first(v);
-        double part = 0.0;
-#pragma unroll
-        for (int e = 0; e < Vector<E>::N; ++e) part += weight(in.one(e), i + e);
-        s += part;
-    }
+#pragma unroll 4
+    for (int v = mine; v < stop; ++v) s += of_vector(x.load(v), v);
     const double from = from_run + team_before<T>(s, sh);
     if (tid == 0) sh.found = -1, sh.lowest = -1;
-    Team<T>::sync();
+    __syncthreads();
     if (s > 0.0 && from <= target) atomicMax(&sh.lowest, tid);
-    Team<T>::sync();
+    __syncthreads();
     // that thread's elements, its warp's lanes side by side
     const int owner = sh.lowest;
     if (owner >= 0 && tid >> 5 == owner >> 5) {
@@ -503,15 +494,25 @@ __device__ __forceinline__ void find(const Row<E>& x, const Runs& runs, int n_ru
         }
         if (lane == 0) sh.found = last, sh.before = last_before, sh.after = last_after;
     }
-    Team<T>::sync();
+    __syncthreads();
 }
 
 // Drawn from what is kept in 64 bits, sh.sum and C being its sums.  log2_S: of the whole row's sum.
 template <class E, int T>
 __device__ __noinline__ void draw_exactly(const SampleArgs& a, int64_t row, const Row<E>& x, const Scale& c, const Exact& w, float u, const Cut cut, double log2_S, double C,
                                           int kept, Shared<T>& sh) {
-    find<E, T>(x, Runs(x.vectors, T / 32), T / 32, u * C, sh, [&](float y, int i) { return cut.keeps(y, i) ? w.weight(y) : 0.0; });
-    if (Team<T>::thread() == 0) {
+    auto weight = [&](float y, int i) { return cut.keeps(y, i) ? w.weight(y) : 0.0; };
+    find<E, T>(x, Runs(x.vectors, T / 32), T / 32, u * C, sh, weight, [&](const Vector<E>& in, int v) {
+        double s = 0.0;
+#pragma unroll 1
+        for (int i = 0; i < Vector<E>::N / 2; ++i) {
+            float y, z;
+            split(in.at(i), y, z);
+            s += weight(y, x.first(v) + 2 * i) + weight(z, x.first(v) + 2 * i + 1);
+        }
+        return s;
+    });
+    if (thread_index() == 0) {
         const int token = sh.found;
         const double z = token < 0 ? 0.0 : ((double)as_float(x.x[token]) - w.m) * c.exact, log2_C = log2(C);
         write(a, row, token, (float)((z - (log2_S == log2_S ? log2_S : log2_C)) * 0.6931471805599453), (float)((z - log2_C) * 0.6931471805599453), kept);
@@ -522,7 +523,7 @@ __device__ __forceinline__ void write_greedy(const SampleArgs& a, int64_t row, c
     set_all<T>(sh.found, 0x7FFFFFFF);
     const Runs runs(x.vectors, T / 32);
     int first = 0x7FFFFFFF;
-    over_vectors(x, runs.begin(Team<T>::warp()), runs.end(Team<T>::warp()), [&](const Batch<E>& in, int v) {
+    over_vectors(x, runs.begin(warp_index()), runs.end(warp_index()), [&](const Batch<E>& in, int v) {
 #pragma unroll
         for (int k = 0; k < kUnroll; ++k)
             if (in[k].max() == m)
@@ -531,27 +532,27 @@ __device__ __forceinline__ void write_greedy(const SampleArgs& a, int64_t row, c
                     if (in[k].one(e) == m) first = min(first, x.first(v + k * 32) + e);
     });
     if (first != 0x7FFFFFFF) atomicMin(&sh.found, first);
-    Team<T>::sync();
-    if (Team<T>::thread() == 0) write(a, row, sh.found, 0.0f, 0.0f, 1);
+    __syncthreads();
+    if (thread_index() == 0) write(a, row, sh.found, 0.0f, 0.0f, 1);
 }
 
-// The team's row, and in a cluster the part of it that the block takes.
+// The block's row, and in a cluster the part of it that the block takes.
 template <int T>
 struct Place {
     int rank = 0, blocks = 1;
-    int64_t row;
-    __device__ __forceinline__ Place() : row((int64_t)blockIdx.x * Team<T>::kPerBlock + Team<T>::index()) {
+    int64_t row = blockIdx.x;
+    __device__ __forceinline__ Place() {
         if constexpr (T == 512) {
             rank = (int)cg::this_cluster().block_rank(), blocks = (int)cg::this_cluster().num_blocks();
             row = blockIdx.x / blocks;
         }
     }
-    __device__ __forceinline__ int run() const { return rank * (T / 32) + Team<T>::warp(); }
+    __device__ __forceinline__ int run() const { return rank * (T / 32) + warp_index(); }
     __device__ __forceinline__ int runs() const { return blocks * (T / 32); }
     // a barrier of all that work on the row
     __device__ __forceinline__ void sync() const {
         if (T == 512 && blocks > 1) cg::this_cluster().sync();
-        else Team<T>::sync();
+        else __syncthreads();
     }
     template <class P>
     __device__ __forceinline__ P* of_block(P* p, int r) const {
@@ -563,15 +564,13 @@ struct Place {
 
 // ---- the whole distribution ----
 template <class E, int T>
-__global__ void __launch_bounds__(T == 32 ? 128 : T) draw_kernel(SampleArgs a) {
-    __shared__ Shared<T> shared[Team<T>::kPerBlock];
-    Shared<T>& sh = shared[Team<T>::index()];
+__global__ void __launch_bounds__(T) draw_kernel(SampleArgs a) {
+    __shared__ Shared<T> sh;
     const Place<T> at;
     const int64_t row = at.row;
-    if (row >= a.rows) return;
     const Asked r = asked_of<false>(a, row);
     if (r.kind) {
-        if (at.rank == 0 && Team<T>::thread() == 0) write_none(a, row, r.kind, 0.0f);
+        if (at.rank == 0 && thread_index() == 0) write_none(a, row, r.kind, 0.0f);
         return;
     }
     const Row<E> x(static_cast<const E*>(a.logits) + row * a.stride, a.vocab);
@@ -586,7 +585,7 @@ __global__ void __launch_bounds__(T == 32 ? 128 : T) draw_kernel(SampleArgs a) {
     if (at.rank) return;
     const Total t = join_runs(sh, at.runs(), c);
     if (!is_finite(t.m)) {
-        if (Team<T>::thread() == 0) write_none(a, row, 0, t.m);
+        if (thread_index() == 0) write_none(a, row, 0, t.m);
         return;
     }
     if (r.T == 0.0f) {
@@ -595,17 +594,18 @@ __global__ void __launch_bounds__(T == 32 ? 128 : T) draw_kernel(SampleArgs a) {
     }
     if (c.holds(t.m)) {
         const double target = r.u * t.S, margin = Error(a.vocab, t.S).at(r.u) * t.S;
-        find<E, T>(x, runs, at.runs(), target, sh, [&](float y, int) { return (double)c.weight(y, t.M); });
+        find<E, T>(x, runs, at.runs(), target, sh, [&](float y, int) { return (double)c.weight(y, t.M); },
+                   [&](const Vector<E>& in, int) { return (double)weights_of_one(in, c, t.M); });
         const int token = sh.found;
         if (token >= 0 && target - sh.before >= margin && sh.after - target >= margin) {
-            if (Team<T>::thread() == 0) {
+            if (thread_index() == 0) {
                 const double log2_S = log2(t.S) - c.of_largest(t.m, t.M);
                 const float logprob = (float)((((double)as_float(x.x[token]) - t.m) * c.exact - log2_S) * 0.6931471805599453);
                 write(a, row, token, logprob, logprob, 0);
             }
             return;
         }
-        Team<T>::sync();
+        __syncthreads();
     }
     fill_table(sh);
     const Exact w(t.m, c, sh.table);
@@ -619,7 +619,7 @@ __global__ void __launch_bounds__(T == 32 ? 128 : T) draw_kernel(SampleArgs a) {
 // The list by rank, which is how many other keys are above: ids and weights.  No two keys are equal.
 template <int T>
 __device__ __forceinline__ void rank_list(Lists<T>& lists, int n, const Exact& w) {
-    for (int i = Team<T>::thread(); i < n; i += T) {
+    for (int i = thread_index(); i < n; i += T) {
         const unsigned long long mine = lists.key[i];
         int rank = 0;
 #pragma unroll 8
@@ -627,24 +627,24 @@ __device__ __forceinline__ void rank_list(Lists<T>& lists, int n, const Exact& w
         lists.id[rank] = position_of(mine);
         lists.weight[rank] = w.weight(value_of((uint32_t)(mine >> 32)));
     }
-    Team<T>::sync();
+    __syncthreads();
 }
 // Keys fall from key[0] to key[n - 1].
 template <int T>
 __device__ __forceinline__ void sort_list(unsigned long long* key, int n) {
     int size = 32;
     while (size < n) size *= 2;
-    for (int i = n + Team<T>::thread(); i < size; i += T) key[i] = 0;
+    for (int i = n + thread_index(); i < size; i += T) key[i] = 0;
     for (int k = 2; k <= size; k *= 2)
         for (int j = k / 2; j; j /= 2) {
-            Team<T>::sync();
-            for (int i = Team<T>::thread(); i < size / 2; i += T) {
+            __syncthreads();
+            for (int i = thread_index(); i < size / 2; i += T) {
                 const int p = 2 * i - (i & (j - 1)), q = p + j;
                 const unsigned long long x = key[p], y = key[q];
                 if ((x < y) == !(p & k)) key[p] = y, key[q] = x;
             }
         }
-    Team<T>::sync();
+    __syncthreads();
 }
 
 // Intervals of the exponents t <= 0 of weights 2^t, from 0 down, kBins in 64 octaves.  With an interval's count goes the sum of what its exponents are
@@ -689,43 +689,43 @@ struct Search {
 
     __device__ __forceinline__ Search(const Row<E>& x, const Scale& c, const Total& t, Shared<T>& sh, Lists<T>& lists)
         : x(x), c(c), w(t.m, c, sh.table), m(t.m), sh(sh), lists(lists), runs(x.vectors, T / 32) {}
-    __device__ __forceinline__ int begin() const { return runs.begin(Team<T>::warp()); }
-    __device__ __forceinline__ int end() const { return runs.end(Team<T>::warp()); }
+    __device__ __forceinline__ int begin() const { return runs.begin(warp_index()); }
+    __device__ __forceinline__ int end() const { return runs.end(warp_index()); }
     // Of the exponent below the largest element's, for which 32 bits do.
     __device__ __forceinline__ int depth(float y) const { return In::depth((y - m) * c.c); }
     __device__ __forceinline__ int bin(float y) const { return depth(y) / In::kParts; }
 
     __device__ __forceinline__ void count(const Cut in, bool parts) {
-        Team<T>::sync();
-        for (int b = Team<T>::thread(); b < kBins; b += T) lists.hist[b] = lists.parts[b] = 0;
-        Team<T>::sync();
+        __syncthreads();
+        for (int b = thread_index(); b < kBins; b += T) lists.hist[b] = lists.parts[b] = 0;
+        __syncthreads();
         over_elements(x, begin(), end(), [&](float y, int i) {
             if (!in.keeps(y, i)) return;
             const int d = depth(y);
             atomicAdd(&lists.hist[d / In::kParts], 1u);
             if (parts) atomicAdd(&lists.parts[d / In::kParts], (uint32_t)(d % In::kParts));
         });
-        Team<T>::sync();
+        __syncthreads();
     }
     // The first interval up to which there are n elements (sh.highest), how many there are before it (sh.before_it) and in it (sh.listed);
     // without so many, the last one.
     __device__ __forceinline__ void reach(int n) {
         constexpr int per = kBins / T;
-        const int b0 = Team<T>::thread() * per;
+        const int b0 = thread_index() * per;
         int mine = 0;
         for (int b = b0; b < b0 + per; ++b) mine += lists.hist[b];
         int sum = team_before<T>(mine, sh);
-        if (sum < n && (sum + mine >= n || Team<T>::thread() == T - 1)) {
+        if (sum < n && (sum + mine >= n || thread_index() == T - 1)) {
             int b = b0;
             for (; b < b0 + per - 1 && sum + (int)lists.hist[b] < n; ++b) sum += lists.hist[b];
             sh.lowest = sh.highest = b, sh.before_it = sum, sh.listed = lists.hist[b];
         }
-        Team<T>::sync();
+        __syncthreads();
     }
     // The intervals sh.lowest to sh.highest in which the running sum reaches B, which is known to `margin`; the elements before and in them.
     __device__ __forceinline__ void bracket(double B, double margin) {
         constexpr int per = kBins / T;
-        const int b0 = Team<T>::thread() * per;
+        const int b0 = thread_index() * per;
         auto sum_of = [&](int b) { return In::sum_of(b, lists.hist[b], lists.parts[b]); };
         double hi = 0.0, lo = 0.0;
         for (int b = b0; b < b0 + per; ++b) {
@@ -733,8 +733,8 @@ struct Search {
             hi += s.most, lo += s.least;
         }
         double sum_hi = team_before<T>(hi, sh), sum_lo = team_before<T>(lo, sh);
-        if (Team<T>::thread() == 0) sh.lowest = sh.highest = kBins - 1;
-        Team<T>::sync();
+        if (thread_index() == 0) sh.lowest = sh.highest = kBins - 1;
+        __syncthreads();
         if (sum_hi + hi >= B - margin || sum_lo + lo >= B + margin)
             for (int b = b0; b < b0 + per; ++b) {
                 const auto s = sum_of(b);
@@ -743,14 +743,14 @@ struct Search {
                 if (sum_lo >= B + margin) atomicMin(&sh.highest, b);
                 if (sum_lo >= B + margin) break;
             }
-        Team<T>::sync();
+        __syncthreads();
         int before = 0, inside = 0;
         const int first = min(sh.lowest, sh.highest), last = sh.highest;
         for (int b = b0; b < b0 + per; ++b) (b < first ? before : inside) += b <= last ? lists.hist[b] : 0;
         before = team_sum<T>(before, sh), inside = team_sum<T>(inside, sh);
-        Team<T>::sync();
-        if (Team<T>::thread() == 0) sh.lowest = first, sh.before_it = before, sh.listed = inside;
-        Team<T>::sync();
+        __syncthreads();
+        if (thread_index() == 0) sh.lowest = first, sh.before_it = before, sh.listed = inside;
+        __syncthreads();
     }
 
     __device__ __forceinline__ void append(float y, int i) {
@@ -760,15 +760,17 @@ struct Search {
     // Everything down to interval `hi`, which is as much as a list holds.
     __device__ __noinline__ void list(int hi) {
         set_all<T>(sh.listed, 0);
-        over_vectors(x, begin(), end(), [&](const Batch<E>& in, int v) {
-            if (bin(largest(in)) > hi) return;
-#pragma unroll
-            for (int k = 0; k < kUnroll; ++k)
-#pragma unroll
-                for (int e = 0; e < Vector<E>::N; ++e)
-                    if (in[k].one(e) > -CUDART_INF_F && bin(in[k].one(e)) <= hi) append(in[k].one(e), x.first(v + k * 32) + e);
+        over_single(x, begin(), end(), [&](const Vector<E>& in, int v) {
+            if (bin(in.max()) > hi) return;
+#pragma unroll 1
+            for (int i = 0; i < Vector<E>::N / 2; ++i) {
+                float y, z;
+                split(in.at(i), y, z);
+                if (y > -CUDART_INF_F && bin(y) <= hi) append(y, x.first(v) + 2 * i);
+                if (z > -CUDART_INF_F && bin(z) <= hi) append(z, x.first(v) + 2 * i + 1);
+            }
         });
-        Team<T>::sync();
+        __syncthreads();
     }
     __device__ __forceinline__ float value(int i) const { return value_of((uint32_t)(lists.key[i] >> 32)); }
     __device__ __forceinline__ Cut cut_at(int i) const { return {value(i), position_of(lists.key[i])}; }
@@ -776,7 +778,7 @@ struct Search {
     // sh.after: the sums on its two sides.
     template <bool kExceeds>
     __device__ __forceinline__ int reach_in_list(int n, double above, double B) {
-        const int per = (n + T - 1) / T, i0 = min(Team<T>::thread() * per, n), i1 = min(i0 + per, n);
+        const int per = (n + T - 1) / T, i0 = min(thread_index() * per, n), i1 = min(i0 + per, n);
         double mine = 0.0;
         for (int i = i0; i < i1; ++i) mine += lists.weight[i];
         const double from = above + team_before<T>(mine, sh);
@@ -789,14 +791,14 @@ struct Search {
                 break;
             }
         }
-        Team<T>::sync();
+        __syncthreads();
         const int at = sh.found;
         if (at >= i0 && at < i1) {
             sum = from;
             for (int i = i0; i < at; ++i) sum += lists.weight[i];
             sh.before = sum, sh.after = sum + lists.weight[at];
         }
-        Team<T>::sync();
+        __syncthreads();
         return at;
     }
 
@@ -806,16 +808,16 @@ struct Search {
     __device__ __noinline__ Cut border(const Cut in, int k, double p, double& of, double& C, int& kept) {
         const int lo = sh.lowest, hi = sh.highest;
         int above = sh.before_it, n = sh.listed;
-        Team<T>::sync();
-        if (Team<T>::thread() == 0) sh.key_low = 0xFFFFFFFFu, sh.key_high = 0, sh.listed = 0;
-        Team<T>::sync();
+        __syncthreads();
+        if (thread_index() == 0) sh.key_low = 0xFFFFFFFFu, sh.key_high = 0, sh.listed = 0;
+        __syncthreads();
         const bool fits = n <= kListed;
         double S = 0.0, A = 0.0, B = 0.0;
         uint32_t low = 0xFFFFFFFFu, high = 0;
         C = CUDART_NAN;
         over_single(x, begin(), end(), [&](const Vector<E>& v, int at) {
             if (k && bin(v.max()) > hi) return;
-#pragma unroll 1
+#pragma unroll 2
             for (int q = 0; q < Vector<E>::N / 2; ++q) {
                 float y, z;
                 split(v.at(q), y, z);
@@ -838,13 +840,13 @@ struct Search {
             of = team_sum<T>(S, sh);
             B = p * of;
             A = warp_sum(A);
-            if ((threadIdx.x & 31) == 0) sh.sum[Team<T>::warp()] = A;
-            Team<T>::sync();
+            if ((threadIdx.x & 31) == 0) sh.sum[warp_index()] = A;
+            __syncthreads();
             A = sum_of_runs(sh, T / 32);
         }
         if (!fits) {
             atomicMin(&sh.key_low, low), atomicMax(&sh.key_high, high);
-            Team<T>::sync();
+            __syncthreads();
             uint32_t bottom = sh.key_low, top = sh.key_high;
             while (n > kListed && bottom < top) {
                 const uint32_t middle = bottom + (top - bottom) / 2;       // the upper half: above it
@@ -864,11 +866,11 @@ struct Search {
                 });
                 upper = team_sum<T>(upper, sh);
                 s = team_sum<T>(s, sh);
-                Team<T>::sync();
-                if (Team<T>::thread() == 0) sh.key_low = 0xFFFFFFFFu, sh.key_high = 0;
-                Team<T>::sync();
+                __syncthreads();
+                if (thread_index() == 0) sh.key_low = 0xFFFFFFFFu, sh.key_high = 0;
+                __syncthreads();
                 atomicMin(&sh.key_low, low), atomicMax(&sh.key_high, high);
-                Team<T>::sync();
+                __syncthreads();
                 if (k ? above + upper >= k : A + s >= B) bottom = sh.key_low, n = upper;
                 else top = sh.key_high, above += upper, n -= upper, A += s;
             }
@@ -879,11 +881,11 @@ struct Search {
                 int mine = 0;
                 over_elements(x, begin(), end(), [&](float y, int i) { mine += y == v && in.keeps(y, i); });
                 mine = __reduce_add_sync(~0u, mine);
-                Team<T>::sync();
-                if ((threadIdx.x & 31) == 0) sh.count[Team<T>::warp()] = mine;
+                __syncthreads();
+                if ((threadIdx.x & 31) == 0) sh.count[warp_index()] = mine;
                 set_all<T>(sh.found, 0);
                 int before = 0;
-                for (int r = 0; r < Team<T>::warp(); ++r) before += sh.count[r];
+                for (int r = 0; r < warp_index(); ++r) before += sh.count[r];
                 if (before < wanted && before + mine >= wanted)            // in this warp's run
                     for (int v0 = begin(); v0 < end() && before < wanted; v0 += 32) {
                         const int at = v0 + (threadIdx.x & 31);
@@ -900,7 +902,7 @@ struct Search {
                                 if (is(e) && ++rank == wanted) sh.found = x.first(at) + e;
                         before += __shfl_sync(~0u, up_to, 31);
                     }
-                Team<T>::sync();
+                __syncthreads();
                 return {v, (uint32_t)sh.found};
             }
             set_all<T>(sh.listed, 0);
@@ -909,21 +911,21 @@ struct Search {
                 if (o >= bottom && o <= top && in.keeps(y, i)) append(y, i);
             });
         }
-        Team<T>::sync();
+        __syncthreads();
         n = min(sh.listed, kListed);
         sort_list<T>(lists.key, n);
         if (k) return cut_at(min(k - above, n) - 1);
-        for (int i = Team<T>::thread(); i < n; i += T) lists.weight[i] = w.weight(value(i));
-        Team<T>::sync();
+        for (int i = thread_index(); i < n; i += T) lists.weight[i] = w.weight(value(i));
+        __syncthreads();
         const int at = reach_in_list<false>(n, A, B);
         if (fits) {
             // those of the list that are kept, to their runs
             double s = 0.0;
             for (int i = threadIdx.x & 31; i <= at; i += 32)
-                if (((int)position_of(lists.key[i]) + x.skip) / Vector<E>::N / runs.per == Team<T>::warp()) s += lists.weight[i];
+                if (((int)position_of(lists.key[i]) + x.skip) / Vector<E>::N / runs.per == warp_index()) s += lists.weight[i];
             s = warp_sum(s);
-            if ((threadIdx.x & 31) == 0) sh.sum[Team<T>::warp()] += s;
-            Team<T>::sync();
+            if ((threadIdx.x & 31) == 0) sh.sum[warp_index()] += s;
+            __syncthreads();
             C = sum_of_runs(sh, T / 32);
             kept = above + at + 1;
         }
@@ -976,16 +978,22 @@ __device__ __noinline__ void draw_from_many(const SampleArgs& a, int64_t row, co
     if (holds && C != C) {
         C = fast_sums<E, T>(x, c, t.M, cut, sh, n);
         const double target = r.u * C, margin = Error(a.vocab, C).at(r.u) * C;
-        find<E, T>(x, search.runs, T / 32, target, sh, [&](float y, int i) { return cut.keeps(y, i) ? (double)c.weight(y, t.M) : 0.0; });
+        auto weight = [&](float y, int i) { return cut.keeps(y, i) ? c.weight(y, t.M) : 0.0f; };
+        find<E, T>(x, search.runs, T / 32, target, sh, [&](float y, int i) { return (double)weight(y, i); }, [&](const Vector<E>& in, int v) {
+            float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int e = 0; e < Vector<E>::N; ++e) sum[e & 1] += weight(in.one(e), x.first(v) + e);
+            return (double)(sum[0] + sum[1]);
+        });
         const int token = sh.found;
         if (token >= 0 && target - sh.before >= margin && sh.after - target >= margin) {
-            if (Team<T>::thread() == 0) {
+            if (thread_index() == 0) {
                 const double z = ((double)as_float(x.x[token]) - t.m) * c.exact, log2_C = log2(C) - one;
                 write(a, row, token, (float)((z - log2_S) * 0.6931471805599453), (float)((z - log2_C) * 0.6931471805599453), n);
             }
             return;
         }
-        Team<T>::sync();
+        __syncthreads();
         C = CUDART_NAN;
     }
     if (C != C) C = exact_sums<E, T>(x, w, cut, sh, n);
@@ -997,9 +1005,9 @@ __device__ __noinline__ void draw_from_many(const SampleArgs& a, int64_t row, co
 template <class E, int T>
 __device__ __noinline__ bool draw_from_list(const SampleArgs& a, int64_t row, const Row<E>& x, const Scale& c, const Asked& r, const Total& t, int n, bool by_count, bool all_sizes,
                                             Shared<T>& sh, Lists<T>& lists) {
-    constexpr int kListed = Sizes<T>::kListed, kRanked = T == 32 ? 64 : 256;
+    constexpr int kListed = Sizes<T>::kListed, kRanked = 256;
     const bool by_sum = r.p < 1.0f, by_size = r.q > 0.0f;
-    const int tid = Team<T>::thread();
+    const int tid = thread_index();
     if (n == 0) return false;
     fill_table(sh);
     Search<E, T> search(x, c, t, sh, lists);
@@ -1013,7 +1021,7 @@ __device__ __noinline__ bool draw_from_list(const SampleArgs& a, int64_t row, co
             lists.id[i] = position_of(lists.key[i]);
             lists.weight[i] = w.weight(search.value(i));
         }
-        Team<T>::sync();
+        __syncthreads();
     }
     double S = t.S * exp2(-c.of_largest(t.m, t.M));                // in 64-bit weights, to the error of its 32-bit ones
     int L = by_count ? min(r.k, n) : n;
@@ -1044,7 +1052,7 @@ __device__ __noinline__ bool draw_from_list(const SampleArgs& a, int64_t row, co
                 atomicMin(&sh.found, i);
                 break;
             }
-        Team<T>::sync();
+        __syncthreads();
         L = max(sh.found, 1);
     }
     double mine = 0.0;
@@ -1066,11 +1074,11 @@ __device__ __noinline__ bool draw_from_list(const SampleArgs& a, int64_t row, co
         double by_id[kListed / T];
 #pragma unroll
         for (int j = 0; j < kListed / T; ++j) by_id[j] = j * T + tid < L ? lists.weight[(uint32_t)lists.key[j * T + tid]] : 0.0;
-        Team<T>::sync();
+        __syncthreads();
 #pragma unroll
         for (int j = 0; j < kListed / T; ++j)
             if (j * T + tid < L) lists.weight[j * T + tid] = by_id[j];
-        Team<T>::sync();
+        __syncthreads();
         const int first = search.template reach_in_list<true>(L, 0.0, target);
         if (tid == 0) {
             int i = first;
@@ -1078,7 +1086,7 @@ __device__ __noinline__ bool draw_from_list(const SampleArgs& a, int64_t row, co
             sh.found = (int)(0xFFFFFFFFu - (uint32_t)(lists.key[i] >> 32));
         }
     }
-    Team<T>::sync();
+    __syncthreads();
     if (tid == 0) {
         const int token = sh.found;
         const double z = ((double)as_float(x.x[token]) - w.m) * c.exact * 0.6931471805599453;
@@ -1092,22 +1100,21 @@ __device__ __noinline__ bool draw_from_list(const SampleArgs& a, int64_t row, co
 // reaches such a bound is in the few groups whose largest does: those are read once more, and what reaches it is listed.  Where
 // that fails, the row's elements are counted, and listed if the counts allow it.
 template <class E, int T>
-__global__ void __launch_bounds__(T == 32 ? 128 : T, T == 512 ? 2 : T == 256 ? 4 : 1) filter_kernel(SampleArgs a) {
+__global__ void __launch_bounds__(T, T == 512 ? 2 : T == 256 ? 4 : 6) filter_kernel(SampleArgs a) {
     using Size = Sizes<T>;
-    constexpr int kListed = Size::kListed, kGroupBins = Size::kBins < 1024 ? Size::kBins : 1024;
+    constexpr int kListed = Size::kListed, kGroupBins = 1024;
     using In = Intervals<kGroupBins>;
     extern __shared__ uint4 dynamic[];
     struct Both {
         Shared<T> sh;
         Lists<T> lists;
     };
-    Both& both = reinterpret_cast<Both*>(dynamic)[Team<T>::index()];
+    Both& both = *reinterpret_cast<Both*>(dynamic);
     Shared<T>& sh = both.sh;
     Lists<T>& lists = both.lists;
-    const int tid = Team<T>::thread(), lane = threadIdx.x & 31;
+    const int tid = thread_index(), lane = tid & 31;
     const Place<T> at;
     const int64_t row = at.row;
-    if (row >= a.rows) return;
     const Asked r = asked_of<true>(a, row);
     if (r.kind) {
         if (at.rank == 0 && tid == 0) write_none(a, row, r.kind, 0.0f);
@@ -1124,81 +1131,88 @@ __global__ void __launch_bounds__(T == 32 ? 128 : T, T == 512 ? 2 : T == 256 ? 4
     float most;
     double sum;
     {
-        int n = 0;
+        int n = 0, g = 0;
         float group = -CUDART_INF_F;
         sum_run(x, begin, end, c, most, sum, [&](float l) {
             group = max_nan(group, l);
-            if (++n % span == 0) {
-                lists.group[(n / span - 1) * T + tid] = group;
-                group = -CUDART_INF_F;
-            }
+            if (++n < span) return;
+            lists.group[g++ * T + tid] = group;
+            group = -CUDART_INF_F;
+            n = 0;
         });
-        for (int g = n / span; g < groups; ++g) {
+        for (; g < groups; ++g) {
             lists.group[g * T + tid] = group;
             group = -CUDART_INF_F;
         }
     }
     for (int b = tid; b < kGroupBins; b += T) lists.hist[b] = lists.parts[b] = 0;
     if (tid == 0) sh.listed = 0;
-    if (T == 512 && at.blocks > 1) at.sync();                  // every block has begun
+    if (lane == 0) sh.more[warp_index()] = most;
+    at.sync();                                                 // every block has begun
     if (lane == 0) at.of_block(sh.most, 0)[at.run()] = most, at.of_block(sh.sum, 0)[at.run()] = sum;
-    // the block's bound
-    float bound = -CUDART_INF_F, block_most = most;
-    if (T != 32) {
-        Team<T>::sync();
-        if (lane == 0) sh.more[Team<T>::warp()] = most;
-        Team<T>::sync();
-        block_most = (float)sh.more[0];
+    float block_most = (float)sh.more[0];
 #pragma unroll
-        for (int w = 1; w < T / 32; ++w) block_most = max_nan(block_most, (float)sh.more[w]);
-    }
-    if (r.T != 0.0f && is_finite(block_most) && c.holds(block_most) && (by_count ? r.k < groups * T : by_sum)) {
+    for (int w = 1; w < T / 32; ++w) block_most = max_nan(block_most, (float)sh.more[w]);
+    // The block's groups in intervals of their exponents with its own base.  Bases are whole numbers, so another's intervals are these, shifted.
+    const bool counting = r.T != 0.0f && (by_count || by_sum), here = is_finite(block_most) && c.holds(block_most);
+    double block_sum = 0.0;
+    if (counting) {
         const float M = c.base(block_most);
-        const double S = team_sum<T>(lane == 0 && most > -CUDART_INF_F ? sum * power(c.base(most) - M) : 0.0, sh);
-        Team<T>::sync();
-        for (int g = 0; g < groups; ++g) {
-            const int d = In::depth(c.exponent(lists.group[g * T + tid], M));
-            atomicAdd(&lists.hist[d / In::kParts], 1u);
-            if (!by_count) atomicAdd(&lists.parts[d / In::kParts], (uint32_t)(d % In::kParts));
-        }
-        Team<T>::sync();
+        block_sum = team_sum<T>(here && lane == 0 && most > -CUDART_INF_F ? sum * power(c.base(most) - M) : 0.0, sh);
+        if (here)
+            for (int g = 0; g < groups; ++g) {
+                const int d = In::depth(c.exponent(lists.group[g * T + tid], M));
+                atomicAdd(&lists.hist[d / In::kParts], 1u);
+                if (!by_count) atomicAdd(&lists.parts[d / In::kParts], (uint32_t)(d % In::kParts));
+            }
+    }
+    if (tid < at.blocks) at.of_block(sh.block_most, tid)[at.rank] = block_most, at.of_block(sh.block_sum, tid)[at.rank] = block_sum;
+    at.sync();
+    float m = sh.block_most[0];
+    for (int b = 1; b < at.blocks; ++b) m = max_nan(m, sh.block_most[b]);
+    const bool holds = is_finite(m) && c.holds(m);
+    float bound = -CUDART_INF_F;
+    if (counting && holds) {
+        const float M = c.base(m);
+        double S = 0.0;
+        for (int b = 0; b < at.blocks; ++b)
+            if (sh.block_most[b] > -CUDART_INF_F && c.holds(sh.block_most[b])) S += sh.block_sum[b] * power(c.base(sh.block_most[b]) - M);
         constexpr int per = kGroupBins / T;
         const double wanted = by_count ? (double)r.k : r.p * S * (1.0 + 1e-5);
-        auto part_of = [&](int b) { return by_count ? (double)lists.hist[b] : In::sum_of(b, lists.hist[b], lists.parts[b]).least; };
-        double mine = 0.0;
-        for (int b = tid * per; b < (tid + 1) * per; ++b) mine += part_of(b);
+        double part[per], mine = 0.0;
+#pragma unroll
+        for (int q = 0; q < per; ++q) {
+            const int bin = tid * per + q;
+            uint32_t count = 0, parts = 0;
+            for (int b = 0; b < at.blocks; ++b) {
+                // the last interval holds whatever is below
+                const float down = sh.block_most[b] > -CUDART_INF_F && c.holds(sh.block_most[b]) ? M - c.base(sh.block_most[b]) : 64.0f;
+                const int from = bin - (int)fminf(down, 64.0f) * In::kPerOctave;
+                if (from < 0 || (from == kGroupBins - 1 && bin < kGroupBins - 1)) continue;
+                count += at.of_block(lists.hist, b)[from], parts += at.of_block(lists.parts, b)[from];
+            }
+            part[q] = bin == kGroupBins - 1 ? 0.0 : by_count ? (double)count : In::sum_of(bin, count, parts).least;
+            mine += part[q];
+        }
         double before = team_before<T>(mine, sh);
         set_all<T>(sh.lowest, kGroupBins - 1);
         if (before + mine >= wanted)
-            for (int b = tid * per; b < (tid + 1) * per; ++b) {
-                before += part_of(b);
-                if (before < wanted || before == 0.0) continue;   // one at least, if none is wanted
-                atomicMin(&sh.lowest, b);
-                break;
+#pragma unroll
+            for (int q = 0; q < per; ++q) {
+                before += part[q];
+                if (before >= wanted && before > 0.0) atomicMin(&sh.lowest, tid * per + q);   // one at least, if none is wanted
             }
-        Team<T>::sync();
+        __syncthreads();
         // below every element of the interval
         const int b = sh.lowest;
-        if (b < kGroupBins - 1) bound = fminf(__double2float_rd(((double)M - (b + 1.01) / In::kPerOctave) / c.c), block_most);
-    }
-    if (tid < at.blocks) {
-        at.of_block(sh.bound, tid)[at.rank] = bound;
-        at.of_block(sh.block_most, tid)[at.rank] = block_most;
-    }
-    at.sync();
-    // Of the blocks' bounds any does for a count, for a share the least.
-    float m = sh.block_most[0];
-    bound = sh.bound[0];
-    for (int b = 1; b < at.blocks; ++b) {
-        m = max_nan(m, sh.block_most[b]);
-        bound = by_count ? fmaxf(bound, sh.bound[b]) : fminf(bound, sh.bound[b]);
+        if (b < kGroupBins - 1) bound = fminf(__double2float_rd(((double)M - (b + 1.01) / In::kPerOctave) / c.c), m);
     }
     bool all_sizes = false;
     if (by_size && !(by_count && by_sum) && is_finite(m)) {
         const float q = __double2float_rd((double)m + (double)r.T * log((double)r.q) * 1.0000001);
         if (q >= bound) bound = fminf(q, m), all_sizes = true;
     }
-    const bool listing = r.T != 0.0f && is_finite(m) && c.holds(m) && (bound > -CUDART_INF_F || a.vocab <= kListed);
+    const bool listing = r.T != 0.0f && holds && (bound > -CUDART_INF_F || a.vocab <= kListed);
     if (listing) {
         int* const listed = at.of_block(&sh.listed, 0);
         uint16_t* const hit = reinterpret_cast<uint16_t*>(lists.id);
@@ -1221,17 +1235,22 @@ __global__ void __launch_bounds__(T == 32 ? 128 : T, T == 512 ? 2 : T == 256 ? 4
                 if (v >= runs.end(at.rank * (T / 32) + of / 32)) continue;
                 const Vector<E> in = x.load(v);
                 if (!(in.max() >= bound)) continue;
-#pragma unroll
-                for (int e = 0; e < Vector<E>::N; ++e) {
-                    const float y = in.one(e);
-                    if (y >= bound && y > -CUDART_INF_F) {
-                        const int i = atomicAdd(listed, 1);
-                        if (i < kListed) key[i] = key_of(y, x.first(v) + e);
-                    }
+                auto take = [&](float y, int id) {
+                    if (!(y >= bound) || y == -CUDART_INF_F) return;
+                    const int i = atomicAdd(listed, 1);
+                    if (i < kListed) key[i] = key_of(y, id);
+                };
+#pragma unroll 1
+                for (int i = 0; i < Vector<E>::N / 2; ++i) {
+                    float y, z;
+                    split(in.at(i), y, z);
+                    take(y, x.first(v) + 2 * i), take(z, x.first(v) + 2 * i + 1);
                 }
             }
         }
         at.sync();
+    } else {
+        at.sync();                                             // the blocks have read one another's counts
     }
     if (at.rank) return;
     const Total t = join_runs(sh, at.runs(), c);
@@ -1254,7 +1273,6 @@ __global__ void __launch_bounds__(T == 32 ? 128 : T, T == 512 ? 2 : T == 256 ? 4
             search.reach(r.k);
             by_count = sh.before_it + sh.listed >= r.k;        // otherwise fewer are not masked
         }
-        const bool holds = c.holds(t.m);
         if (holds && !by_count && by_sum) {
             const double S = t.S * exp2(-c.of_largest(t.m, t.M));
             search.bracket(r.p * S, 2.0 * Error(a.vocab, t.S).both() * S);
@@ -1262,12 +1280,11 @@ __global__ void __launch_bounds__(T == 32 ? 128 : T, T == 512 ? 2 : T == 256 ? 4
         n = sh.before_it + sh.listed;
         if (holds && (by_count || by_sum) && n <= kListed) {
             const int hi = sh.highest;
-            Team<T>::sync();
             search.list(hi);
             if (draw_from_list<E, T>(a, row, x, c, r, t, n, by_count, false, sh, lists)) return;
             counted = false;
         }
-        Team<T>::sync();
+        __syncthreads();
     }
     draw_from_many<E, T>(a, row, x, c, r, t, by_count, counted, sh, lists);
 }
@@ -1331,6 +1348,139 @@ __global__ void __launch_bounds__(256) narrow_kernel(SampleArgs a) {
     }
 }
 
+// ---- some tokens: a lane has N neighbouring ones, and everything in 64 bits ----
+// The largest order o such that at(o), which falls, is `enough`.  The lowest `skip` bits of all orders are alike for each sign.
+template <class F>
+__device__ __forceinline__ uint32_t last_order(int skip, F&& enough) {
+    uint32_t o = 0;
+#pragma unroll 1
+    for (int b = 31; b >= skip; --b)
+        if (enough(o | 1u << b)) o |= 1u << b;
+    return o;
+}
+template <class E, int N, bool kFilter>
+__global__ void __launch_bounds__(128) middle_kernel(SampleArgs a) {
+    __shared__ double table[kSteps];
+    if (threadIdx.x < kSteps) table[threadIdx.x] = exp2(threadIdx.x / (double)kSteps);
+    __syncthreads();
+    const int lane = threadIdx.x & 31;
+    const int64_t row = (int64_t)blockIdx.x * 4 + warp_index();
+    if (row >= a.rows) return;
+    const Asked r = asked_of<kFilter>(a, row);
+    if (r.kind) {
+        if (lane == 0) write_none(a, row, r.kind, 0.0f);
+        return;
+    }
+    const E* const from = static_cast<const E*>(a.logits) + row * a.stride;
+    float x[N], m = -CUDART_INF_F;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int i = lane * N + j;
+        x[j] = i < a.vocab ? as_float(from[i]) : -CUDART_INF_F;
+        m = max_nan(m, x[j]);
+    }
+    m = warp_max_nan(m);
+    if (!is_finite(m)) {
+        if (lane == 0) write_none(a, row, 0, m);
+        return;
+    }
+    if (r.T == 0.0f) {
+        int first = 0x7FFFFFFF;
+#pragma unroll
+        for (int j = N - 1; j >= 0; --j)
+            if (x[j] == m) first = lane * N + j;
+        first = __reduce_min_sync(~0u, first);
+        if (lane == 0) write(a, row, first, 0.0f, 0.0f, 1);
+        return;
+    }
+    const Scale c(r.T);
+    const Exact exact(m, c, table);
+    double w[N], mine = 0.0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        w[j] = exact.weight(x[j]);
+        mine += w[j];
+    }
+    const double S = warp_sum(mine);
+    double C = S;
+    uint32_t in = 0;               // bit j: x[j] is kept
+    int kept = 0;
+    if (kFilter) {
+        constexpr int kSkip = sizeof(E) == 4 ? 0 : std::is_same_v<E, __half> ? 13 : 16;
+        uint32_t order[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            order[j] = x[j] > -CUDART_INF_F ? order_of(x[j]) : 0u;
+            in |= (uint32_t)(x[j] > -CUDART_INF_F) << j;
+        }
+        // Only those above `o` stay, and of those equal to it the first `n` by id.
+        auto keep = [&](uint32_t o, int n) {
+            int equal = 0;
+#pragma unroll
+            for (int j = 0; j < N; ++j) equal += order[j] >> kSkip == o >> kSkip && (in >> j & 1);
+            int rank = without_own(warp_before(equal));
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const bool same = order[j] >> kSkip == o >> kSkip && (in >> j & 1);
+                if (order[j] >> kSkip < o >> kSkip || (same && rank >= n)) in &= ~(1u << j);
+                rank += same;
+            }
+        };
+        if (r.k > 0 && r.k < (int)__reduce_add_sync(~0u, __popc(in))) {
+            auto at_least = [&](uint32_t o) {
+                int n = 0;
+#pragma unroll
+                for (int j = 0; j < N; ++j) n += order[j] >= o;
+                return (int)__reduce_add_sync(~0u, n);
+            };
+            const uint32_t o = last_order(kSkip, [&](uint32_t y) { return at_least(y) >= r.k; });
+            keep(o, r.k - at_least(o + (1u << kSkip)));
+        }
+        if (r.p < 1.0f) {
+            auto sum_from = [&](uint32_t o) {
+                double s = 0.0;
+#pragma unroll
+                for (int j = 0; j < N; ++j) s += order[j] >= o && (in >> j & 1) ? w[j] : 0.0;
+                return warp_sum(s);
+            };
+            const double B = r.p * sum_from(0);
+            // the row's largest, if none is wanted
+            const uint32_t top = order_of(m) >> kSkip << kSkip;
+            const uint32_t o = B > 0.0 ? last_order(kSkip, [&](uint32_t y) { return sum_from(y) >= B; }) : top;
+            const uint32_t above = o + (1u << kSkip);
+            const double A = sum_from(above), each = exact.weight(value_of(o | (o >> 31 ? 0u : (1u << kSkip) - 1)));
+            keep(o, (int)fmin(fmax(ceil((B - A) / each), 1.0), 1e9));
+        }
+        if (r.q > 0.0f)
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (w[j] < r.q) in &= ~(1u << j);
+        mine = 0.0;
+#pragma unroll
+        for (int j = 0; j < N; ++j) mine += in >> j & 1 ? w[j] : 0.0;
+        kept = __reduce_add_sync(~0u, __popc(in));
+    } else {
+        in = ~0u;
+    }
+    // by id: the last token that weighs before which the sum does not exceed the target
+    const double upto = warp_before(mine), before = without_own(upto);
+    if (kFilter) C = __shfl_sync(~0u, upto, 31);
+    const double target = r.u * C;
+    const unsigned int here = __ballot_sync(~0u, mine > 0.0 && before <= target);
+    if (lane != 31 - __clz(here)) return;
+    double sum = before;
+    int token = 0;
+    float at = m;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const double v = in >> j & 1 ? w[j] : 0.0;
+        if (v > 0.0 && sum <= target) token = lane * N + j, at = x[j];
+        sum += v;
+    }
+    const double z = ((double)at - (double)m) * c.exact * 0.6931471805599453;
+    write(a, row, token, (float)(z - log(S)), (float)(z - log(C)), kept);
+}
+
 // ---- launches ----
 
 template <class F>
@@ -1366,11 +1516,13 @@ constexpr int kSms = 148;
 
 template <class E, int T>
 cudaError_t launch_team(const SampleArgs& a, bool filter, int cluster, cudaStream_t st) {
-    constexpr int teams = Team<T>::kPerBlock, threads = T * teams;
-    const int64_t blocks = (a.rows + teams - 1) / teams * cluster;
     constexpr size_t smem = sizeof(Shared<T>) + sizeof(Lists<T>);
-    static_assert(teams * smem <= kMostShared);
-    return filter ? launch(filter_kernel<E, T>, blocks, threads, teams * smem, cluster, st, a) : launch(draw_kernel<E, T>, blocks, threads, 0, cluster, st, a);
+    static_assert(smem <= kMostShared);
+    return filter ? launch(filter_kernel<E, T>, a.rows * cluster, T, smem, cluster, st, a) : launch(draw_kernel<E, T>, a.rows * cluster, T, 0, cluster, st, a);
+}
+template <class E, int N>
+cudaError_t launch_middle(const SampleArgs& a, bool filter, cudaStream_t st) {
+    return launch(filter ? middle_kernel<E, N, true> : middle_kernel<E, N, false>, (a.rows + 3) / 4, 128, 0, 1, st, a);
 }
 template <class E, bool kFilter>
 cudaError_t launch_narrow(const SampleArgs& a, cudaStream_t st) {
@@ -1380,8 +1532,12 @@ cudaError_t launch_narrow(const SampleArgs& a, cudaStream_t st) {
 template <class E>
 cudaError_t launch_sample(const SampleArgs& a, bool filter, cudaStream_t st) {
     if (a.vocab <= 32) return filter ? launch_narrow<E, true>(a, st) : launch_narrow<E, false>(a, st);
+    if (a.vocab <= 64) return launch_middle<E, 2>(a, filter, st);
+    if (a.vocab <= 128) return launch_middle<E, 4>(a, filter, st);
+    if (a.vocab <= 256) return launch_middle<E, 8>(a, filter, st);
+    if (a.vocab <= 512) return launch_middle<E, 16>(a, filter, st);
+    if (a.vocab <= 1024) return launch_middle<E, 32>(a, filter, st);
     const int vectors = (a.vocab + 2 * (Vector<E>::N - 1)) / Vector<E>::N;
-    if (vectors <= 256) return launch_team<E, 32>(a, filter, 1, st);
     if (vectors <= 2048 && a.rows > 2 * kSms) return launch_team<E, 128>(a, filter, 1, st);
     if (a.rows > kSms) return launch_team<E, 256>(a, filter, 1, st);
     int cluster = 1;
