@@ -160,7 +160,7 @@ constexpr int kMaxCluster = 8;     // of blocks of 512
 // Elements that are listed and sorted at most, intervals of a row's values, and groups of elements whose largest one is kept
 template <int T>
 struct Sizes {
-    static constexpr int kListed = T == 128 ? 1024 : 2048, kBins = 2048, kGroups = 2048;
+    static constexpr int kListed = T == 128 ? 1024 : 2048, kBins = T == 128 ? 512 : 2048, kGroups = 2048;
 };
 template <int T>
 struct Shared {
@@ -269,17 +269,13 @@ __device__ __forceinline__ void over_vectors(const Row<E>& x, int begin, int end
         f(in, v + lane);
     }
 }
-// .. a vector at a time, the next one on its way: f(vector, its number).  For what is too much code to stand there eight times.
+// .. a vector at a time: f(vector, its number)
 template <class E, class F>
 __device__ __forceinline__ void over_single(const Row<E>& x, int begin, int end, F&& f) {
-    const int lane = threadIdx.x & 31;
-    auto load = [&](int v) { return v < end ? x.load(v) : Row<E>::nothing(); };
-    Vector<E> next = load(begin + lane);
-    for (int v = begin; v < end; v += 32) {
-        const Vector<E> in = next;
-        next = load(v + 32 + lane);
-        f(in, v + lane);
-    }
+    over_vectors(x, begin, end, [&](const Batch<E>& in, int v) {
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) f(in[k], v + k * 32);
+    });
 }
 // .. element by element, two at a time: f(element, id)
 template <class E, class F>
@@ -396,7 +392,7 @@ __device__ __forceinline__ Total join_runs(Shared<T>& sh, int runs, const Scale&
 }
 // The sums of the runs over what is kept, in 32-bit weights with base M; how many are kept.
 template <class E, int T>
-__device__ __noinline__ double fast_sums(const Row<E>& x, const Scale& c, float M, const Cut cut, Shared<T>& sh, int& kept) {
+__device__ __noinline__ double fast_sums(const Row<E> x, const Scale c, float M, const Cut cut, Shared<T>& sh, int& kept) {
     const Runs runs(x.vectors, T / 32);
     const int warp = warp_index();
     double s = 0.0;
@@ -421,7 +417,7 @@ __device__ __noinline__ double fast_sums(const Row<E>& x, const Scale& c, float 
 }
 // .. in 64-bit weights
 template <class E, int T>
-__device__ __noinline__ double exact_sums(const Row<E>& x, const Exact& w, const Cut cut, Shared<T>& sh, int& kept) {
+__device__ __forceinline__ double exact_sums(const Row<E>& x, const Exact& w, const Cut& cut, Shared<T>& sh, int& kept) {
     const Runs runs(x.vectors, T / 32);
     const int warp = warp_index();
     double s = 0.0;
@@ -499,8 +495,8 @@ __device__ __forceinline__ void find(const Row<E>& x, const Runs& runs, int n_ru
 
 // Drawn from what is kept in 64 bits, sh.sum and C being its sums.  log2_S: of the whole row's sum.
 template <class E, int T>
-__device__ __noinline__ void draw_exactly(const SampleArgs& a, int64_t row, const Row<E>& x, const Scale& c, const Exact& w, float u, const Cut cut, double log2_S, double C,
-                                          int kept, Shared<T>& sh) {
+__device__ __forceinline__ void draw_exactly(const SampleArgs& a, int64_t row, const Row<E>& x, const Scale& c, const Exact& w, float u, const Cut& cut, double log2_S, double C,
+                                             int kept, Shared<T>& sh) {
     auto weight = [&](float y, int i) { return cut.keeps(y, i) ? w.weight(y) : 0.0; };
     find<E, T>(x, Runs(x.vectors, T / 32), T / 32, u * C, sh, weight, [&](const Vector<E>& in, int v) {
         double s = 0.0;
@@ -629,22 +625,43 @@ __device__ __forceinline__ void rank_list(Lists<T>& lists, int n, const Exact& w
     }
     __syncthreads();
 }
-// Keys fall from key[0] to key[n - 1].
+// Keys fall from key[0] to key[n - 1], n <= kListed.  Distances below 64 stay in a warp's registers, two keys a lane: 2,048 keys take 15 passes
+// through shared memory and six of those instead of 66 (34,000 cycles).
 template <int T>
 __device__ __forceinline__ void sort_list(unsigned long long* key, int n) {
-    int size = 32;
+    const int lane = threadIdx.x & 31;
+    int size = 64;
     while (size < n) size *= 2;
     for (int i = n + thread_index(); i < size; i += T) key[i] = 0;
-    for (int k = 2; k <= size; k *= 2)
-        for (int j = k / 2; j; j /= 2) {
-            __syncthreads();
+    __syncthreads();
+    for (int k = 64; k <= size; k *= 2) {
+        for (int j = k / 2; j >= 64; j /= 2) {
             for (int i = thread_index(); i < size / 2; i += T) {
                 const int p = 2 * i - (i & (j - 1)), q = p + j;
                 const unsigned long long x = key[p], y = key[q];
                 if ((x < y) == !(p & k)) key[p] = y, key[q] = x;
             }
+            __syncthreads();
         }
-    __syncthreads();
+        for (int part = warp_index(); part < size / 64; part += T / 32) {
+            unsigned long long a = key[part * 64 + lane], b = key[part * 64 + 32 + lane];
+            const bool falls = !(part * 64 & k);
+            if (k == 64) {
+                a = sorted(a);
+                b = __shfl_sync(~0u, sorted(b), 31 - lane);
+            }
+            const unsigned long long x = larger_if(falls, a, b), y = larger_if(!falls, a, b);
+            a = x, b = y;
+#pragma unroll
+            for (int j = 16; j; j /= 2) {
+                const bool first = !(lane & j) == falls;
+                a = larger_if(first, a, __shfl_xor_sync(~0u, a, j));
+                b = larger_if(first, b, __shfl_xor_sync(~0u, b, j));
+            }
+            key[part * 64 + lane] = a, key[part * 64 + 32 + lane] = b;
+        }
+        __syncthreads();
+    }
 }
 
 // Intervals of the exponents t <= 0 of weights 2^t, from 0 down, kBins in 64 octaves.  With an interval's count goes the sum of what its exponents are
@@ -659,17 +676,16 @@ struct Intervals {
         return __float_as_int(d + 12582912.0f) - 0x4B400000;      // 1.5 x 2^23
     }
     struct Bounds {
-        double least, most;
+        float least, most;
     };
     static __device__ __forceinline__ Bounds sum_of(int b, uint32_t count, uint32_t parts) {
-        if (count == 0) return {0.0, 0.0};
+        if (count == 0) return {0.0f, 0.0f};
         constexpr float per = 1.0f / kPerOctave;
-        // the roundings to 256ths, of exponents of up to 64 in 32 bits, and of this
-        constexpr double slack = 0.36 / (kParts * kPerOctave) + 1.6e-5;
-        const double n = count;
-        const float mean = __fdividef((float)parts, (float)count) * (1.0f / kParts), first = exp2_fast(b * -per), next = exp2_fast((b + 1) * -per);
+        // the roundings to 256ths, of exponents of up to 64 in 32 bits, and of this and what adds up a thread's intervals
+        constexpr float slack = 0.36f / (kParts * kPerOctave) + 1.8e-5f;
+        const float n = (float)count, mean = __fdividef((float)parts, n) * (1.0f / kParts), first = exp2_fast(b * -per), next = exp2_fast((b + 1) * -per);
         // the last interval goes on to 0
-        return {b == kBins - 1 ? 0.0 : n * exp2_fast((b + mean) * -per) * (1.0 - slack), n * (first + (next - first) * mean) * (1.0 + slack)};
+        return {b == kBins - 1 ? 0.0f : n * exp2_fast((b + mean) * -per) * (1.0f - slack), n * (first + (next - first) * mean) * (1.0f + slack)};
     }
 };
 
@@ -679,8 +695,8 @@ template <class E, int T>
 struct Search {
     static constexpr int kBins = Sizes<T>::kBins, kListed = Sizes<T>::kListed;
     using In = Intervals<kBins>;
-    const Row<E>& x;
-    const Scale& c;
+    const Row<E> x;
+    const Scale c;
     const Exact w;
     const float m;
     Shared<T>& sh;
@@ -695,12 +711,16 @@ struct Search {
     __device__ __forceinline__ int depth(float y) const { return In::depth((y - m) * c.c); }
     __device__ __forceinline__ int bin(float y) const { return depth(y) / In::kParts; }
 
-    __device__ __forceinline__ void count(const Cut in, bool parts) {
+    // kAll: nothing but what is masked is left out
+    template <bool kAll>
+    static __device__ __forceinline__ bool keeps(const Cut& in, float y, int i) { return kAll ? y > -CUDART_INF_F : in.keeps(y, i); }
+    template <bool kAll>
+    __device__ __forceinline__ void count(const Cut& in, bool parts) {
         __syncthreads();
         for (int b = thread_index(); b < kBins; b += T) lists.hist[b] = lists.parts[b] = 0;
         __syncthreads();
         over_elements(x, begin(), end(), [&](float y, int i) {
-            if (!in.keeps(y, i)) return;
+            if (!keeps<kAll>(in, y, i)) return;
             const int d = depth(y);
             atomicAdd(&lists.hist[d / In::kParts], 1u);
             if (parts) atomicAdd(&lists.parts[d / In::kParts], (uint32_t)(d % In::kParts));
@@ -727,12 +747,12 @@ struct Search {
         constexpr int per = kBins / T;
         const int b0 = thread_index() * per;
         auto sum_of = [&](int b) { return In::sum_of(b, lists.hist[b], lists.parts[b]); };
-        double hi = 0.0, lo = 0.0;
+        float hi = 0.0f, lo = 0.0f;
         for (int b = b0; b < b0 + per; ++b) {
             const auto s = sum_of(b);
             hi += s.most, lo += s.least;
         }
-        double sum_hi = team_before<T>(hi, sh), sum_lo = team_before<T>(lo, sh);
+        double sum_hi = team_before<T>((double)hi, sh), sum_lo = team_before<T>((double)lo, sh);
         if (thread_index() == 0) sh.lowest = sh.highest = kBins - 1;
         __syncthreads();
         if (sum_hi + hi >= B - margin || sum_lo + lo >= B + margin)
@@ -758,7 +778,7 @@ struct Search {
         if (n < kListed) lists.key[n] = key_of(y, i);
     }
     // Everything down to interval `hi`, which is as much as a list holds.
-    __device__ __noinline__ void list(int hi) {
+    __device__ __forceinline__ void list(int hi) {
         set_all<T>(sh.listed, 0);
         over_single(x, begin(), end(), [&](const Vector<E>& in, int v) {
             if (bin(in.max()) > hi) return;
@@ -805,7 +825,8 @@ struct Search {
     // The border in intervals sh.lowest to sh.highest: of the first k elements of `in`, or (k = 0) of those whose sum reaches p times that of `in`,
     // in 64-bit weights.  With k = 0, `of` is that sum, and C and `kept` are the sum and the number of what is kept, sh.sum the runs' sums of it, unless
     // C is NaN.
-    __device__ __noinline__ Cut border(const Cut in, int k, double p, double& of, double& C, int& kept) {
+    template <bool kAll>
+    __device__ __forceinline__ Cut border(const Cut& in, int k, double p, double& of, double& C, int& kept) {
         const int lo = sh.lowest, hi = sh.highest;
         int above = sh.before_it, n = sh.listed;
         __syncthreads();
@@ -822,7 +843,7 @@ struct Search {
                 float y, z;
                 split(v.at(q), y, z);
                 const int id = x.first(at) + 2 * q;
-                const int b_y = in.keeps(y, id) ? bin(y) : kBins, b_z = in.keeps(z, id + 1) ? bin(z) : kBins;
+                const int b_y = keeps<kAll>(in, y, id) ? bin(y) : kBins, b_z = keeps<kAll>(in, z, id + 1) ? bin(z) : kBins;
                 if (k == 0) {
                     const double one = w.weight(y), two = w.weight(z);
                     S += (b_y < kBins ? one : 0.0) + (b_z < kBins ? two : 0.0);
@@ -855,7 +876,7 @@ struct Search {
                 low = 0xFFFFFFFFu, high = 0;
                 over_elements(x, begin(), end(), [&](float y, int i) {
                     const uint32_t o = order_of(y);
-                    if (o < bottom || o > top || !in.keeps(y, i)) return;
+                    if (o < bottom || o > top || !keeps<kAll>(in, y, i)) return;
                     if (o > middle) {
                         ++upper;
                         low = min(low, o);
@@ -879,7 +900,7 @@ struct Search {
                 const float v = value_of(top);
                 const int wanted = k ? k - above : (int)fmin(fmax(ceil((B - A) / w.weight(v)), 1.0), (double)n);
                 int mine = 0;
-                over_elements(x, begin(), end(), [&](float y, int i) { mine += y == v && in.keeps(y, i); });
+                over_elements(x, begin(), end(), [&](float y, int i) { mine += y == v && keeps<kAll>(in, y, i); });
                 mine = __reduce_add_sync(~0u, mine);
                 __syncthreads();
                 if ((threadIdx.x & 31) == 0) sh.count[warp_index()] = mine;
@@ -890,7 +911,7 @@ struct Search {
                     for (int v0 = begin(); v0 < end() && before < wanted; v0 += 32) {
                         const int at = v0 + (threadIdx.x & 31);
                         const Vector<E> in_v = at < end() ? x.load(at) : Row<E>::nothing();
-                        auto is = [&](int e) { return in_v.one(e) == v && in.keeps(v, x.first(at) + e); };
+                        auto is = [&](int e) { return in_v.one(e) == v && keeps<kAll>(in, v, x.first(at) + e); };
                         int equal = 0;
 #pragma unroll
                         for (int e = 0; e < Vector<E>::N; ++e) equal += is(e);
@@ -908,7 +929,7 @@ struct Search {
             set_all<T>(sh.listed, 0);
             over_elements(x, begin(), end(), [&](float y, int i) {
                 const uint32_t o = order_of(y);
-                if (o >= bottom && o <= top && in.keeps(y, i)) append(y, i);
+                if (o >= bottom && o <= top && keeps<kAll>(in, y, i)) append(y, i);
             });
         }
         __syncthreads();
@@ -935,7 +956,7 @@ struct Search {
 
 // Rows of which more is kept than a list holds.  `counted`: by_count's, or of everything, are the counts that the search has.
 template <class E, int T>
-__device__ __noinline__ void draw_from_many(const SampleArgs& a, int64_t row, const Row<E>& x, const Scale& c, const Asked& r, const Total& t, bool by_count, bool counted,
+__device__ __noinline__ void draw_from_many(const SampleArgs& a, int64_t row, const Row<E> x, const Scale c, const Asked r, const Total t, bool by_count, bool counted,
                                             Shared<T>& sh, Lists<T>& lists) {
     const bool by_sum = r.p < 1.0f, by_size = r.q > 0.0f;
     fill_table(sh);
@@ -948,9 +969,9 @@ __device__ __noinline__ void draw_from_many(const SampleArgs& a, int64_t row, co
     int n = 0;
     if (!holds && (by_count || by_size)) log2_S = log2(exact_sums<E, T>(x, w, unmasked(), sh, n));
     if (by_count) {
-        if (!counted) search.count(unmasked(), false);
+        if (!counted) search.template count<true>(unmasked(), false);
         search.reach(r.k);
-        cut = search.border(unmasked(), r.k, 0.0, of, C, n);
+        cut = search.template border<true>(unmasked(), r.k, 0.0, of, C, n);
     }
     if (by_sum) {
         const Cut in = cut;
@@ -962,9 +983,10 @@ __device__ __noinline__ void draw_from_many(const SampleArgs& a, int64_t row, co
             error = Error(a.vocab, about).both();
             about *= to_largest;
         }
-        if (by_count || !counted) search.count(in, true);
+        if (by_count) search.template count<false>(in, true);
+        else if (!counted) search.template count<true>(in, true);
         search.bracket(r.p * about, 2.0 * error * about);
-        cut = tighter(in, search.border(in, 0, r.p, of, C, n));
+        cut = tighter(in, by_count ? search.template border<false>(in, 0, r.p, of, C, n) : search.template border<true>(in, 0, r.p, of, C, n));
         if (!by_count) log2_S = log2(of);
     }
     if (by_size) {
@@ -1003,7 +1025,7 @@ __device__ __noinline__ void draw_from_many(const SampleArgs& a, int64_t row, co
 // Draws from a list of n elements that holds all that may be kept.  Of a share top_p alone it may fall short (unless `all_sizes`: min_p
 // keeps nothing below it): false then.
 template <class E, int T>
-__device__ __noinline__ bool draw_from_list(const SampleArgs& a, int64_t row, const Row<E>& x, const Scale& c, const Asked& r, const Total& t, int n, bool by_count, bool all_sizes,
+__device__ __noinline__ bool draw_from_list(const SampleArgs& a, int64_t row, const Row<E> x, const Scale c, const Asked r, const Total t, int n, bool by_count, bool all_sizes,
                                             Shared<T>& sh, Lists<T>& lists) {
     constexpr int kListed = Sizes<T>::kListed, kRanked = 256;
     const bool by_sum = r.p < 1.0f, by_size = r.q > 0.0f;
@@ -1102,7 +1124,7 @@ __device__ __noinline__ bool draw_from_list(const SampleArgs& a, int64_t row, co
 template <class E, int T>
 __global__ void __launch_bounds__(T, T == 512 ? 2 : T == 256 ? 4 : 6) filter_kernel(SampleArgs a) {
     using Size = Sizes<T>;
-    constexpr int kListed = Size::kListed, kGroupBins = 1024;
+    constexpr int kListed = Size::kListed, kGroupBins = Size::kBins < 1024 ? Size::kBins : 1024, kBlocks = T == 512 ? kMaxCluster : 1;
     using In = Intervals<kGroupBins>;
     extern __shared__ uint4 dynamic[];
     struct Both {
@@ -1179,19 +1201,25 @@ __global__ void __launch_bounds__(T, T == 512 ? 2 : T == 256 ? 4 : 6) filter_ker
             if (sh.block_most[b] > -CUDART_INF_F && c.holds(sh.block_most[b])) S += sh.block_sum[b] * power(c.base(sh.block_most[b]) - M);
         constexpr int per = kGroupBins / T;
         const double wanted = by_count ? (double)r.k : r.p * S * (1.0 + 1e-5);
+        uint32_t count[per] = {}, parts[per] = {};
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+            if (b >= at.blocks) continue;
+            const float down = sh.block_most[b] > -CUDART_INF_F && c.holds(sh.block_most[b]) ? M - c.base(sh.block_most[b]) : 64.0f;
+            const int by = (int)fminf(down, 64.0f) * In::kPerOctave;
+            const uint32_t *const hist = at.of_block(lists.hist, b), *const part = at.of_block(lists.parts, b);
+#pragma unroll
+            for (int q = 0; q < per; ++q) {
+                const int from = tid * per + q - by;
+                if (from < 0 || from >= kGroupBins - 1) continue;      // the last interval holds whatever is below
+                count[q] += hist[from];
+                if (!by_count) parts[q] += part[from];
+            }
+        }
         double part[per], mine = 0.0;
 #pragma unroll
         for (int q = 0; q < per; ++q) {
-            const int bin = tid * per + q;
-            uint32_t count = 0, parts = 0;
-            for (int b = 0; b < at.blocks; ++b) {
-                // the last interval holds whatever is below
-                const float down = sh.block_most[b] > -CUDART_INF_F && c.holds(sh.block_most[b]) ? M - c.base(sh.block_most[b]) : 64.0f;
-                const int from = bin - (int)fminf(down, 64.0f) * In::kPerOctave;
-                if (from < 0 || (from == kGroupBins - 1 && bin < kGroupBins - 1)) continue;
-                count += at.of_block(lists.hist, b)[from], parts += at.of_block(lists.parts, b)[from];
-            }
-            part[q] = bin == kGroupBins - 1 ? 0.0 : by_count ? (double)count : In::sum_of(bin, count, parts).least;
+            part[q] = by_count ? (double)count[q] : (double)In::sum_of(tid * per + q, count[q], parts[q]).least;
             mine += part[q];
         }
         double before = team_before<T>(mine, sh);
@@ -1267,7 +1295,7 @@ __global__ void __launch_bounds__(T, T == 512 ? 2 : T == 256 ? 4 : 6) filter_ker
     bool counted = false;
     if (by_count || by_sum) {
         Search<E, T> search(x, c, t, sh, lists);
-        search.count(unmasked(), by_sum);
+        search.template count<true>(unmasked(), by_sum);
         counted = true;
         if (by_count) {
             search.reach(r.k);
