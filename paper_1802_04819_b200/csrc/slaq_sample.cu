@@ -68,8 +68,8 @@ __device__ __forceinline__ void write_none(const SampleArgs& a, int64_t row, int
 __device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < CUDART_INF_F; }
 
 // Weights in 32 bits: 2^t, t = x c - M with c = log2(e) / T rounded to 32 bits, M a whole number above m c, so that sums with another M are brought to
-// this one exactly.  A weight is off by the exponential's 2^-22 and by |t| ln 2 (2^-24 + 2^-25), t's rounding and c's (what c's puts on all weights
-// alike cancels).  Of the sum S of V weights the mean of |t| is at most log2(V / S): the entropy of the shares is at most that of equal ones.
+// this one exactly.  A weight is off by the exponential's 2^-22 and by |t| ln 2 times 2^-24, t's rounding, and c's (what c's puts on all weights alike
+// cancels).  Of the sum S of V weights the mean of |t| is at most log2(V / S): the entropy of the shares is at most that of equal ones.
 // Five additions in 32 bits lead to what is added up in 64.
 constexpr float kMostExponent = 4194304.0f;                    // 2^22: beyond, M is not above m c by a little
 struct Scale {
@@ -86,8 +86,8 @@ struct Scale {
 // Bounds of a sum's error: of its weights alike, and through their exponents.
 struct Error {
     double alike, exponents;
-    __device__ __forceinline__ Error(int V, double S)
-        : alike(5.0 * 5.97e-8 + 2.4e-7), exponents(6.3e-8 * fmax(log2((double)V / S), 0.0)) {}
+    __device__ __forceinline__ Error(int V, double S, const Scale& c)
+        : alike(5.0 * 5.97e-8 + 2.4e-7), exponents(0.6932 * (5.97e-8 + fabs(c.c / c.exact - 1.0)) * fmax(log2((double)V / S), 0.0)) {}
     __device__ __forceinline__ double both() const { return alike + exponents; }
     // .. of the difference between the sum up to a token and u times the sum, near 0: (1 - u) of the errors before it and u of those behind
     __device__ __forceinline__ double at(double u) const { return alike * 2.0 * u * (1.0 - u) + exponents * fmax(u, 1.0 - u) + 1e-15; }
@@ -96,25 +96,34 @@ struct Error {
 // Weights in 64 bits, of the largest 1: exp((x - m) / T) as 2^t, t = (x - m) c = k / 16 + f: a table of 2^(j / 16) and the series of 2^f
 // to its seventh term, |f ln 2| <= 0.0217 (the next is 4e-16).  What is less than 2^-1000 counts as 0.  exp() takes three times as long for a row: its
 // branches leave one weight at a time in work.
+//
+// The series' terms stand in constant memory, where an instruction finds them; as literals each takes two instructions of its own at every use (56
+// instructions a weight instead of 46).
 constexpr int kSteps = 16;
+constexpr double kLn2Wide = 0.6931471805599453;
+__constant__ double kSeries[8] = {1.0, kLn2Wide, kLn2Wide* kLn2Wide / 2.0, kLn2Wide* kLn2Wide* kLn2Wide / 6.0, kLn2Wide* kLn2Wide* kLn2Wide* kLn2Wide / 24.0,
+                                        kLn2Wide* kLn2Wide* kLn2Wide* kLn2Wide* kLn2Wide / 120.0,
+                                        kLn2Wide* kLn2Wide* kLn2Wide* kLn2Wide* kLn2Wide* kLn2Wide / 720.0, 422212465065984.0};   // .. and 1.5 x 2^48
 struct Exact {
     double c, m;
     float least;                   // 0 below
     const double* table;
     __device__ __forceinline__ Exact(float m, const Scale& s, const double* t)
         : c(s.exact), m(m), least((float)((double)m - 1000.0 / s.exact)), table(t) {}
-    __device__ __forceinline__ double weight(float x) const {
-        constexpr double kLn2 = 0.6931471805599453, kMagic = 422212465065984.0;   // 1.5 x 2^48: a 16th is its last place
-        const double d = (double)x - m, r = fma(d, c, kMagic), f = fma(d, c, kMagic - r);
+    // 0 if it is not wanted
+    __device__ __forceinline__ double weight(float x, bool wanted = true) const {
+        // r = (x - m) c + 1.5 x 2^48, whose last place is a 16th
+        const double d = (double)x - m, r = fma(d, c, kSeries[7]), f = fma(d, c, kSeries[7] - r);
         const int k = __double2loint(r);
-        double p = kLn2 * kLn2 * kLn2 * kLn2 * kLn2 * kLn2 / 720.0;
-        p = fma(p, f, kLn2 * kLn2 * kLn2 * kLn2 * kLn2 / 120.0);
-        p = fma(p, f, kLn2 * kLn2 * kLn2 * kLn2 / 24.0);
-        p = fma(p, f, kLn2 * kLn2 * kLn2 / 6.0);
-        p = fma(p, f, kLn2 * kLn2 / 2.0);
-        p = fma(p, f, kLn2);
-        p = fma(p, f, 1.0) * table[k & (kSteps - 1)];
-        return x >= least ? __hiloint2double(__double2hiint(p) + ((k >> 4) << 20), __double2loint(p)) : 0.0;
+        double p = kSeries[6];
+        p = fma(p, f, kSeries[5]);
+        p = fma(p, f, kSeries[4]);
+        p = fma(p, f, kSeries[3]);
+        p = fma(p, f, kSeries[2]);
+        p = fma(p, f, kSeries[1]);
+        p = fma(p, f, kSeries[0]) * table[k & (kSteps - 1)];
+        const bool on = wanted && x >= least;
+        return __hiloint2double(on ? __double2hiint(p) + ((k & -kSteps) << 16) : 0, on ? __double2loint(p) : 0);
     }
 };
 // 2^d for a whole number d <= 0, exactly; 0 far below
@@ -428,8 +437,7 @@ __device__ __forceinline__ double exact_sums(const Row<E>& x, const Exact& w, co
             float y, z;
             split(in.at(i), y, z);
             const bool keep_y = cut.keeps(y, x.first(v) + 2 * i), keep_z = cut.keeps(z, x.first(v) + 2 * i + 1);
-            const double a = w.weight(y), b = w.weight(z);
-            s += (keep_y ? a : 0.0) + (keep_z ? b : 0.0);
+            s += w.weight(y, keep_y) + w.weight(z, keep_z);
             n += keep_y + keep_z;
         }
     });
@@ -497,7 +505,7 @@ __device__ __forceinline__ void find(const Row<E>& x, const Runs& runs, int n_ru
 template <class E, int T>
 __device__ __forceinline__ void draw_exactly(const SampleArgs& a, int64_t row, const Row<E>& x, const Scale& c, const Exact& w, float u, const Cut& cut, double log2_S, double C,
                                              int kept, Shared<T>& sh) {
-    auto weight = [&](float y, int i) { return cut.keeps(y, i) ? w.weight(y) : 0.0; };
+    auto weight = [&](float y, int i) { return w.weight(y, cut.keeps(y, i)); };
     find<E, T>(x, Runs(x.vectors, T / 32), T / 32, u * C, sh, weight, [&](const Vector<E>& in, int v) {
         double s = 0.0;
 #pragma unroll 1
@@ -589,7 +597,7 @@ __global__ void __launch_bounds__(T) draw_kernel(SampleArgs a) {
         return;
     }
     if (c.holds(t.m)) {
-        const double target = r.u * t.S, margin = Error(a.vocab, t.S).at(r.u) * t.S;
+        const double target = r.u * t.S, margin = Error(a.vocab, t.S, c).at(r.u) * t.S;
         find<E, T>(x, runs, at.runs(), target, sh, [&](float y, int) { return (double)c.weight(y, t.M); },
                    [&](const Vector<E>& in, int) { return (double)weights_of_one(in, c, t.M); });
         const int token = sh.found;
@@ -777,18 +785,27 @@ struct Search {
         const int n = atomicAdd(&sh.listed, 1);
         if (n < kListed) lists.key[n] = key_of(y, i);
     }
+    // .. those elements of vector v of which the bits are set
+    __device__ __forceinline__ void append(const Vector<E>& in, int v, uint32_t which) {
+        if (!which) return;
+        int n = atomicAdd(&sh.listed, __popc(which));
+#pragma unroll 1
+        for (; which; which &= which - 1, ++n) {
+            const int e = __ffs(which) - 1;
+            float y, z;
+            split(in.at(e / 2), y, z);
+            if (n < kListed) lists.key[n] = key_of(e & 1 ? z : y, x.first(v) + e);
+        }
+    }
     // Everything down to interval `hi`, which is as much as a list holds.
     __device__ __forceinline__ void list(int hi) {
         set_all<T>(sh.listed, 0);
         over_single(x, begin(), end(), [&](const Vector<E>& in, int v) {
             if (bin(in.max()) > hi) return;
-#pragma unroll 1
-            for (int i = 0; i < Vector<E>::N / 2; ++i) {
-                float y, z;
-                split(in.at(i), y, z);
-                if (y > -CUDART_INF_F && bin(y) <= hi) append(y, x.first(v) + 2 * i);
-                if (z > -CUDART_INF_F && bin(z) <= hi) append(z, x.first(v) + 2 * i + 1);
-            }
+            uint32_t which = 0;
+#pragma unroll
+            for (int e = 0; e < Vector<E>::N; ++e) which |= (uint32_t)(in.one(e) > -CUDART_INF_F && bin(in.one(e)) <= hi) << e;
+            append(in, v, which);
         });
         __syncthreads();
     }
@@ -845,8 +862,8 @@ struct Search {
                 const int id = x.first(at) + 2 * q;
                 const int b_y = keeps<kAll>(in, y, id) ? bin(y) : kBins, b_z = keeps<kAll>(in, z, id + 1) ? bin(z) : kBins;
                 if (k == 0) {
-                    const double one = w.weight(y), two = w.weight(z);
-                    S += (b_y < kBins ? one : 0.0) + (b_z < kBins ? two : 0.0);
+                    const double one = w.weight(y, b_y < kBins), two = w.weight(z, b_z < kBins);
+                    S += one + two;
                     A += (b_y < lo ? one : 0.0) + (b_z < lo ? two : 0.0);
                 }
                 auto take = [&](float value, int i, int b) {
@@ -980,7 +997,7 @@ __device__ __noinline__ void draw_from_many(const SampleArgs& a, int64_t row, co
             about = exact_sums<E, T>(x, w, in, sh, n);
         } else {
             if (by_count) about = fast_sums<E, T>(x, c, t.M, in, sh, n);
-            error = Error(a.vocab, about).both();
+            error = Error(a.vocab, about, c).both();
             about *= to_largest;
         }
         if (by_count) search.template count<false>(in, true);
@@ -999,7 +1016,7 @@ __device__ __noinline__ void draw_from_many(const SampleArgs& a, int64_t row, co
     }
     if (holds && C != C) {
         C = fast_sums<E, T>(x, c, t.M, cut, sh, n);
-        const double target = r.u * C, margin = Error(a.vocab, C).at(r.u) * C;
+        const double target = r.u * C, margin = Error(a.vocab, C, c).at(r.u) * C;
         auto weight = [&](float y, int i) { return cut.keeps(y, i) ? c.weight(y, t.M) : 0.0f; };
         find<E, T>(x, search.runs, T / 32, target, sh, [&](float y, int i) { return (double)weight(y, i); }, [&](const Vector<E>& in, int v) {
             float sum[2] = {0.0f, 0.0f};
@@ -1056,7 +1073,7 @@ __device__ __noinline__ bool draw_from_list(const SampleArgs& a, int64_t row, co
         }
         int last = search.template reach_in_list<false>(L, 0.0, r.p * of);
         if (!by_count) {
-            const double margin = Error(a.vocab, t.S).both() * S;
+            const double margin = Error(a.vocab, t.S, c).both() * S;
             if (!all_sizes && sh.after < r.p * of - margin) return false;
             if (r.p * of - sh.before < margin || fabs(sh.after - r.p * of) < margin) {
                 int everything;
@@ -1303,7 +1320,7 @@ __global__ void __launch_bounds__(T, T == 512 ? 2 : T == 256 ? 4 : 6) filter_ker
         }
         if (holds && !by_count && by_sum) {
             const double S = t.S * exp2(-c.of_largest(t.m, t.M));
-            search.bracket(r.p * S, 2.0 * Error(a.vocab, t.S).both() * S);
+            search.bracket(r.p * S, 2.0 * Error(a.vocab, t.S, c).both() * S);
         }
         n = sh.before_it + sh.listed;
         if (holds && (by_count || by_sum) && n <= kListed) {
