@@ -379,18 +379,25 @@ int create(slaq_grad_norms_handle* h, void* dev_ws, size_t bytes, int32_t n_tens
     h->n_tensors = n_tensors, h->n_groups = n_groups;
     h->refs.resize((size_t)n_tensors);
     h->in_place.resize((size_t)n_tensors);
-    int sm = 0, per_norm = 0, per_apply = 0;
-    if (!done(cudaGetDevice(&h->device)) || !done(cudaDeviceGetAttribute(&sm, cudaDevAttrMultiProcessorCount, h->device)) ||
-        !done(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_norm, norm_kernel, kThreads, 0)) ||
-        !done(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_apply, apply_kernel, kThreads, 0)))
-        return SLAQ_E_CUDA;
     // units are numbered group by group
     std::vector<int64_t> first((size_t)n_groups + 1);
     for (int32_t t = 0; t < n_tensors; ++t) first[(size_t)tensors[t].group + 1] += units_of(tensors[t].n, tensors[t].type);
     for (int32_t k = 0; k < n_groups; ++k) first[(size_t)k + 1] += first[k];
     const int64_t n_units = first[n_groups];
-    auto grid = [&](int per) { return (int)std::max<int64_t>(1, std::min<int64_t>((n_units + kWarps - 1) / kWarps, (int64_t)sm * std::max(per, 1))); };
+    for (int32_t t = 0; t < n_tensors; ++t) {
+        const slaq_grad_tensor& x = tensors[t];
+        h->in_place[t] = !x.out || x.out == x.grad;
+        h->refs[t] = {x.grad, x.out ? x.out : const_cast<void*>(x.grad), x.n, x.group, 0, x.type, 0};
+    }
+    if (const int rc = check(h->refs, &h->err)) return rc;
+    int sm = 0, per_norm = 0, per_apply = 0;
+    if (!done(cudaGetDevice(&h->device)) || !done(cudaDeviceGetAttribute(&sm, cudaDevAttrMultiProcessorCount, h->device)) ||
+        !done(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_norm, norm_kernel, kThreads, 0)) ||
+        !done(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_apply, apply_kernel, kThreads, 0)))
+        return SLAQ_E_CUDA;
+    if (captured(st)) return SLAQ_E_ARG;
     h->n_units = (int32_t)n_units;
+    auto grid = [&](int per) { return (int)std::max<int64_t>(1, std::min<int64_t>((n_units + kWarps - 1) / kWarps, (int64_t)sm * std::max(per, 1))); };
     h->norm_grid = grid(per_norm), h->apply_grid = grid(per_apply);
     const int64_t warps = (int64_t)h->norm_grid * kWarps;
     std::vector<GroupRef> groups((size_t)n_groups);
@@ -403,13 +410,9 @@ int create(slaq_grad_norms_handle* h, void* dev_ws, size_t bytes, int32_t n_tens
     // A thread has eight sums in flight.
     h->team = place > (int64_t)n_groups * 256 ? kThreads : place > (int64_t)n_groups * 8 ? 32 : 1;
     for (int32_t t = 0; t < n_tensors; ++t) {
-        const slaq_grad_tensor& x = tensors[t];
-        h->in_place[t] = !x.out || x.out == x.grad;
-        h->refs[t] = {x.grad, x.out ? x.out : const_cast<void*>(x.grad), x.n, x.group, (int32_t)first[x.group], x.type, 0};
-        first[x.group] += units_of(x.n, x.type);
+        h->refs[t].first = (int32_t)first[tensors[t].group];
+        first[tensors[t].group] += units_of(tensors[t].n, tensors[t].type);
     }
-    if (const int rc = check(h->refs, &h->err)) return rc;
-    if (captured(st)) return SLAQ_E_ARG;
     const int64_t most = most_units(n_tensors, numels.data());
     const size_t need = layout(nullptr, nullptr, n_tensors, most, n_groups);
     if (dev_ws) {

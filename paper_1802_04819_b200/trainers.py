@@ -17,12 +17,13 @@ import numpy as np
 
 class SoftmaxJobs:
     """``n_jobs`` jobs of ``rows`` examples, ``features`` features (a constant one among them) and ``classes`` classes.  Labels
-    follow a random linear model with noise; learning rates are drawn log-uniform from ``rates``."""
+    follow a random linear model with noise; learning rates are drawn log-uniform from ``rates``.  With ``max_norm`` every job's
+    gradient is clipped to that norm."""
 
-    def __init__(self, n_jobs, rows=256, features=24, classes=10, rates=(2e-3, 5e-2), noise=1.0, state_bits=32, seed=0):
+    def __init__(self, n_jobs, rows=256, features=24, classes=10, rates=(2e-3, 5e-2), noise=1.0, state_bits=32, seed=0, max_norm=None):
         import torch
 
-        from .training import AdamW, job_row_grad
+        from .training import AdamW, GradNorms, job_row_grad
         g = torch.Generator(device="cuda").manual_seed(seed)
         draw = lambda *shape: torch.randn(*shape, generator=g, device="cuda")   # noqa: E731
         self.n_jobs, self.rows, self.classes = n_jobs, rows, classes
@@ -36,6 +37,14 @@ class SoftmaxJobs:
         self.row_grad = job_row_grad(self.offsets, self.labels)
         rate = torch.exp(math.log(rates[0]) + math.log(rates[1] / rates[0]) * torch.rand(n_jobs, generator=g, device="cuda")).tolist()
         self.adamw = AdamW(list(self.weights), list(self.grads), range(n_jobs), [dict(lr=r, weight_decay=0.0) for r in rate], state_bits=state_bits)
+        self.max_norm, self.norms = max_norm, None if max_norm is None else GradNorms(list(self.grads), range(n_jobs))
+
+    def _update(self, grad, active):
+        """The step of the weights for the gradient by the logits."""
+        import torch
+        torch.bmm(self.x.transpose(1, 2), grad.view(self.n_jobs, self.rows, self.classes), out=self.grads)
+        factors = None if self.norms is None else self.norms.measure(self.max_norm, active).factor
+        self.adamw.step(active, factors=factors)
 
     def step(self, active=None, losses=None):
         """One iteration of the jobs with an entry above 0 in ``active`` (int32 [n_jobs]; None: all).  Returns every job's loss before it
@@ -45,9 +54,8 @@ class SoftmaxJobs:
         from .training import job_losses, token_loss
         logits = torch.bmm(self.x, self.weights).view(-1, self.classes)
         logprob, grad = token_loss(logits, self.labels, self.row_grad, out=logits)
-        torch.bmm(self.x.transpose(1, 2), grad.view(self.n_jobs, self.rows, self.classes), out=self.grads)
         losses = job_losses(self.offsets, self.labels, logprob, out=losses)
-        self.adamw.step(active)
+        self._update(grad, active)
         return losses
 
     def histories(self, iterations):
@@ -57,6 +65,32 @@ class SoftmaxJobs:
         for k in range(iterations):
             self.step(losses=out[k])
         return out.t().contiguous().cpu().numpy()
+
+
+class RewardedJobs(SoftmaxJobs):
+    """The same jobs where nobody tells them the labels: in every iteration a job answers each of its examples with a class drawn from
+    its model and learns which answers were right (the policy gradient, with the job's mean reward as the baseline).  It reports the share of wrong answers."""
+
+    def __init__(self, n_jobs, temperature=1.0, seed=0, **more):
+        import torch
+        super().__init__(n_jobs, seed=seed, **more)
+        self.temperature = temperature
+        self.draws = torch.Generator(device="cuda").manual_seed(seed + 1)
+
+    def step(self, active=None, losses=None):
+        import torch
+
+        from .training import sample_tokens, token_loss
+        logits = torch.bmm(self.x, self.weights).view(-1, self.classes)
+        self.uniform = torch.rand(logits.shape[0], generator=self.draws, device="cuda")
+        self.answers = sample_tokens(logits, self.uniform, self.temperature)
+        right = (self.answers.token == self.labels).view(self.n_jobs, self.rows).float()
+        share = right.mean(1, keepdim=True)
+        row_grad = ((share - right) / self.rows).flatten()
+        _, grad = token_loss(logits, self.answers.token, row_grad, scale=1.0 / self.temperature, out=logits)
+        wrong = 1.0 - share[:, 0].double()
+        self._update(grad, active)
+        return wrong if losses is None else losses.copy_(wrong)
 
 
 def run(policy="slaq", n_jobs=64, epochs=80, total_cores=64, max_cores_per_job=16, epoch_seconds=3.0, max_hist=64, seed=0):
