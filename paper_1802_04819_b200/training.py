@@ -539,7 +539,13 @@ class GradNorms:
             rc = self._lib.slaq_grad_norms_create(self._ws.data_ptr(), need, n, table, n_groups, raw, ctypes.byref(self._h))
         _check(rc, {-1: "tensors that overlap, or a stream that is being captured"}.get(rc))
         self.grads, self.out, self._gpu, self._n_groups = grads, out, gpu, n_groups
+        self._written = self._counters(grads if out is None else out)
         self._streams = {raw}                       # those that the workspace is kept for
+
+    @staticmethod
+    def _counters(tensors):
+        """One tensor of each that count their changes together: views of one buffer do."""
+        return list({id(b): b for b in (t if t._base is None else t._base for t in tensors)}.values())
 
     def _ok(self, rc):
         return _check(rc, self._lib.slaq_grad_norms_last_error(self._h).decode() if rc < 0 else None)
@@ -589,7 +595,7 @@ class GradNorms:
         rc = _calls.grad_norms_apply(_at["grad_norms_apply"], self._h.value, a, f, self._here())
         if rc < 0:
             self._ok(rc)
-        _changed(self.grads if self.out is None else self.out)
+        _changed(self._written)
 
     def set_grads(self, grads, stream=None):
         """Other gradient tensors of the same types and sizes from the next call on."""
@@ -600,6 +606,8 @@ class GradNorms:
         with contextlib.nullcontext() if _is_here(stream, self._gpu) else _elsewhere(stream, self._gpu):
             self._ok(self._lib.slaq_grad_norms_set_grads(self._h, rows, self._here()))
         self.grads = grads
+        if self.out is None:
+            self._written = self._counters(grads)
 
     def close(self):
         if getattr(self, "_h", None):

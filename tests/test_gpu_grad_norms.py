@@ -269,6 +269,10 @@ def test_what_is_written_counts_as_changed(slaq):
     assert g._version == v
     plan.apply(torch.ones(1, device="cuda"))
     assert g._version == v + 1
+    flat = torch.ones(30, device="cuda")
+    parts, v = [flat[:10], flat[10:]], flat._version
+    slaq.GradNorms(parts).apply(torch.ones(1, device="cuda"))
+    assert flat._version == parts[0]._version == parts[1]._version == v + 1
     given = torch.empty(1, device="cuda")
     v = given._version
     slaq.GradNorms([g], out=[o]).measure(1.0, norm=given)
