@@ -1359,7 +1359,8 @@ __global__ void __launch_bounds__(256) narrow_kernel(SampleArgs a) {
 #pragma unroll
     for (int o = L / 2; o; o >>= 1) S += __shfl_xor_sync(~0u, S, o);
     bool keep = x > -CUDART_INF_F;
-    if (kFilter || greedy) {
+    // A warp has two rows, of which one may be greedy and the other not: all lanes take part in what lanes exchange.
+    if (kFilter || __any_sync(~0u, greedy)) {
         // how many are before this one in the row's order, and their sum
         int rank = 0;
         double before = 0.0;
@@ -1371,14 +1372,14 @@ __global__ void __launch_bounds__(256) narrow_kernel(SampleArgs a) {
             rank += earlier;
             if (earlier) before += v;
         }
-        if (kFilter && !greedy) {
-            keep = keep && (r.k <= 0 || rank < r.k);
-            double of = keep ? w : 0.0;
+        if (kFilter) {
+            const bool counts = keep && (r.k <= 0 || rank < r.k);
+            double of = counts ? w : 0.0;
 #pragma unroll
             for (int o = L / 2; o; o >>= 1) of += __shfl_xor_sync(~0u, of, o);
-            keep = keep && (rank == 0 || ((r.p >= 1.0f || before < r.p * of) && w >= r.q));
+            keep = counts && (rank == 0 || ((r.p >= 1.0f || before < r.p * of) && w >= r.q));
         }
-        if (greedy) keep = keep && rank == 0;
+        if (greedy) keep = x > -CUDART_INF_F && rank == 0;
     }
     // the running sum by id; the last token before which it does not exceed the target
     double upto = keep ? w : 0.0;
