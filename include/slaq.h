@@ -563,8 +563,8 @@ int slaq_token_loss(const void* d_logits, int type, int64_t rows, int32_t vocab,
  * Errors: as slaq_token_logprobs, with the numbers for all rows out of range SLAQ_E_ARG.
  */
 int slaq_sample_tokens(const void* d_logits, int type, int64_t rows, int32_t vocab, int64_t row_stride, const float* d_uniform,
-                       float temperature, const float* d_temperatures, int32_t top_k, const int32_t* d_top_ks, float top_p,
-                       const float* d_top_ps, float min_p, const float* d_min_ps, int64_t* d_out_token, float* d_out_logprob,
+                       double temperature, const float* d_temperatures, int32_t top_k, const int32_t* d_top_ks, double top_p,
+                       const float* d_top_ps, double min_p, const float* d_min_ps, int64_t* d_out_token, float* d_out_logprob,
                        float* d_out_kept_logprob, int32_t* d_out_kept, void* cuda_stream);
 
 /*

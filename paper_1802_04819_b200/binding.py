@@ -128,7 +128,7 @@ def load_library(variant: str | None = None):
         "slaq_token_logprobs": (c_int, [vp, c_int, c_int64, c_int32, c_int64, vp, c_float, vp, vp, vp, c_int32, vp, vp, vp]),
         "slaq_token_logprobs_grad": (c_int, [vp, c_int, c_int64, c_int32, c_int64, vp, c_float, vp, vp, vp, vp, vp, c_int64, vp]),
         "slaq_token_loss": (c_int, [vp, c_int, c_int64, c_int32, c_int64, vp, c_float, vp, vp, vp, c_int64, vp]),
-        "slaq_sample_tokens": (c_int, [vp, c_int, c_int64, c_int32, c_int64, vp, c_float, vp, c_int32, vp, c_float, vp, c_float, vp, vp, vp, vp, vp, vp]),
+        "slaq_sample_tokens": (c_int, [vp, c_int, c_int64, c_int32, c_int64, vp, c_double, vp, c_int32, vp, c_double, vp, c_double, vp, vp, vp, vp, vp, vp]),
         "slaq_job_row_grad": (c_int, [c_int32, vp, c_int64, vp, vp, vp, c_int32, vp]),
         "slaq_job_losses": (c_int, [c_int32, vp, c_int64, vp, vp, vp, vp, vp]),
         "slaq_append_token_losses": (c_int, [vp, c_int32, vp, vp, c_int64, vp, vp, vp, vp, vp, vp]),

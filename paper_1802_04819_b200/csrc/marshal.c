@@ -138,7 +138,7 @@ typedef int (*logprobs_fn)(const void*, int, int64_t, int32_t, int64_t, const in
 typedef int (*grad_fn)(const void*, int, int64_t, int32_t, int64_t, const int64_t*, float, const float*, const float*, const float*, const float*, void*,
                        int64_t, void*);
 typedef int (*loss_fn)(const void*, int, int64_t, int32_t, int64_t, const int64_t*, float, const float*, float*, void*, int64_t, void*);
-typedef int (*sample_fn)(const void*, int, int64_t, int32_t, int64_t, const float*, float, const float*, int32_t, const int32_t*, float, const float*, float,
+typedef int (*sample_fn)(const void*, int, int64_t, int32_t, int64_t, const float*, double, const float*, int32_t, const int32_t*, double, const float*, double,
                          const float*, int64_t*, float*, float*, int32_t*, void*);
 typedef int (*row_grad_fn)(int32_t, const int64_t*, int64_t, const int64_t*, const float*, float*, int32_t, void*);
 typedef int (*losses_fn)(int32_t, const int64_t*, int64_t, const int64_t*, const float*, const float*, double*, void*);
@@ -221,13 +221,13 @@ CALL(sample_tokens, 20, sample_fn, {
     const long long vocab = number_of(a[4]);
     const int64_t pitch = number_of(a[5]);
     const float* const uniform = pointer_of(a[6]);
-    const float temperature = (float)PyFloat_AsDouble(a[7]);
+    const double temperature = PyFloat_AsDouble(a[7]);
     const float* const temperatures = pointer_of(a[8]);
     const long long k = number_of(a[9]);
     const int32_t* const ks = pointer_of(a[10]);
-    const float p = (float)PyFloat_AsDouble(a[11]);
+    const double p = PyFloat_AsDouble(a[11]);
     const float* const ps = pointer_of(a[12]);
-    const float q = (float)PyFloat_AsDouble(a[13]);
+    const double q = PyFloat_AsDouble(a[13]);
     const float* const qs = pointer_of(a[14]);
     int64_t* const token = pointer_of(a[15]);
     float *const logprob = pointer_of(a[16]), *const kept_logprob = pointer_of(a[17]);

@@ -17,7 +17,7 @@ namespace slaq {
 namespace {
 
 constexpr int kMaxVocab = 1 << 22;
-constexpr float kMostTemperature = 1e30f, kLeastTemperature = 1e-30f;
+constexpr double kMostTemperature = 1.0000001e30, kLeastTemperature = 0.9999999e-30;   // 1e30 and 1e-30, rounded to 32 bits or not
 constexpr int kUnroll = 4;         // vectors that a lane has in flight
 
 struct SampleArgs {
@@ -29,7 +29,7 @@ struct SampleArgs {
     const int32_t* top_ks;
     const float* top_ps;
     const float* min_ps;
-    float temperature, top_p, min_p;
+    double temperature, top_p, min_p;
     int32_t top_k;
     int64_t* token;
     float *logprob, *kept_logprob;
@@ -38,7 +38,8 @@ struct SampleArgs {
 
 // A row's numbers.
 struct Asked {
-    float u, T, p, q;
+    float u;
+    double T, p, q;
     int k;
     int kind;                      // 0: to be drawn; 1: nobody asked; 2: numbers out of range
 };
@@ -46,11 +47,11 @@ template <bool kFilter>
 __device__ __forceinline__ Asked asked_of(const SampleArgs& a, int64_t row) {
     Asked r;
     r.u = a.uniform[row];
-    r.T = a.temperatures ? a.temperatures[row] : a.temperature;
+    r.T = a.temperatures ? (double)a.temperatures[row] : a.temperature;
     r.k = !kFilter ? 0 : a.top_ks ? a.top_ks[row] : a.top_k;
-    r.p = !kFilter ? 1.0f : a.top_ps ? a.top_ps[row] : a.top_p;
-    r.q = !kFilter ? 0.0f : a.min_ps ? a.min_ps[row] : a.min_p;
-    const bool ok = r.u < 1.0f && (r.T == 0.0f || (r.T >= kLeastTemperature && r.T <= kMostTemperature)) && r.p >= 0.0f && r.p <= 1.0f && r.q >= 0.0f && r.q <= 1.0f;
+    r.p = !kFilter ? 1.0 : a.top_ps ? (double)a.top_ps[row] : a.top_p;
+    r.q = !kFilter ? 0.0 : a.min_ps ? (double)a.min_ps[row] : a.min_p;
+    const bool ok = r.u < 1.0f && (r.T == 0.0 || (r.T >= kLeastTemperature && r.T <= kMostTemperature)) && r.p >= 0.0 && r.p <= 1.0 && r.q >= 0.0 && r.q <= 1.0;
     r.kind = r.u < 0.0f ? 1 : ok ? 0 : 2;
     return r;
 }
@@ -75,7 +76,7 @@ constexpr float kMostExponent = 4194304.0f;                    // 2^22: beyond, 
 struct Scale {
     double exact;                  // c before it is rounded
     float c;
-    __device__ __forceinline__ explicit Scale(float T) : exact(1.4426950408889634 / (double)T), c((float)exact) {}
+    __device__ __forceinline__ explicit Scale(double T) : exact(1.4426950408889634 / T), c((float)exact) {}
     __device__ __forceinline__ float base(float m) const { return m == -CUDART_INF_F ? 0.0f : ceilf(m * c) + 1.0f; }
     __device__ __forceinline__ float exponent(float x, float M) const { return fmaf(x, c, -M); }
     __device__ __forceinline__ float weight(float x, float M) const { return exp2_fast(exponent(x, M)); }
@@ -582,7 +583,7 @@ __global__ void __launch_bounds__(T) draw_kernel(SampleArgs a) {
         return;
     }
     const Row<E> x(static_cast<const E*>(a.logits) + row * a.stride, a.vocab);
-    const Scale c(r.T == 0.0f ? 1.0f : r.T);
+    const Scale c(r.T == 0.0 ? 1.0 : r.T);
     const Runs runs(x.vectors, at.runs());
     float most;
     double sum;
@@ -596,7 +597,7 @@ __global__ void __launch_bounds__(T) draw_kernel(SampleArgs a) {
         if (thread_index() == 0) write_none(a, row, 0, t.m);
         return;
     }
-    if (r.T == 0.0f) {
+    if (r.T == 0.0) {
         write_greedy<E, T>(a, row, x, t.m, sh);
         return;
     }
@@ -979,7 +980,7 @@ struct Search {
 template <class E, int T>
 __device__ __noinline__ void draw_from_many(const SampleArgs& a, int64_t row, const Row<E> x, const Scale c, const Asked r, const Total t, bool by_count, bool counted,
                                             Shared<T>& sh, Lists<T>& lists) {
-    const bool by_sum = r.p < 1.0f, by_size = r.q > 0.0f;
+    const bool by_sum = r.p < 1.0, by_size = r.q > 0.0;
     fill_table(sh);
     Search<E, T> search(x, c, t, sh, lists);
     const Exact& w = search.w;
@@ -1011,7 +1012,7 @@ __device__ __noinline__ void draw_from_many(const SampleArgs& a, int64_t row, co
         if (!by_count) log2_S = log2(of);
     }
     if (by_size) {
-        float f = __double2float_ru((double)t.m + (double)r.T * log((double)r.q));
+        float f = __double2float_ru((double)t.m + r.T * log(r.q));
         if (w.weight(f) < r.q) f = nextafterf(f, CUDART_INF_F);
         else if (w.weight(nextafterf(f, -CUDART_INF_F)) >= r.q) f = nextafterf(f, -CUDART_INF_F);
         const Cut least = {fminf(f, t.m), 0xFFFFFFFFu}, both = tighter(cut, least);
@@ -1049,7 +1050,7 @@ template <class E, int T>
 __device__ __noinline__ bool draw_from_list(const SampleArgs& a, int64_t row, const Row<E> x, const Scale c, const Asked r, const Total t, int n, bool by_count, bool all_sizes,
                                             Shared<T>& sh, Lists<T>& lists) {
     constexpr int kListed = Sizes<T>::kListed, kRanked = 256;
-    const bool by_sum = r.p < 1.0f, by_size = r.q > 0.0f;
+    const bool by_sum = r.p < 1.0, by_size = r.q > 0.0;
     const int tid = thread_index();
     if (n == 0) return false;
     fill_table(sh);
@@ -1167,8 +1168,8 @@ __global__ void __launch_bounds__(T, T == 512 ? 2 : T == 256 ? 4 : 6) filter_ker
         return;
     }
     const Row<E> x(static_cast<const E*>(a.logits) + row * a.stride, a.vocab);
-    const Scale c(r.T == 0.0f ? 1.0f : r.T);
-    const bool by_sum = r.p < 1.0f, by_size = r.q > 0.0f;
+    const Scale c(r.T == 0.0 ? 1.0 : r.T);
+    const bool by_sum = r.p < 1.0, by_size = r.q > 0.0;
     bool by_count = r.k > 0 && r.k < a.vocab;
     const Runs runs(x.vectors, at.runs());
     const int begin = runs.begin(at.run()), end = runs.end(at.run());
@@ -1200,7 +1201,7 @@ __global__ void __launch_bounds__(T, T == 512 ? 2 : T == 256 ? 4 : 6) filter_ker
 #pragma unroll
     for (int w = 1; w < T / 32; ++w) block_most = max_nan(block_most, (float)sh.more[w]);
     // The block's groups in intervals of their exponents with its own base.  Bases are whole numbers, so another's intervals are these, shifted.
-    const bool counting = r.T != 0.0f && (by_count || by_sum), here = is_finite(block_most) && c.holds(block_most);
+    const bool counting = r.T != 0.0 && (by_count || by_sum), here = is_finite(block_most) && c.holds(block_most);
     double block_sum = 0.0;
     if (counting) {
         const float M = c.base(block_most);
@@ -1261,10 +1262,10 @@ __global__ void __launch_bounds__(T, T == 512 ? 2 : T == 256 ? 4 : 6) filter_ker
     }
     bool all_sizes = false;
     if (by_size && !(by_count && by_sum) && is_finite(m)) {
-        const float q = __double2float_rd((double)m + (double)r.T * log((double)r.q) * 1.0000001);
+        const float q = __double2float_rd((double)m + r.T * log(r.q) * 1.0000001);
         if (q >= bound) bound = fminf(q, m), all_sizes = true;
     }
-    const bool listing = r.T != 0.0f && holds && (bound > -CUDART_INF_F || a.vocab <= kListed);
+    const bool listing = r.T != 0.0 && holds && (bound > -CUDART_INF_F || a.vocab <= kListed);
     if (listing) {
         int* const listed = at.of_block(&sh.listed, 0);
         uint16_t* const hit = reinterpret_cast<uint16_t*>(lists.id);
@@ -1310,7 +1311,7 @@ __global__ void __launch_bounds__(T, T == 512 ? 2 : T == 256 ? 4 : 6) filter_ker
         if (tid == 0) write_none(a, row, 0, t.m);
         return;
     }
-    if (r.T == 0.0f) {
+    if (r.T == 0.0) {
         write_greedy<E, T>(a, row, x, t.m, sh);
         return;
     }
@@ -1353,8 +1354,8 @@ __global__ void __launch_bounds__(256) narrow_kernel(SampleArgs a) {
     float m = x;
 #pragma unroll
     for (int o = L / 2; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(~0u, m, o));
-    const bool greedy = r.T == 0.0f, ok = is_finite(m);
-    const double z = ok && mine && x > -CUDART_INF_F ? ((double)x - (double)m) / (greedy ? 1.0 : (double)r.T) : -CUDART_INF;
+    const bool greedy = r.T == 0.0, ok = is_finite(m);
+    const double z = ok && mine && x > -CUDART_INF_F ? ((double)x - (double)m) / (greedy ? 1.0 : r.T) : -CUDART_INF;
     double w = exp(z), S = w;
 #pragma unroll
     for (int o = L / 2; o; o >>= 1) S += __shfl_xor_sync(~0u, S, o);
@@ -1377,7 +1378,7 @@ __global__ void __launch_bounds__(256) narrow_kernel(SampleArgs a) {
             double of = counts ? w : 0.0;
 #pragma unroll
             for (int o = L / 2; o; o >>= 1) of += __shfl_xor_sync(~0u, of, o);
-            keep = counts && (rank == 0 || ((r.p >= 1.0f || before < r.p * of) && w >= r.q));
+            keep = counts && (rank == 0 || ((r.p >= 1.0 || before < r.p * of) && w >= r.q));
         }
         if (greedy) keep = x > -CUDART_INF_F && rank == 0;
     }
@@ -1437,7 +1438,7 @@ __global__ void __launch_bounds__(128) middle_kernel(SampleArgs a) {
         if (lane == 0) write_none(a, row, 0, m);
         return;
     }
-    if (r.T == 0.0f) {
+    if (r.T == 0.0) {
         int first = 0x7FFFFFFF;
 #pragma unroll
         for (int j = N - 1; j >= 0; --j)
@@ -1489,7 +1490,7 @@ __global__ void __launch_bounds__(128) middle_kernel(SampleArgs a) {
             const uint32_t o = last_order(kSkip, [&](uint32_t y) { return at_least(y) >= r.k; });
             keep(o, r.k - at_least(o + (1u << kSkip)));
         }
-        if (r.p < 1.0f) {
+        if (r.p < 1.0) {
             auto sum_from = [&](uint32_t o) {
                 double s = 0.0;
 #pragma unroll
@@ -1504,7 +1505,7 @@ __global__ void __launch_bounds__(128) middle_kernel(SampleArgs a) {
             const double A = sum_from(above), each = exact.weight(value_of(o | (o >> 31 ? 0u : (1u << kSkip) - 1)));
             keep(o, (int)fmin(fmax(ceil((B - A) / each), 1.0), 1e9));
         }
-        if (r.q > 0.0f)
+        if (r.q > 0.0)
 #pragma unroll
             for (int j = 0; j < N; ++j)
                 if (w[j] < r.q) in &= ~(1u << j);
@@ -1606,15 +1607,15 @@ cudaError_t launch_sample(const SampleArgs& a, bool filter, cudaStream_t st) {
 }  // namespace slaq
 
 extern "C" int slaq_sample_tokens(const void* d_logits, int type, int64_t rows, int32_t vocab, int64_t row_stride, const float* d_uniform,
-                                  float temperature, const float* d_temperatures, int32_t top_k, const int32_t* d_top_ks, float top_p,
-                                  const float* d_top_ps, float min_p, const float* d_min_ps, int64_t* d_out_token, float* d_out_logprob,
+                                  double temperature, const float* d_temperatures, int32_t top_k, const int32_t* d_top_ks, double top_p,
+                                  const float* d_top_ps, double min_p, const float* d_min_ps, int64_t* d_out_token, float* d_out_logprob,
                                   float* d_out_kept_logprob, int32_t* d_out_kept, void* cuda_stream) {
     using namespace slaq;
     SampleArgs a = {d_logits, rows, row_stride, vocab, d_uniform, d_temperatures, d_top_ks, d_top_ps, d_min_ps, temperature, top_p, min_p, top_k,
                     d_out_token, d_out_logprob, d_out_kept_logprob, d_out_kept};
     if (type != SLAQ_F32 && type != SLAQ_BF16 && type != SLAQ_F16) return SLAQ_E_ARG;
-    auto share = [](float x) { return x >= 0.0f && x <= 1.0f; };
-    if (rows < 0 || vocab < 1 || (!d_temperatures && temperature != 0.0f && !(temperature >= kLeastTemperature && temperature <= kMostTemperature)) ||
+    auto share = [](double x) { return x >= 0.0 && x <= 1.0; };
+    if (rows < 0 || vocab < 1 || (!d_temperatures && temperature != 0.0 && !(temperature >= kLeastTemperature && temperature <= kMostTemperature)) ||
         (!d_top_ps && !share(top_p)) || (!d_min_ps && !share(min_p)))
         return SLAQ_E_ARG;
     if (vocab > kMaxVocab || rows > 0x7FFFFFFF) return SLAQ_E_RANGE;
@@ -1623,6 +1624,6 @@ extern "C" int slaq_sample_tokens(const void* d_logits, int type, int64_t rows, 
         !aligned(d_uniform, d_temperatures, d_top_ks, d_top_ps, d_min_ps, d_out_token, d_out_logprob, d_out_kept_logprob, d_out_kept))
         return SLAQ_E_ARG;
     if (rows == 0) return SLAQ_OK;
-    const bool filter = d_out_kept || d_top_ks || d_top_ps || d_min_ps || top_k > 0 || top_p < 1.0f || min_p > 0.0f;
+    const bool filter = d_out_kept || d_top_ks || d_top_ps || d_min_ps || top_k > 0 || top_p < 1.0 || min_p > 0.0;
     return by_type(type, [&](auto e) { return launch_sample<decltype(e)>(a, filter, static_cast<cudaStream_t>(cuda_stream)); });
 }

@@ -4,11 +4,11 @@ import math
 
 import numpy as np
 
-LIMITS = float(np.float32(1e-30)), float(np.float32(1e30))    # of a temperature, which is a number of 32 bits
+LIMITS = 0.9999999e-30, 1.0000001e30    # of a temperature: 1e-30 and 1e30, rounded to 32 bits or not
 
 def draw(x, u, T=1.0, k=0, p=1.0, q=0.0):
     """(token, logprob, kept_logprob, kept, distance): distance is how near the nearest decision was, relative to the sums."""
-    x, u, T, p, q = np.asarray(x, np.float64), float(np.float32(u)), float(np.float32(T)), float(np.float32(p)), float(np.float32(q))
+    x, u, T, p, q = np.asarray(x, np.float64), float(np.float32(u)), float(T), float(p), float(q)   # of rows' own: 32 bits already
     if u < 0:
         return -1, 0.0, 0.0, 0, 1.0
     if not (u < 1) or not (T == 0 or LIMITS[0] <= T <= LIMITS[1]) or not 0 <= p <= 1 or not 0 <= q <= 1 or np.isnan(x).any() or (x == np.inf).any():
@@ -27,7 +27,8 @@ def draw(x, u, T=1.0, k=0, p=1.0, q=0.0):
     if p < 1:
         B = p * sums[K - 1]
         L = min(K, int(np.searchsorted(sums[:K], B)) + 1)
-        near = np.abs(sums[:K] / B - 1).min() if B > 0 else 1.0
+        off = np.abs(sums[:K] / B - 1) if B > 0 else np.ones(1)
+        near = off[off > 0].min() if (off > 0).any() else 1.0     # equal to the border: whole weights, whose sums are exact
     L = max(1, min(L, int((w[order[:L]] >= q).sum())))
     kept = np.zeros(len(x), bool)
     kept[order[:L]] = True
