@@ -151,7 +151,7 @@ def _prepare_tensors(case, seed):
     # Some of the jobs are beyond their largest norm, and their gradients differ in size from layer to layer.
     group = torch.tensor(group_of, device="cuda")[tensor_of]
     per_group = torch.exp(1.5 * torch.randn(case["groups"], generator=g, device="cuda"))
-    elements = torch.zeros(case["groups"], dtype=torch.int64, device="cuda").index_add_(0, group, inside.sum(1))   # whole numbers: the same every time
+    elements = torch.zeros(case["groups"], device="cuda").index_add_(0, group, inside.sum(1).float())
     size = torch.exp(torch.randn(nb, 1, generator=g, device="cuda")) * (per_group / elements.sqrt())[group][:, None]
     st = dict(case, inside=inside, group=group, g=(flat(1.0) * size).to(t),
               active=torch.tensor([0 if case["idle"] and k % 5 == 4 else 1 + k % 3 for k in range(case["groups"])], dtype=torch.int32, device="cuda"))
