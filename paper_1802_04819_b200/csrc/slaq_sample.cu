@@ -77,7 +77,9 @@ struct Scale {
     double exact;                  // c before it is rounded
     float c;
     __device__ __forceinline__ explicit Scale(double T) : exact(1.4426950408889634 / T), c((float)exact) {}
-    __device__ __forceinline__ float base(float m) const { return m == -CUDART_INF_F ? 0.0f : ceilf(m * c) + 1.0f; }
+    // Not below -2^22: a row whose largest element lies there is not weighed in 32 bits, and in the others what does lie there (masked by a large finite
+    // number) weighs nothing, where a base of its own, a rounded one, would give it any weight.
+    __device__ __forceinline__ float base(float m) const { return m == -CUDART_INF_F ? 0.0f : fmaxf(ceilf(m * c) + 1.0f, -kMostExponent); }
     __device__ __forceinline__ float exponent(float x, float M) const { return fmaf(x, c, -M); }
     __device__ __forceinline__ float weight(float x, float M) const { return exp2_fast(exponent(x, M)); }
     __device__ __forceinline__ bool holds(float m) const { return fabsf(m * c) <= kMostExponent; }
