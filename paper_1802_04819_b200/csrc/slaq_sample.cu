@@ -107,12 +107,17 @@ constexpr double kLn2Wide = 0.6931471805599453;
 __constant__ double kSeries[8] = {1.0, kLn2Wide, kLn2Wide* kLn2Wide / 2.0, kLn2Wide* kLn2Wide* kLn2Wide / 6.0, kLn2Wide* kLn2Wide* kLn2Wide* kLn2Wide / 24.0,
                                         kLn2Wide* kLn2Wide* kLn2Wide* kLn2Wide* kLn2Wide / 120.0,
                                         kLn2Wide* kLn2Wide* kLn2Wide* kLn2Wide* kLn2Wide* kLn2Wide / 720.0, 422212465065984.0};   // .. and 1.5 x 2^48
+__device__ __forceinline__ float not_below(double x) {
+    float y;
+    asm("cvt.rp.f32.f64 %0, %1;" : "=f"(y) : "d"(x));
+    return y;
+}
 struct Exact {
     double c, m;
-    float least;                   // 0 below
+    float least;                   // 0 below.  Rounded up: no exponent is below -1000, whatever a step of 32-bit numbers beside m is worth, and -inf always is 0
     const double* table;
     __device__ __forceinline__ Exact(float m, const Scale& s, const double* t)
-        : c(s.exact), m(m), least((float)((double)m - 1000.0 / s.exact)), table(t) {}
+        : c(s.exact), m(m), least(not_below((double)m - 1000.0 / s.exact)), table(t) {}
     // 0 if it is not wanted
     __device__ __forceinline__ double weight(float x, bool wanted = true) const {
         // r = (x - m) c + 1.5 x 2^48, whose last place is a 16th
