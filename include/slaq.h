@@ -693,7 +693,7 @@ const char* slaq_grad_norms_last_error(const slaq_grad_norms_t* h);
 /*
  * Norms and factors, asynchronous on cuda_stream, one launch.  d_active as in slaq_adamw_step; a group that is not active is not read: norm
  * 0, factor 1.  scale: the gradients count as scale x what is stored (the grad_scale of the step that follows), finite in 32 bits.
- * max_norm >= 0, infinity for none; d_max_norms [n_groups] in its place where it is not NULL (NaN gives the factor NaN).
+ * max_norm >= 0, infinity for none; d_max_norms [n_groups] in its place where it is not NULL (what is NaN or negative gives the factor NaN).
  * d_out_norm [n_groups], d_out_factor [n_groups] or NULL.  A norm beyond 32 bits is infinity there, its factor is not.
  * Calls of one plan must run one after the other (one stream, or ordered streams), replayed graphs included.  The sums are always
  * added in the same order.  Errors: SLAQ_E_ARG, SLAQ_E_CUDA.

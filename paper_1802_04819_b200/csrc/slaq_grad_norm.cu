@@ -133,7 +133,7 @@ __device__ __forceinline__ double warp_sum(double x) {
 __device__ __forceinline__ void write_norm(const NormArgs& a, int g, double sum) {
     const double norm = sqrt(sum) * a.scale, most = a.mosts ? (double)a.mosts[g] : a.most;
     a.norm[g] = (float)norm;
-    if (a.factor) a.factor[g] = !(norm < CUDART_INF) || most != most ? CUDART_NAN_F : norm > most ? (float)(most / norm) : 1.0f;
+    if (a.factor) a.factor[g] = !(norm < CUDART_INF) || !(most >= 0.0) ? CUDART_NAN_F : norm > most ? (float)(most / norm) : 1.0f;
 }
 
 // 209 M bf16 in 300 tensors: 63 us (6.6 TB/s, 101 % of a copy); with the rare sum in 64 bits inline, which took the vectors out of registers, 115.  320

@@ -565,7 +565,8 @@ class GradNorms:
 
     def measure(self, max_norm=math.inf, active=None, scale: float = 1.0, norm=None, factor=None, stream=None) -> GradNorm:
         """Norms of the groups whose entry of ``active`` (int32 [groups]) is above 0, None: of all, and the factors that bring
-        them down to ``max_norm``: a number, or float32 [groups] on the GPU.  The gradients count as ``scale`` times what is stored.
+        them down to ``max_norm``: a number, or float32 [groups] on the GPU (an entry that is negative or NaN gives the factor NaN, which
+        leaves its group alone).  The gradients count as ``scale`` times what is stored.
         A group that is not active has norm 0 and factor 1.  ``norm`` and ``factor`` may be given (float32 [groups])."""
         if not _is_here(stream, self._gpu):
             with _elsewhere(stream, self._gpu):
