@@ -669,7 +669,7 @@ int slaq_adamw_get_steps(slaq_adamw_t* h, int64_t* out_steps, void* cuda_stream)
  */
 typedef struct slaq_grad_tensor {
     const void* grad;
-    void* out;               /* where slaq_grad_norms_apply puts the product, of the same type; NULL: in place */
+    void* out;               /* where slaq_grad_norms_apply puts the product, of the same type, whatever the gradient; NULL: in place */
     int64_t n;               /* elements; 0 is allowed, its pointers are not looked at then */
     int32_t group;
     int32_t type;            /* of this tensor: they may differ */

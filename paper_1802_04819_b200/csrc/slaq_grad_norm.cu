@@ -390,7 +390,7 @@ int create(slaq_grad_norms_handle* h, void* dev_ws, size_t bytes, int32_t n_tens
     const int64_t n_units = first[n_groups];
     for (int32_t t = 0; t < n_tensors; ++t) {
         const slaq_grad_tensor& x = tensors[t];
-        h->in_place[t] = !x.out || x.out == x.grad;
+        h->in_place[t] = !x.out;
         h->refs[t] = {x.grad, x.out ? x.out : const_cast<void*>(x.grad), x.n, x.group, 0, x.type, 0};
     }
     if (const int rc = check(h->refs, &h->err)) return rc;
