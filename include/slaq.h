@@ -680,7 +680,8 @@ typedef struct slaq_grad_norms_handle slaq_grad_norms_t;
  * Make a plan.  dev_ws as in slaq_adamw_create, slaq_grad_norms_workspace_bytes() long.  Host array; the call returns when the plan is on
  * the device and must not be captured.  Any alignment that suits the types will do.
  * Errors: SLAQ_E_ARG (null, an unknown type, a group out of range, what apply writes overlapping itself or a gradient that is not
- * written in place, a stream that is captured), SLAQ_E_RANGE (more than 2^38 elements), SLAQ_E_NOMEM, SLAQ_E_CUDA.
+ * written in place, a stream that is captured), SLAQ_E_RANGE (more than 2^38 elements, 2^30 tensors or 2^30 groups),
+ * SLAQ_E_NOMEM, SLAQ_E_CUDA.
  */
 int slaq_grad_norms_create(void* dev_ws, size_t bytes, int32_t n_tensors, const slaq_grad_tensor* tensors, int32_t n_groups,
                            void* cuda_stream, slaq_grad_norms_t** out);

@@ -343,7 +343,10 @@ int64_t most_units(int32_t n_tensors, const int64_t* numels) {
     for (int32_t t = 0; t < n_tensors; ++t) n += units_of(numels[t], SLAQ_F32);
     return n;
 }
-bool sizes_ok(int32_t n_tensors, const int64_t* numels) {
+// Units, and the steps of blocks and warps beyond them and beyond the groups, are counted in 31 bits.
+constexpr int32_t kMost = 1 << 30;       // tensors, or groups
+bool sizes_ok(int32_t n_tensors, const int64_t* numels, int32_t n_groups) {
+    if (n_tensors > kMost || n_groups > kMost) return false;
     int64_t n = 0;
     for (int32_t t = 0; t < n_tensors; ++t) {
         if (numels[t] < 0 || numels[t] > kMostElements) return false;
@@ -379,7 +382,7 @@ int create(slaq_grad_norms_handle* h, void* dev_ws, size_t bytes, int32_t n_tens
         if (x.n < 0 || x.group < 0 || x.group >= n_groups || (x.type != SLAQ_F32 && x.type != SLAQ_BF16 && x.type != SLAQ_F16)) return SLAQ_E_ARG;
         numels[t] = x.n;
     }
-    if (!sizes_ok(n_tensors, numels.data())) return SLAQ_E_RANGE;
+    if (!sizes_ok(n_tensors, numels.data(), n_groups)) return SLAQ_E_RANGE;
     h->n_tensors = n_tensors, h->n_groups = n_groups;
     h->refs.resize((size_t)n_tensors);
     h->in_place.resize((size_t)n_tensors);
@@ -441,7 +444,7 @@ int create(slaq_grad_norms_handle* h, void* dev_ws, size_t bytes, int32_t n_tens
 extern "C" {
 
 size_t slaq_grad_norms_workspace_bytes(int32_t n_tensors, const int64_t* numels, int32_t n_groups) {
-    if (n_tensors < 0 || n_groups < 1 || (n_tensors && !numels) || !slaq::sizes_ok(n_tensors, numels)) return 0;
+    if (n_tensors < 0 || n_groups < 1 || (n_tensors && !numels) || !slaq::sizes_ok(n_tensors, numels, n_groups)) return 0;
     return slaq::layout(nullptr, nullptr, n_tensors, slaq::most_units(n_tensors, numels), n_groups);
 }
 

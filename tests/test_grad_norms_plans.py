@@ -54,3 +54,14 @@ def test_a_given_output_stays_where_it_is(fake):
     assert fake.slaq_grad_norms_set_grads(h, rows(C, B), None) == 0
     assert fake.slaq_grad_norms_set_grads(h, rows(A, C), None) == 0
     fake.slaq_grad_norms_destroy(h)
+
+
+def test_how_many_groups_a_plan_may_have(lib):
+    """2^30: the groups' numbers, and what a block's threads add to them, stay within 31 bits."""
+    one = (c_int64 * 1)(10)
+    assert lib.slaq_grad_norms_workspace_bytes(1, one, 1 << 30) > 1 << 34
+    for groups in ((1 << 30) + 1, (1 << 31) - 300, (1 << 31) - 1):
+        assert lib.slaq_grad_norms_workspace_bytes(1, one, groups) == 0
+        h = c_void_p(1)
+        assert lib.slaq_grad_norms_create(None, 0, 1, _tensors((A, None)), groups, None, byref(h)) == -2
+        assert h.value is None
