@@ -112,6 +112,11 @@ __device__ __forceinline__ float not_below(double x) {
     asm("cvt.rp.f32.f64 %0, %1;" : "=f"(y) : "d"(x));
     return y;
 }
+__device__ __forceinline__ float not_above(double x) {
+    float y;
+    asm("cvt.rm.f32.f64 %0, %1;" : "=f"(y) : "d"(x));
+    return y;
+}
 struct Exact {
     double c, m;
     float least;                   // 0 below.  Rounded up: no exponent is below -1000, whatever a step of 32-bit numbers beside m is worth, and -inf always is 0
@@ -983,6 +988,21 @@ struct Search {
     }
 };
 
+// Where weights, as 64 bits hold them, reach min_p: m + T ln q, and near 1, where many logits have the weight 1, as far below as that rounding goes.  Nothing
+// below the first reaches it, everything from the second on does.
+__device__ __forceinline__ float below_min_p(const Asked& r, float m) { return fminf(not_above((double)m + r.T * (log(r.q) * 1.0000001 - 4e-15)), m); }
+__device__ __forceinline__ float above_min_p(const Asked& r, float m) { return fminf(not_below((double)m + r.T * (log(r.q) * 0.9999999 + 4e-15)), m); }
+// The lowest logit that reaches it: a few trials
+__device__ __forceinline__ float least_of(const Exact& w, const Asked& r, float m) {
+    uint32_t lo = order_of(below_min_p(r, m)), hi = order_of(above_min_p(r, m));
+    while (lo < hi) {
+        const uint32_t middle = lo + (hi - lo) / 2;
+        if (w.weight(value_of(middle)) >= r.q) hi = middle;
+        else lo = middle + 1;
+    }
+    return value_of(hi);
+}
+
 // Rows of which more is kept than a list holds.  `counted`: by_count's, or of everything, are the counts that the search has.
 template <class E, int T>
 __device__ __noinline__ void draw_from_many(const SampleArgs& a, int64_t row, const Row<E> x, const Scale c, const Asked r, const Total t, bool by_count, bool counted,
@@ -1019,10 +1039,7 @@ __device__ __noinline__ void draw_from_many(const SampleArgs& a, int64_t row, co
         if (!by_count) log2_S = log2(of);
     }
     if (by_size) {
-        float f = __double2float_ru((double)t.m + r.T * log(r.q));
-        if (w.weight(f) < r.q) f = nextafterf(f, CUDART_INF_F);
-        else if (w.weight(nextafterf(f, -CUDART_INF_F)) >= r.q) f = nextafterf(f, -CUDART_INF_F);
-        const Cut least = {fminf(f, t.m), 0xFFFFFFFFu}, both = tighter(cut, least);
+        const Cut least = {least_of(w, r, t.m), 0xFFFFFFFFu}, both = tighter(cut, least);
         if (both.value != cut.value || both.last != cut.last) C = CUDART_NAN;
         cut = both;
     }
@@ -1269,8 +1286,8 @@ __global__ void __launch_bounds__(T, T == 512 ? 2 : T == 256 ? 4 : 6) filter_ker
     }
     bool all_sizes = false;
     if (by_size && !(by_count && by_sum) && is_finite(m)) {
-        const float q = __double2float_rd((double)m + r.T * log(r.q) * 1.0000001);
-        if (q >= bound) bound = fminf(q, m), all_sizes = true;
+        const float q = below_min_p(r, m);
+        if (q >= bound) bound = q, all_sizes = true;
     }
     const bool listing = r.T != 0.0 && holds && (bound > -CUDART_INF_F || a.vocab <= kListed);
     if (listing) {
