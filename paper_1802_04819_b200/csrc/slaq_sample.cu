@@ -139,6 +139,12 @@ struct Exact {
         return __hiloint2double(on ? __double2hiint(p) + ((k & -kSteps) << 16) : 0, on ? __double2loint(p) : 0);
     }
 };
+// p S, rounded: it is not merged with the difference that is taken from it, so that a share of equal weights that comes out whole is the same in every kernel
+__device__ __forceinline__ double share_of(double p, double S) {
+    double x;
+    asm("mul.rn.f64 %0, %1, %2;" : "=d"(x) : "d"(p), "d"(S));
+    return x;
+}
 // 2^d for a whole number d <= 0, exactly; 0 far below
 __device__ __forceinline__ double power(float d) { return d > -1000.0f ? __hiloint2double((1023 + (int)d) << 20, 0) : 0.0; }
 
@@ -893,7 +899,7 @@ struct Search {
         });
         if (k == 0) {
             of = team_sum<T>(S, sh);
-            B = p * of;
+            B = share_of(p, of);
             A = warp_sum(A);
             if ((threadIdx.x & 31) == 0) sh.sum[warp_index()] = A;
             __syncthreads();
@@ -1521,7 +1527,7 @@ __global__ void __launch_bounds__(128) middle_kernel(SampleArgs a) {
                 for (int j = 0; j < N; ++j) s += order[j] >= o && (in >> j & 1) ? w[j] : 0.0;
                 return warp_sum(s);
             };
-            const double B = r.p * sum_from(0);
+            const double B = share_of(r.p, sum_from(0));
             // the row's largest, if none is wanted
             const uint32_t top = order_of(m) >> kSkip << kSkip;
             const uint32_t o = B > 0.0 ? last_order(kSkip, [&](uint32_t y) { return sum_from(y) >= B; }) : top;
