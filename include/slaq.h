@@ -547,7 +547,8 @@ int slaq_token_loss(const void* d_logits, int type, int64_t rows, int32_t vocab,
 
 /*
  * Tokens drawn from rows of logits (as above) with given random numbers.  With m the row's largest logit x, T its temperature:
- * w_i = exp((x_i - m) / T), in 64 bits; the order of a row is that of falling logits, equal ones lowest id first.
+ * w_i = exp((x_i - m) / T), in 64 bits (less than 2^-1000 may count as 0); the order of a row is that of falling logits, equal ones
+ * lowest id first.
  *   K = the first top_k of the order (0 or less, or more than there are: all that are not -inf), S their sum of w;
  *   kept = of these the shortest beginning of the order whose sum reaches top_p S, at least one token (1: all of K), and of that the tokens
  *   with w >= min_p (0: all);
@@ -692,7 +693,7 @@ int slaq_grad_norms_destroy(slaq_grad_norms_t* h);
 /* Message for the last error of h. */
 const char* slaq_grad_norms_last_error(const slaq_grad_norms_t* h);
 /*
- * Norms and factors, asynchronous on cuda_stream, one launch.  d_active as in slaq_adamw_step; a group that is not active is not read: norm
+ * Norms and factors, asynchronous on cuda_stream, one launch, or two where there are many groups.  d_active as in slaq_adamw_step; a group that is not active is not read: norm
  * 0, factor 1.  scale: the gradients count as scale x what is stored (the grad_scale of the step that follows), finite in 32 bits.
  * max_norm >= 0, infinity for none; d_max_norms [n_groups] in its place where it is not NULL (what is NaN or negative gives the factor NaN).
  * d_out_norm [n_groups], d_out_factor [n_groups] or NULL.  A norm beyond 32 bits is infinity there, its factor is not.
@@ -702,7 +703,7 @@ const char* slaq_grad_norms_last_error(const slaq_grad_norms_t* h);
 int slaq_grad_norms_measure(slaq_grad_norms_t* h, const int32_t* d_active, double scale, double max_norm, const float* d_max_norms,
                             float* d_out_norm, float* d_out_factor, void* cuda_stream);
 /*
- * out = grad x d_factor[group], rounded once to the type.  Groups that are not active, or whose factor is NaN, stay as they are, and so do
+ * out = grad x d_factor[group], the product in 32 bits, and that rounded to the type.  Groups that are not active, or whose factor is NaN, stay as they are, and so do
  * gradients in place whose factor is 1.  Errors: SLAQ_E_ARG, SLAQ_E_CUDA.
  */
 int slaq_grad_norms_apply(slaq_grad_norms_t* h, const int32_t* d_active, const float* d_factor, void* cuda_stream);

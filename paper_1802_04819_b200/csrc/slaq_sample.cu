@@ -1174,7 +1174,7 @@ __device__ __noinline__ bool draw_from_list(const SampleArgs& a, int64_t row, co
 // reaches such a bound is in the few groups whose largest does: those are read once more, and what reaches it is listed.  Where
 // that fails, the row's elements are counted, and listed if the counts allow it.
 //
-// 4,096 x 128,000 bf16, top 50: 270 us, of a row's 68,000 cycles (four at a time on an SM) 40,000 go to reading it, 12,000 to the bound, 8,000 to the
+// 4,096 x 128,000 bf16, top 50: 270 to 295 us by the rows' likely tokens, of a row's 68,000 cycles (four at a time on an SM) 40,000 go to reading it, 12,000 to the bound, 8,000 to the
 // list, 8,000 to the draw: latencies of a few dozen barriers.  Rows that keep thousands take ten times that: counting 40,000 cycles a row, 64-bit sums 110,000.
 template <class E, int T>
 __global__ void __launch_bounds__(T, T == 512 ? 2 : T == 256 ? 4 : 6) filter_kernel(SampleArgs a) {
@@ -1613,10 +1613,13 @@ cudaError_t launch_narrow(const SampleArgs& a, cudaStream_t st) {
     if (a.vocab <= 16) return launch(narrow_kernel<E, 16, kFilter>, (a.rows + 15) / 16, 256, 0, 1, st, a);
     return launch(narrow_kernel<E, 32, kFilter>, (a.rows + 7) / 8, 256, 0, 1, st, a);
 }
-// Up to 32 tokens have a lane each (200,000 x 10 fp32: 49 us, with a share 80; a block to a row 367 and 2,769), up to 1,024 a warp's registers (60,000 x 400
-// bf16: 78 us, with a share 319; in blocks 129 and 1,893).  Beyond, with more rows than SMs, blocks of 256: four on an SM hide one another's
+// Up to 32 tokens have a lane each (200,000 x 10 fp32: 51 us, with a share 85; a block to a row 367 and 2,769), up to 1,024 a warp's registers (60,000 x 400
+// bf16: 77 us, with a share 321; in blocks 129 and 1,893).  Beyond, with more rows than SMs, blocks of 256: four on an SM hide one another's
 // ends.  512 x 65,536 bf16: top 40 28 us, the whole distribution 52; with 512 threads 41 and 42, with 128 30 and 94.  4,096 x 128,000: 270 and 269,
-// with 512 threads 350 and 283, with 128 277 and 390.  With fewer rows a cluster shares one: 64 x 130,001 fp32 11 us, a block alone 15.
+// with 512 threads 350 and 283, with 128 277 and 390.  Up to 2,048 vectors and for more than two rows an SM, blocks of 128, in which less waits for less: 20,000 x
+// 5,000 bf16, whole, top 50 and a share of 0.9, 112, 355 and 1,018 us, with 256 threads 164, 538 and 1,118; 20,000 x 1,100 80, 343 and 695 (146, 526, 891).  At
+// 6,000 x 16,000 71, 130 and 539 (75, 186, 525), but for flat rows, which keep most of their tokens, 73, 132 and 1,028 (77, 186, 722).  300 x 5,000: 16, 15 and 54
+// (13, 17, 42).  With fewer rows a cluster shares one: 64 x 130,001 fp32 11 us, a block alone 15.
 template <class E>
 cudaError_t launch_sample(const SampleArgs& a, bool filter, cudaStream_t st) {
     if (a.vocab <= 32) return filter ? launch_narrow<E, true>(a, st) : launch_narrow<E, false>(a, st);
